@@ -339,6 +339,106 @@ BITRL_API bitrl_status bitrl_bitlinear5_forward_multi(int32_t count, const bitrl
                                                       const void* const* x, void* const* y, int32_t M,
                                                       int32_t out_dtype, void* stream);
 
+/* ---- a paged key/value cache: attention over an episode, drafted trees, eviction -------------------------------
+ * (The paper encodes every state on its own, Eq. 3; an agent whose state is the episode so far keeps the keys and
+ * values of the tokens that it has read.  The paper has no counterpart; the attention is that of bitrl_attention.)
+ * A cache holds, for each of n_layers blocks, n_pages pages of page_tokens tokens:
+ *   k, v: dev bf16 [n_layers, n_pages, n_kv_heads, page_tokens, head_dim]      (keys after the rotary embedding)
+ *   mass: dev fp32 [n_layers, n_pages, n_kv_heads, page_tokens], the attention weight that a slot has received, or NULL
+ *   pos:  dev int32, same shape, the position of the token in the slot
+ * Slot t of sequence s is row t % page_tokens of page page_table[s, t / page_tokens] in every layer;
+ * page_table: dev int32 [n_seq, max_pages] (entries that no slot in use needs are never read as pages).
+ * used: dev int32 [n_seq], slots in use; seen: dev int32 [n_seq], tokens that the sequence has read so far (the position
+ * of its next token; larger than used once slots have been evicted).  Both are read by every call below and changed by
+ * bitrl_kv_advance alone, so that the calls of one step, layer by layer, all see the same state.
+ * page_tokens is 16, 32, 64 or 128; head_dim 64 or 128.  Sequences may share pages for reading; a page that a call
+ * writes (new tokens, weights, moved rows) must belong to one sequence.
+ *
+ * New tokens: sequence s has the tokens state_off[s] .. state_off[s+1]-1 of the batch (dev int32 [n_seq + 1], ascending
+ * from 0, at most max_new_len each; none is allowed), or, with state_off NULL, max_new_len tokens each (T = n_seq *
+ * max_new_len).  Rows of the batch behind the last sequence are left as they are.  New token i of s takes slot used[s] + i.
+ * parent: NULL, then every new token sees all earlier ones; or dev int32 [T], a tree of drafted tokens: the index (inside
+ * the sequence's new tokens) of the token that it continues, smaller than its own, BITRL_PARENT_PAST for a token that
+ * continues the cached ones, BITRL_PARENT_PAD for a place that holds no token.  A tree has at most BITRL_TREE_MAX_TOKENS.
+ * anc(i) = i and the tokens above it; depth(i) = |anc(i)| - 1 (= i without a tree).
+ * What is wrong on the device (offsets, a parent that is not an earlier token, a page out of range, more slots than
+ * max_pages hold) makes a call skip that sequence, and the next bitrl_poll_status returns BITRL_ERR_SHAPE. */
+#define BITRL_TREE_MAX_TOKENS 256
+#define BITRL_KV_MAX_SLOTS (1 << 19) /* max_pages * page_tokens at most; beyond it BITRL_ERR_LIMIT */
+#define BITRL_PARENT_PAST (-1)
+#define BITRL_PARENT_PAD (-2)
+typedef struct bitrl_kv_cache {
+  void* k;
+  void* v;
+  float* mass;
+  int32_t* pos;
+  const int32_t* page_table;
+  int32_t* used;
+  int32_t* seen;
+  int32_t n_layers, n_pages, n_kv_heads, page_tokens, head_dim, n_seq, max_pages;
+} bitrl_kv_cache_t;
+
+/* Appends the new tokens to layer `layer`: q and k of qkv (dev bf16 [T, (n_heads + 2 n_kv_heads) * head_dim] = [q|k|v]) are
+ * rotated by their position seen[s] + depth(i), as for bitrl_attention (angles in fp64, rotation in fp32, one rounding to
+ * bf16); q goes to q_out (dev bf16 [T, n_heads * head_dim]), k and v to their slots, mass becomes 0, pos the position.
+ * Padding writes nothing. */
+BITRL_API bitrl_status bitrl_kv_append(const bitrl_kv_cache_t* cache, int32_t layer, const void* qkv, int32_t T,
+                                       const int32_t* state_off, int32_t max_new_len, const int32_t* parent,
+                                       int32_t n_heads, double theta, void* q_out, void* stream);
+
+/* Attention of the new tokens, already appended, over the cached slots and over one another:
+ *   token i of s sees A(i) = {slots 0 .. used[s]-1} and {slots used[s] + j : j in anc(i)}
+ *   p_r = softmax over r in A(i) of q_i . k_r / sqrt(head_dim);  att_i = sum_r p_r v_r           per query head
+ *   mass[slot r] += sum over the tokens and over the query heads of the kv head of p_r           if accumulate_mass
+ * Query head h reads kv head h / (n_heads / n_kv_heads).  q, att: dev bf16 [T, n_heads * head_dim].  Padding gets zeros
+ * and adds nothing; a slot that a token does not see has no part in its result, whatever it holds.  Scores, softmax
+ * statistics, the sums over keys and mass are fp32; att is rounded once to bf16.  Weights that enter the product with the
+ * values through the tensor cores are rounded to bf16 beforehand where more than 16 rows share a tile.  The same call
+ * gives the same bits: every sum has a fixed order.
+ * workspace: dev, >= bitrl_attention_cached_workspace_bytes(cache, T, max_new_len, n_heads). */
+BITRL_API size_t bitrl_attention_cached_workspace_bytes(const bitrl_kv_cache_t* cache, int32_t T, int32_t max_new_len,
+                                                        int32_t n_heads);
+BITRL_API bitrl_status bitrl_attention_cached(const bitrl_kv_cache_t* cache, int32_t layer, const void* q, int32_t T,
+                                              const int32_t* state_off, int32_t max_new_len, const int32_t* parent,
+                                              int32_t n_heads, int32_t accumulate_mass, void* att, void* workspace,
+                                              size_t workspace_bytes, void* stream);
+
+/* Which rows an eviction to `budget` slots has to move, for every layer, sequence and kv head.  Where used[s] > budget, the
+ * budget slots that stay are the greatest by (protected, mass, lower slot first); a slot is protected when its pos is
+ * >= seen[s] - recent or < sink; a NaN weight ranks below every number.  The slots >= budget that stay move into the slots < budget
+ * that do not, in ascending order: moves[l,s,h,i] = (source slot, destination slot), count[l,s,h] of them; the rest of
+ * moves is left as it is.  Nothing in the cache changes: bitrl_kv_move carries the plan out and bitrl_kv_advance sets used.
+ * moves: dev int32 [n_layers, n_seq, n_kv_heads, max_moves, 2], max_moves >= min(budget, max_pages * page_tokens - budget);
+ * count: dev int32 [n_layers, n_seq, n_kv_heads].  1 <= budget; recent, sink >= 0. */
+BITRL_API bitrl_status bitrl_kv_evict_plan(const bitrl_kv_cache_t* cache, int32_t budget, int32_t recent, int32_t sink,
+                                           int32_t max_moves, int32_t* moves, int32_t* count, void* stream);
+
+/* Moves rows (k, v, mass, pos) inside the cache: for every layer, sequence and kv head the `count` first pairs of its list
+ * (source slot, destination slot), as if every source were read before any destination is written.  In a list sources and
+ * destinations are each strictly ascending and no destination is above its source.  per_head != 0: lists as
+ * bitrl_kv_evict_plan makes them; 0: moves dev int32 [n_seq, max_moves, 2] and count dev int32 [n_seq], the same for
+ * every layer and kv head (the accepted branch of a drafted tree: (used + place of the i-th accepted token, used + i)). */
+BITRL_API bitrl_status bitrl_kv_move(const bitrl_kv_cache_t* cache, const int32_t* moves, const int32_t* count,
+                                     int32_t max_moves, int32_t per_head, void* stream);
+
+/* After all layers of a step: n = new tokens of s (state_off, max_new_len as above), or n_keep[s] of them where n_keep
+ * (dev int32 [n_seq]) is given; used[s] = min(used[s] + n, budget) (budget 0: no limit), seen[s] += n.  With state_off NULL and
+ * max_new_len 0 it applies the budget alone, as after bitrl_kv_evict_plan and bitrl_kv_move. */
+BITRL_API bitrl_status bitrl_kv_advance(const bitrl_kv_cache_t* cache, const int32_t* state_off, int32_t max_new_len,
+                                        const int32_t* n_keep, int32_t budget, void* stream);
+
+/* The encoder over a cache: blocks as in bitrl_encoder_forward_states, with block l's attention by bitrl_kv_append and
+ * bitrl_attention_cached on layer l.  The cache has at least as many layers as the encoder and its head counts.  pooled: NULL, or dev bf16
+ * [n_seq, d], the last new token of every sequence (rows of sequences without new tokens are left as they are).
+ * workspace >= bitrl_encoder_cached_workspace_bytes(enc, cache, T, max_new_len).  used and seen are not advanced. */
+BITRL_API size_t bitrl_encoder_cached_workspace_bytes(const bitrl_encoder_t* enc, const bitrl_kv_cache_t* cache, int32_t T,
+                                                      int32_t max_new_len);
+BITRL_API bitrl_status bitrl_encoder_forward_cached(const bitrl_encoder_t* enc, const bitrl_kv_cache_t* cache,
+                                                    const void* h_in, int32_t T, const int32_t* state_off,
+                                                    int32_t max_new_len, const int32_t* parent, double theta,
+                                                    int32_t accumulate_mass, void* h_out, void* pooled, void* workspace,
+                                                    size_t workspace_bytes, void* stream);
+
 /* ---- status ----------------------------------------------------------------------------------------- */
 /* Synchronizes `stream`, then reads and clears the device status word.  BITRL_OK, BITRL_ERR_TIMEOUT (a kernel
  * wait expired; results of that launch are invalid) or BITRL_ERR_CUDA. */

@@ -9,6 +9,7 @@ The functions mirror the C names without the ``bitrl_`` prefix:
 ``bitlinear_forward_q``, ``rmsnorm_quant``, ``vrepeat_rmsnorm_quant``, ``relu2gate_rmsnorm_quant``, ``attention``,
 ``pool_last_token``, ``Encoder`` (``forward``, ``forward_states``), ``heads_forward``, ``gae``, ``ppo_loss``,
 ``w8_quantize``, ``w8a8_forward``, ``w4_quantize``, ``w4a8_forward``,
+``KVCache`` with ``kv_append``, ``attention_cached``, ``kv_evict_plan``, ``kv_move``, ``kv_advance``, ``Encoder.forward_cached``,
 ``poll_status``.
 """
 from __future__ import annotations
@@ -42,7 +43,14 @@ class HeadDesc(ctypes.Structure):
                 ("W3t", ctypes.c_void_p), ("b3", ctypes.c_void_p), ("n_out", ctypes.c_int32)]
 
 
+class KvCacheDesc(ctypes.Structure):
+    """Mirror of ``bitrl_kv_cache_t``."""
+    _fields_ = [(n, ctypes.c_void_p) for n in ("k", "v", "mass", "pos", "page_table", "used", "seen")] + \
+               [(n, ctypes.c_int32) for n in ("n_layers", "n_pages", "n_kv_heads", "page_tokens", "head_dim", "n_seq", "max_pages")]
+
+
 _f32 = ctypes.c_float
+_kv = ctypes.POINTER(KvCacheDesc)
 
 EXPORTS = {
     "bitrl_pack_workspace_bytes": (_sz, [_i32, _i32]),
@@ -69,6 +77,14 @@ EXPORTS = {
     "bitrl_pool_last_token": (_i32, [_vp, _i32, _vp, _i32, _i32, _i32, _vp, _vp]),
     "bitrl_encoder_states_workspace_bytes": (_sz, [_vp, _i32, _i32]),
     "bitrl_encoder_forward_states": (_i32, [_vp, _vp, _i32, _vp, _i32, _i32, ctypes.c_double, _vp, _vp, _vp, _sz, _vp]),
+    "bitrl_kv_append": (_i32, [_kv, _i32, _vp, _i32, _vp, _i32, _vp, _i32, ctypes.c_double, _vp, _vp]),
+    "bitrl_attention_cached_workspace_bytes": (_sz, [_kv, _i32, _i32, _i32]),
+    "bitrl_attention_cached": (_i32, [_kv, _i32, _vp, _i32, _vp, _i32, _vp, _i32, _i32, _vp, _vp, _sz, _vp]),
+    "bitrl_kv_evict_plan": (_i32, [_kv, _i32, _i32, _i32, _i32, _vp, _vp, _vp]),
+    "bitrl_kv_move": (_i32, [_kv, _vp, _vp, _i32, _i32, _vp]),
+    "bitrl_kv_advance": (_i32, [_kv, _vp, _i32, _vp, _i32, _vp]),
+    "bitrl_encoder_cached_workspace_bytes": (_sz, [_vp, _kv, _i32, _i32]),
+    "bitrl_encoder_forward_cached": (_i32, [_vp, _kv, _vp, _i32, _vp, _i32, _vp, ctypes.c_double, _i32, _vp, _vp, _vp, _sz, _vp]),
     "bitrl_heads_forward": (_i32, [_vp, _i32, _i32, _i32, _i32, ctypes.POINTER(HeadDesc), _i32, ctypes.POINTER(_vp), _vp]),
     "bitrl_gae": (_i32, [_vp, _vp, _vp, _i32, _i32, _f32, _f32, _vp, _vp, _vp]),
     "bitrl_ppo_loss": (_i32, [_vp, _vp, _vp, _vp, _vp, _vp, _i32, _i32, _f32, _f32, _vp, _vp, _vp, _vp, _vp]),
@@ -444,6 +460,181 @@ def pool_last_token(h: torch.Tensor, states) -> torch.Tensor:
     return out
 
 
+PARENT_PAST, PARENT_PAD = -1, -2
+TREE_MAX_TOKENS = 256
+KV_MAX_SLOTS = 1 << 19
+
+
+def _here(t: torch.Tensor, dtype, name: str, device) -> torch.Tensor:
+    """A contiguous CUDA tensor of that dtype on the cache's device, which has to be the current one."""
+    _dev(t, dtype, name)
+    if t.device != device:
+        raise ValueError(f"{name}: on {t.device}, the cache is on {device}")
+    return t
+
+
+class KVCache:
+    """A paged key/value cache (``bitrl_kv_cache_t``) over tensors that the caller owns.
+
+    ``k``, ``v``: bf16 [n_layers, n_pages, n_kv_heads, page_tokens, head_dim]; ``page_table``: int32 [n_seq, max_pages];
+    ``used``, ``seen``: int32 [n_seq]; ``mass`` fp32 and ``pos`` int32 [n_layers, n_pages, n_kv_heads, page_tokens]
+    (``mass`` may be None: nothing accumulates and nothing can be evicted by weight)."""
+
+    def __init__(self, k, v, page_table, used, seen, mass=None, pos=None):
+        _dev(k, torch.bfloat16, "k")
+        if k.dim() != 5 or page_table.dim() != 2:
+            raise ValueError("k is [layers, pages, kv heads, page tokens, head dim], page_table [sequences, pages]")
+        self.device = k.device
+        if pos is None:
+            pos = torch.zeros(k.shape[:4], dtype=torch.int32, device=k.device)
+        for t, dt, name in ((v, torch.bfloat16, "v"), (page_table, torch.int32, "page_table"), (used, torch.int32, "used"),
+                            (seen, torch.int32, "seen"), (pos, torch.int32, "pos")):
+            _here(t, dt, name, self.device)
+        if mass is not None:
+            _here(mass, torch.float32, "mass", self.device)
+        n_layers, n_pages, n_kv, page, hd = k.shape
+        n_seq, max_pages = page_table.shape
+        if v.shape != k.shape or pos.shape != k.shape[:4] or (mass is not None and mass.shape != k.shape[:4]):
+            raise ValueError("v, mass and pos must match k")
+        if used.shape != (n_seq,) or seen.shape != (n_seq,):
+            raise ValueError("used and seen hold one entry per sequence")
+        self.k, self.v, self.mass, self.pos = k, v, mass, pos
+        self.page_table, self.used, self.seen = page_table, used, seen
+        self.n_layers, self.n_pages, self.n_kv_heads, self.page_tokens, self.head_dim = n_layers, n_pages, n_kv, page, hd
+        self.n_seq, self.max_pages = n_seq, max_pages
+        self.desc = KvCacheDesc(k.data_ptr(), v.data_ptr(), 0 if mass is None else mass.data_ptr(), pos.data_ptr(),
+                                page_table.data_ptr(), used.data_ptr(), seen.data_ptr(), n_layers, n_pages, n_kv, page, hd,
+                                n_seq, max_pages)
+        self._ref = ctypes.byref(self.desc)
+
+    @classmethod
+    def empty(cls, n_layers: int, n_seq: int, max_tokens: int, n_kv_heads: int, head_dim: int, page_tokens: int = 64,
+              device="cuda") -> "KVCache":
+        """A cache with room for ``max_tokens`` tokens of every sequence, its pages dealt out in order, nothing in it."""
+        max_pages = (max_tokens + page_tokens - 1) // page_tokens
+        shape = (n_layers, n_seq * max_pages, n_kv_heads, page_tokens)
+        kv = [torch.empty(*shape, head_dim, dtype=torch.bfloat16, device=device) for _ in range(2)]
+        table = torch.arange(n_seq * max_pages, dtype=torch.int32, device=device).reshape(n_seq, max_pages)
+        used, seen = (torch.zeros(n_seq, dtype=torch.int32, device=device) for _ in range(2))
+        return cls(*kv, table, used, seen, mass=torch.zeros(shape, device=device),
+                   pos=torch.zeros(shape, dtype=torch.int32, device=device))
+
+    def _check_current(self):
+        if self.device.index != torch.cuda.current_device():
+            raise ValueError(f"the cache is on {self.device}, the current device is cuda:{torch.cuda.current_device()}")
+
+    def batch(self, states, T: int, parent):
+        """Checks the new tokens of a call: (offsets or None, max_new_len, parent)."""
+        self._check_current()
+        if isinstance(states, int):
+            if states < 0 or T != states * self.n_seq:
+                raise ValueError("T must be the common number of new tokens times the number of sequences")
+            off, max_len = None, states
+        else:
+            off, max_len = states
+            _here(off, torch.int32, "state offsets", self.device)
+            if off.numel() != self.n_seq + 1:
+                raise ValueError("state offsets: one entry more than sequences")
+        if parent is not None:
+            _here(parent, torch.int32, "parent", self.device)
+            if parent.numel() != T:
+                raise ValueError("parent: one entry per new token")
+        return off, int(max_len), parent
+
+
+def kv_append(cache: KVCache, layer: int, qkv: torch.Tensor, states, n_heads: int, parent: torch.Tensor | None = None,
+              theta: float = ROPE_THETA, q_out: torch.Tensor | None = None) -> torch.Tensor:
+    """Rotates q and k of the new tokens qkv bf16 [T, (nh+2nkv)*hd], writes k and v into the cache and returns q [T, nh*hd].
+    ``states``: an int (that many new tokens for every sequence) or (offsets int32 [n_seq+1], largest number)."""
+    _here(qkv, torch.bfloat16, "qkv", cache.device)
+    T = qkv.shape[0]
+    if qkv.dim() != 2 or qkv.shape[1] != (n_heads + 2 * cache.n_kv_heads) * cache.head_dim:
+        raise ValueError("qkv must be [T, (n_heads + 2 n_kv_heads) * head_dim]")
+    off, max_len, parent = cache.batch(states, T, parent)
+    if q_out is None:
+        q_out = torch.zeros((T, n_heads * cache.head_dim), dtype=torch.bfloat16, device=qkv.device)
+    elif _here(q_out, torch.bfloat16, "q_out", cache.device).shape != (T, n_heads * cache.head_dim):
+        raise ValueError("q_out must be [T, n_heads * head_dim]")
+    _check(lib().bitrl_kv_append(cache._ref, layer, _ptr(qkv), T, _ptr(off), max_len, _ptr(parent), n_heads, float(theta),
+                                 _ptr(q_out), _stream()), "bitrl_kv_append")
+    return q_out
+
+
+def attention_cached_workspace_bytes(cache: KVCache, T: int, max_new_len: int, n_heads: int) -> int:
+    return int(lib().bitrl_attention_cached_workspace_bytes(cache._ref, T, max_new_len, n_heads))
+
+
+def attention_cached(cache: KVCache, layer: int, q: torch.Tensor, states, n_heads: int, parent: torch.Tensor | None = None,
+                     accumulate_mass: bool = True, att: torch.Tensor | None = None,
+                     workspace: torch.Tensor | None = None) -> torch.Tensor:
+    """Attention of the appended new tokens (q bf16 [T, nh*hd] from ``kv_append``) over the cache and one another; adds the
+    weights to ``cache.mass`` unless told not to.  Returns att bf16 [T, nh*hd]."""
+    _here(q, torch.bfloat16, "q", cache.device)
+    T = q.shape[0]
+    if q.dim() != 2 or q.shape[1] != n_heads * cache.head_dim:
+        raise ValueError("q must be [T, n_heads * head_dim]")
+    off, max_len, parent = cache.batch(states, T, parent)
+    if att is None:
+        att = torch.zeros_like(q)
+    elif _here(att, torch.bfloat16, "att", cache.device).shape != q.shape:
+        raise ValueError("att must have q's shape")
+    if workspace is None:
+        workspace = torch.empty((max(attention_cached_workspace_bytes(cache, T, max_len, n_heads), 16),), dtype=torch.uint8,
+                                device=q.device)
+    else:
+        _here(workspace, torch.uint8, "workspace", cache.device)
+    _check(lib().bitrl_attention_cached(cache._ref, layer, _ptr(q), T, _ptr(off), max_len, _ptr(parent), n_heads,
+                                        int(accumulate_mass), _ptr(att), _ptr(workspace), workspace.numel(), _stream()),
+           "bitrl_attention_cached")
+    return att
+
+
+def kv_evict_plan(cache: KVCache, budget: int, recent: int, sink: int = 0, moves: torch.Tensor | None = None,
+                  count: torch.Tensor | None = None):
+    """The rows that an eviction to ``budget`` slots moves: (moves int32 [layers, n_seq, n_kv, max_moves, 2] of (source,
+    destination), count int32 [layers, n_seq, n_kv]).  Entries behind the count are left as they are (-1 if allocated here)."""
+    cache._check_current()
+    lists = (cache.n_layers, cache.n_seq, cache.n_kv_heads)
+    if moves is None:
+        room = cache.max_pages * cache.page_tokens
+        moves = torch.full((*lists, max(1, min(budget, room - budget)), 2), -1, dtype=torch.int32, device=cache.device)
+    if count is None:
+        count = torch.empty(lists, dtype=torch.int32, device=cache.device)
+    _here(moves, torch.int32, "moves", cache.device)
+    _here(count, torch.int32, "count", cache.device)
+    if moves.shape[:3] != lists or moves.dim() != 5 or moves.shape[4] != 2 or count.shape != lists:
+        raise ValueError("moves is [layers, sequences, kv heads, max_moves, 2], count [layers, sequences, kv heads]")
+    _check(lib().bitrl_kv_evict_plan(cache._ref, budget, recent, sink, moves.shape[3], _ptr(moves), _ptr(count), _stream()),
+           "bitrl_kv_evict_plan")
+    return moves, count
+
+
+def kv_move(cache: KVCache, moves: torch.Tensor, count: torch.Tensor) -> None:
+    """Moves rows inside the cache: lists per (layer, sequence, kv head) as from ``kv_evict_plan``, or moves [n_seq, max_moves, 2]
+    and count [n_seq], the same for every layer and kv head."""
+    cache._check_current()
+    _here(moves, torch.int32, "moves", cache.device)
+    _here(count, torch.int32, "count", cache.device)
+    per_head = moves.dim() == 5
+    lists = (cache.n_layers, cache.n_seq, cache.n_kv_heads) if per_head else (cache.n_seq,)
+    if moves.shape[:-2] != lists or moves.shape[-1] != 2 or count.shape != lists:
+        raise ValueError("moves and count must hold one list per (layer, sequence, kv head) or per sequence")
+    _check(lib().bitrl_kv_move(cache._ref, _ptr(moves), _ptr(count), moves.shape[-2], int(per_head), _stream()), "bitrl_kv_move")
+
+
+def kv_advance(cache: KVCache, states, n_keep: torch.Tensor | None = None, budget: int = 0) -> None:
+    """After all layers of a step: used = min(used + n, budget), seen += n, with n = the new tokens, or ``n_keep`` [n_seq] of them.
+    ``states`` 0 applies the budget alone."""
+    cache._check_current()
+    if isinstance(states, int):
+        off, max_len = None, states
+    else:
+        off, max_len, _ = cache.batch(states, 0, None)
+    if n_keep is not None and _here(n_keep, torch.int32, "n_keep", cache.device).shape != (cache.n_seq,):
+        raise ValueError("n_keep: one entry per sequence")
+    _check(lib().bitrl_kv_advance(cache._ref, _ptr(off), max_len, _ptr(n_keep), budget, _stream()), "bitrl_kv_advance")
+
+
 def w8_quantize(W: torch.Tensor):
     """W CUDA fp32 [N,K] -> (W_q int8 [N,K], scale fp32 [2]; scale[0] is the scale)."""
     _dev(W, torch.float32, "W")
@@ -647,6 +838,36 @@ class Encoder:
         _check(lib().bitrl_encoder_forward_states(self.handle, _ptr(h_in), T, _ptr(off), n_states, max_len,
                                                   float(theta), _ptr(h_out), _ptr(pooled), _ptr(workspace),
                                                   workspace.numel(), _stream()), "bitrl_encoder_forward_states")
+        return (h_out, pooled) if pooled is not None else h_out
+
+    def cached_workspace_bytes(self, cache: KVCache, T: int, max_new_len: int) -> int:
+        return int(lib().bitrl_encoder_cached_workspace_bytes(self.handle, cache._ref, T, max_new_len))
+
+    def forward_cached(self, h_in: torch.Tensor, cache: KVCache, states, parent: torch.Tensor | None = None,
+                       theta: float = ROPE_THETA, accumulate_mass: bool = True, h_out: torch.Tensor | None = None,
+                       pooled: torch.Tensor | None = None, want_pooled: bool = False, workspace: torch.Tensor | None = None):
+        """The encoder over a cache: the new tokens h_in [T,d] attend to what their sequences have cached and to one another, and
+        their keys and values are appended in every layer (``kv_advance`` then counts them).  Returns h_out, or (h_out, pooled)."""
+        _here(h_in, torch.bfloat16, "h_in", cache.device)
+        T = h_in.shape[0]
+        if h_in.dim() != 2 or h_in.shape[1] != self.d:
+            raise ValueError("h_in must be [T, d]")
+        off, max_len, parent = cache.batch(states, T, parent)
+        if h_out is None:
+            h_out = torch.empty_like(h_in)
+        elif _here(h_out, torch.bfloat16, "h_out", cache.device).shape != h_in.shape:
+            raise ValueError("h_out must have h_in's shape")
+        if pooled is None and want_pooled:
+            pooled = torch.zeros((cache.n_seq, self.d), dtype=torch.bfloat16, device=h_in.device)
+        elif pooled is not None and _here(pooled, torch.bfloat16, "pooled", cache.device).shape != (cache.n_seq, self.d):
+            raise ValueError("pooled must be [n_seq, d]")
+        if workspace is None:
+            workspace = torch.empty((max(self.cached_workspace_bytes(cache, T, max_len), 16),), dtype=torch.uint8,
+                                    device=h_in.device)
+        _check(lib().bitrl_encoder_forward_cached(self.handle, cache._ref, _ptr(h_in), T, _ptr(off), max_len, _ptr(parent),
+                                                  float(theta), int(accumulate_mass), _ptr(h_out), _ptr(pooled),
+                                                  _ptr(workspace), workspace.numel(), _stream()),
+               "bitrl_encoder_forward_cached")
         return (h_out, pooled) if pooled is not None else h_out
 
     def close(self):

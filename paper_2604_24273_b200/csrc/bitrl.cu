@@ -1,6 +1,7 @@
 // C-ABI entry points of the bitrl library (declared and documented in include/bitrl.h).  Host code here only
 // validates arguments, carves workspaces and launches the kernels of pack.cuh / quant.cuh / gemv.cuh / gemm.cuh.
 #include <atomic>
+#include <climits>
 #include <cstdlib>
 #include <new>
 #include <vector>
@@ -108,6 +109,8 @@ static bitrl_status check_arch() {
 #include "gemv_multi.cuh"
 #include "gemm.cuh"
 #include "attention.cuh"
+#include "kv_cache.cuh"
+#include "attention_cached.cuh"
 #include "heads.cuh"
 #include "gemm_w8.cuh"
 #include "w4.cuh"
@@ -468,16 +471,16 @@ bool attention_shape_ok(int n_heads, int n_kv_heads, int head_dim, int max_state
          max_state_len >= 1 && max_state_len <= BITRL_ATTN_MAX_STATE_TOKENS;
 }
 
-// One pass over the blocks.  max_state_len == 0: identity attention (V repeated); else real attention per state.
-bitrl_status encoder_run(const bitrl_encoder_t* enc, const void* h_in, int32_t T, const int32_t* state_off,
-                         int32_t n_states, int32_t max_state_len, double theta, void* h_out, void* pooled,
-                         void* workspace, cudaStream_t st) {
+extern "C++" {  // a template
+// One pass over the blocks.  attend(l) turns the block's [q | k | v] in w.wide into the quantized input (w.xq, w.absmax,
+// w.rowsum) of its output projection.
+template <class Attend>
+bitrl_status encoder_blocks(const bitrl_encoder_t* enc, const void* h_in, int32_t T, void* h_out, const EncWs& w,
+                            cudaStream_t st, Attend attend) {
   bitrl_status s;
-  EncWs w = carve_enc(workspace, enc, T, max_state_len);
   const int d = enc->d, F = enc->d_ff;
   if (h_out != h_in)
     BITRL_CUDA(cudaMemcpyAsync(h_out, h_in, static_cast<size_t>(T) * d * 2, cudaMemcpyDeviceToDevice, st));
-  if (max_state_len > 0 && (s = launch_rope_table(w.rope, max_state_len, enc->head_dim, theta, st)) != BITRL_OK) return s;
   auto linear = [&](const bitrl_linear* lin, void* y, const void* residual) -> bitrl_status {
     if (T <= gemv_q_max_m() && gemv_fits(T, lin->l.K))
       return launch_gemv(&lin->l, nullptr, w.xq, w.absmax, T, y, BITRL_OUT_BF16, residual, nullptr, nullptr, nullptr, st);
@@ -487,21 +490,34 @@ bitrl_status encoder_run(const bitrl_encoder_t* enc, const void* h_in, int32_t T
     const bitrl_linear* const* q = enc->layers.data() + 4 * l;
     if ((s = launch_rmsnorm_quant(h_out, T, d, w.xq, w.absmax, w.rowsum, nullptr, st)) != BITRL_OK) return s;
     if ((s = linear(q[0], w.wide, nullptr)) != BITRL_OK) return s;
-    if (max_state_len > 0) {
-      if ((s = launch_attention(w.wide, T, state_off, n_states, max_state_len, enc->n_heads, enc->n_kv_heads,
-                                enc->head_dim, w.rope, w.att, st)) != BITRL_OK) return s;
-      if ((s = launch_rmsnorm_quant(w.att, T, d, w.xq, w.absmax, w.rowsum, nullptr, st)) != BITRL_OK) return s;
-    } else {
-      if ((s = launch_vrepeat_rmsnorm_quant(w.wide, T, enc->n_heads, enc->n_kv_heads, enc->head_dim, w.xq, w.absmax,
-                                            w.rowsum, nullptr, st)) != BITRL_OK) return s;
-    }
+    if ((s = attend(l)) != BITRL_OK) return s;
     if ((s = linear(q[1], h_out, h_out)) != BITRL_OK) return s;
     if ((s = launch_rmsnorm_quant(h_out, T, d, w.xq, w.absmax, w.rowsum, nullptr, st)) != BITRL_OK) return s;
     if ((s = linear(q[2], w.wide, nullptr)) != BITRL_OK) return s;
     if ((s = launch_relu2gate_rmsnorm_quant(w.wide, T, F, w.xq, w.absmax, w.rowsum, nullptr, st)) != BITRL_OK) return s;
     if ((s = linear(q[3], h_out, h_out)) != BITRL_OK) return s;
   }
-  if (pooled) return launch_pool_last_token(h_out, T, state_off, n_states, max_state_len, d, pooled, st);
+  return BITRL_OK;
+}
+}  // extern "C++"
+
+// max_state_len == 0: identity attention (V repeated); else real attention per state.
+bitrl_status encoder_run(const bitrl_encoder_t* enc, const void* h_in, int32_t T, const int32_t* state_off,
+                         int32_t n_states, int32_t max_state_len, double theta, void* h_out, void* pooled,
+                         void* workspace, cudaStream_t st) {
+  bitrl_status s;
+  const EncWs w = carve_enc(workspace, enc, T, max_state_len);
+  if (max_state_len > 0 && (s = launch_rope_table(w.rope, max_state_len, enc->head_dim, theta, st)) != BITRL_OK) return s;
+  s = encoder_blocks(enc, h_in, T, h_out, w, st, [&](int) -> bitrl_status {
+    if (max_state_len == 0)
+      return launch_vrepeat_rmsnorm_quant(w.wide, T, enc->n_heads, enc->n_kv_heads, enc->head_dim, w.xq, w.absmax,
+                                          w.rowsum, nullptr, st);
+    const bitrl_status r = launch_attention(w.wide, T, state_off, n_states, max_state_len, enc->n_heads, enc->n_kv_heads,
+                                            enc->head_dim, w.rope, w.att, st);
+    return r != BITRL_OK ? r : launch_rmsnorm_quant(w.att, T, enc->d, w.xq, w.absmax, w.rowsum, nullptr, st);
+  });
+  if (s != BITRL_OK) return s;
+  if (pooled) return launch_pool_last_token(h_out, T, state_off, n_states, max_state_len, enc->d, pooled, st);
   return BITRL_OK;
 }
 }  // namespace
@@ -577,6 +593,187 @@ bitrl_status bitrl_pool_last_token(const void* h, int32_t T, const int32_t* stat
   bitrl_status s = check_arch();
   if (s != BITRL_OK) return s;
   return launch_pool_last_token(h, T, state_off, n_states, max_state_len, d, out, static_cast<cudaStream_t>(stream));
+}
+
+// ---- paged key/value cache --------------------------------------------------------------------------------
+
+namespace {
+// What every call on a cache checks first.
+bitrl_status kv_check(const bitrl_kv_cache_t* c) {
+  if (!c || !c->k || !c->v || !c->pos || !c->page_table || !c->used || !c->seen) return BITRL_ERR_NULL;
+  if (c->n_layers < 1 || c->n_pages < 1 || c->n_kv_heads < 1 || c->n_seq < 1 || c->max_pages < 1) return BITRL_ERR_SHAPE;
+  if (c->page_tokens != 16 && c->page_tokens != 32 && c->page_tokens != 64 && c->page_tokens != 128) return BITRL_ERR_SHAPE;
+  if (c->head_dim != 64 && c->head_dim != 128) return BITRL_ERR_SHAPE;
+  if (static_cast<long long>(c->max_pages) * c->page_tokens > BITRL_KV_MAX_SLOTS) return BITRL_ERR_LIMIT;
+  if (!aligned16(c->k) || !aligned16(c->v) || !aligned16(c->mass) || !aligned16(c->pos)) return BITRL_ERR_ALIGN;
+  return BITRL_OK;
+}
+// What a call with new tokens checks.  Grids are counted in 64 bits; one that a launch cannot hold is refused.
+bitrl_status kv_check_batch(const bitrl_kv_cache_t* c, int32_t layer, int32_t T, const int32_t* state_off, int32_t max_new,
+                            const int32_t* parent, int32_t n_heads) {
+  if (layer < 0 || layer >= c->n_layers || T < 0 || max_new < 0) return BITRL_ERR_SHAPE;
+  if (n_heads < 1 || n_heads % c->n_kv_heads != 0) return BITRL_ERR_SHAPE;
+  if (!state_off && static_cast<long long>(c->n_seq) * max_new != T) return BITRL_ERR_SHAPE;
+  if (parent && max_new > BITRL_TREE_MAX_TOKENS) return BITRL_ERR_LIMIT;
+  if (max_new > static_cast<long long>(c->max_pages) * c->page_tokens) return BITRL_ERR_SHAPE;
+  if (static_cast<long long>(c->n_seq) * max_new * n_heads > INT_MAX || static_cast<long long>(T) * n_heads > INT_MAX)
+    return BITRL_ERR_LIMIT;
+  return BITRL_OK;
+}
+KvView kv_view(const bitrl_kv_cache_t* c, int layer) {
+  const long long rows = static_cast<long long>(layer) * c->n_pages * c->n_kv_heads * c->page_tokens;
+  int shift = 4;
+  while ((1 << shift) < c->page_tokens) ++shift;
+  return KvView{static_cast<unsigned short*>(c->k) + rows * c->head_dim, static_cast<unsigned short*>(c->v) + rows * c->head_dim,
+                c->mass ? c->mass + rows : nullptr, c->pos + rows, c->page_table, c->used, c->seen,
+                c->n_layers, c->n_pages, c->n_kv_heads, shift, c->head_dim, c->n_seq, c->max_pages};
+}
+// Lists of a call over all layers (one per layer, sequence and kv head).
+bool kv_lists_ok(const bitrl_kv_cache_t* c) {
+  return static_cast<long long>(c->n_layers) * c->n_seq * c->n_kv_heads <= INT_MAX / 1024;
+}
+}  // namespace
+
+bitrl_status bitrl_kv_append(const bitrl_kv_cache_t* cache, int32_t layer, const void* qkv, int32_t T,
+                             const int32_t* state_off, int32_t max_new_len, const int32_t* parent, int32_t n_heads,
+                             double theta, void* q_out, void* stream) {
+  bitrl_status s = kv_check(cache);
+  if (s != BITRL_OK) return s;
+  if ((s = kv_check_batch(cache, layer, T, state_off, max_new_len, parent, n_heads)) != BITRL_OK) return s;
+  if (!(theta > 0.0)) return BITRL_ERR_SHAPE;
+  if (T == 0 || max_new_len == 0) return BITRL_OK;
+  if (!qkv || !q_out) return BITRL_ERR_NULL;
+  if (!aligned16(qkv) || !aligned16(q_out)) return BITRL_ERR_ALIGN;
+  if ((s = check_arch()) != BITRL_OK) return s;
+  return launch_kv_append(kv_view(cache, layer), KvBatch{state_off, parent, max_new_len, T}, qkv, n_heads, theta, q_out,
+                          static_cast<cudaStream_t>(stream));
+}
+
+size_t bitrl_attention_cached_workspace_bytes(const bitrl_kv_cache_t* cache, int32_t T, int32_t max_new_len, int32_t n_heads) {
+  if (kv_check(cache) != BITRL_OK || T < 1 || max_new_len < 1 || n_heads < 1 || n_heads % cache->n_kv_heads != 0) return 0;
+  return ac_plan(kv_view(cache, 0), T, max_new_len, n_heads).bytes();
+}
+
+bitrl_status bitrl_attention_cached(const bitrl_kv_cache_t* cache, int32_t layer, const void* q, int32_t T,
+                                    const int32_t* state_off, int32_t max_new_len, const int32_t* parent, int32_t n_heads,
+                                    int32_t accumulate_mass, void* att, void* workspace, size_t workspace_bytes,
+                                    void* stream) {
+  bitrl_status s = kv_check(cache);
+  if (s != BITRL_OK) return s;
+  if ((s = kv_check_batch(cache, layer, T, state_off, max_new_len, parent, n_heads)) != BITRL_OK) return s;
+  if (accumulate_mass && !cache->mass) return BITRL_ERR_NULL;
+  if (T == 0 || max_new_len == 0) return BITRL_OK;
+  if (!q || !att) return BITRL_ERR_NULL;
+  const KvView c = kv_view(cache, layer);
+  const AcPlan p = ac_plan(c, T, max_new_len, n_heads);
+  if (!p.launchable(c)) return BITRL_ERR_LIMIT;
+  if (!workspace || workspace_bytes < p.bytes()) return BITRL_ERR_WORKSPACE;
+  if (!aligned16(q) || !aligned16(att) || !aligned16(workspace)) return BITRL_ERR_ALIGN;
+  if ((s = check_arch()) != BITRL_OK) return s;
+  return launch_attention_cached(c, KvBatch{state_off, parent, max_new_len, T}, q, n_heads, accumulate_mass != 0, att,
+                                 workspace, static_cast<cudaStream_t>(stream));
+}
+
+bitrl_status bitrl_kv_evict_plan(const bitrl_kv_cache_t* cache, int32_t budget, int32_t recent, int32_t sink,
+                                 int32_t max_moves, int32_t* moves, int32_t* count, void* stream) {
+  bitrl_status s = kv_check(cache);
+  if (s != BITRL_OK) return s;
+  if (!cache->mass || !moves || !count) return BITRL_ERR_NULL;
+  if (budget < 1 || recent < 0 || sink < 0 || max_moves < 0) return BITRL_ERR_SHAPE;
+  const int room = cache->max_pages * cache->page_tokens;
+  if (budget < room && max_moves < (budget < room - budget ? budget : room - budget)) return BITRL_ERR_SHAPE;
+  if (!kv_lists_ok(cache)) return BITRL_ERR_LIMIT;
+  if (!aligned16(moves) || !aligned16(count)) return BITRL_ERR_ALIGN;
+  if ((s = check_arch()) != BITRL_OK) return s;
+  return launch_kv_evict_plan(kv_view(cache, 0), budget, recent, sink, max_moves, moves, count, static_cast<cudaStream_t>(stream));
+}
+
+bitrl_status bitrl_kv_move(const bitrl_kv_cache_t* cache, const int32_t* moves, const int32_t* count, int32_t max_moves,
+                           int32_t per_head, void* stream) {
+  bitrl_status s = kv_check(cache);
+  if (s != BITRL_OK) return s;
+  if (max_moves < 0) return BITRL_ERR_SHAPE;
+  if (!kv_lists_ok(cache)) return BITRL_ERR_LIMIT;
+  if (max_moves == 0) return BITRL_OK;
+  if (!moves || !count) return BITRL_ERR_NULL;
+  if (!aligned16(moves) || !aligned16(count)) return BITRL_ERR_ALIGN;
+  if ((s = check_arch()) != BITRL_OK) return s;
+  return launch_kv_move(kv_view(cache, 0), moves, count, max_moves, per_head != 0, static_cast<cudaStream_t>(stream));
+}
+
+bitrl_status bitrl_kv_advance(const bitrl_kv_cache_t* cache, const int32_t* state_off, int32_t max_new_len,
+                              const int32_t* n_keep, int32_t budget, void* stream) {
+  bitrl_status s = kv_check(cache);
+  if (s != BITRL_OK) return s;
+  if (max_new_len < 0 || budget < 0) return BITRL_ERR_SHAPE;
+  if ((s = check_arch()) != BITRL_OK) return s;
+  return launch_kv_advance(kv_view(cache, 0), KvBatch{state_off, nullptr, max_new_len, 0}, n_keep, budget,
+                           static_cast<cudaStream_t>(stream));
+}
+
+namespace {
+// Workspace of the encoder over a cache: that of bitrl_encoder_forward, then the rotated queries, the attention's output
+// and its workspace.
+struct EncCachedWs {
+  EncWs e;
+  unsigned short* q;
+  unsigned short* att;
+  void* attn;
+  size_t bytes;
+};
+EncCachedWs carve_enc_cached(void* ws, const bitrl_encoder_t* enc, const bitrl_kv_cache_t* cache, int T, int max_new) {
+  EncCachedWs w;
+  w.e = carve_enc(ws, enc, T, 0);
+  unsigned char* b = static_cast<unsigned char*>(ws);
+  size_t off = align_up(w.e.bytes, 256);
+  w.q = reinterpret_cast<unsigned short*>(b + off);
+  off += align_up(static_cast<size_t>(T) * enc->d * 2, 256);
+  w.att = reinterpret_cast<unsigned short*>(b + off);
+  off += align_up(static_cast<size_t>(T) * enc->d * 2, 256);
+  w.attn = b + off;
+  off += ac_plan(kv_view(cache, 0), T, max_new, enc->n_heads).bytes();
+  w.bytes = off;
+  return w;
+}
+bool enc_cache_match(const bitrl_encoder_t* enc, const bitrl_kv_cache_t* cache) {
+  return cache->n_layers >= enc->L && cache->n_kv_heads == enc->n_kv_heads && cache->head_dim == enc->head_dim;
+}
+}  // namespace
+
+size_t bitrl_encoder_cached_workspace_bytes(const bitrl_encoder_t* enc, const bitrl_kv_cache_t* cache, int32_t T,
+                                            int32_t max_new_len) {
+  if (!enc || kv_check(cache) != BITRL_OK || !enc_cache_match(enc, cache) || T < 1 || max_new_len < 1) return 0;
+  return carve_enc_cached(nullptr, enc, cache, T, max_new_len).bytes;
+}
+
+bitrl_status bitrl_encoder_forward_cached(const bitrl_encoder_t* enc, const bitrl_kv_cache_t* cache, const void* h_in,
+                                          int32_t T, const int32_t* state_off, int32_t max_new_len, const int32_t* parent,
+                                          double theta, int32_t accumulate_mass, void* h_out, void* pooled, void* workspace,
+                                          size_t workspace_bytes, void* stream) {
+  if (!enc) return BITRL_ERR_NULL;
+  bitrl_status s = kv_check(cache);
+  if (s != BITRL_OK) return s;
+  if (!enc_cache_match(enc, cache) || !(theta > 0.0)) return BITRL_ERR_SHAPE;
+  if ((s = kv_check_batch(cache, 0, T, state_off, max_new_len, parent, enc->n_heads)) != BITRL_OK) return s;
+  if (accumulate_mass && !cache->mass) return BITRL_ERR_NULL;
+  if (T == 0 || max_new_len == 0) return BITRL_OK;
+  if (!h_in || !h_out) return BITRL_ERR_NULL;
+  if (!ac_plan(kv_view(cache, 0), T, max_new_len, enc->n_heads).launchable(kv_view(cache, 0))) return BITRL_ERR_LIMIT;
+  if (!workspace || workspace_bytes < carve_enc_cached(nullptr, enc, cache, T, max_new_len).bytes) return BITRL_ERR_WORKSPACE;
+  if (!aligned16(h_in) || !aligned16(h_out) || !aligned16(workspace) || !aligned16(pooled)) return BITRL_ERR_ALIGN;
+  if ((s = check_arch()) != BITRL_OK) return s;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  const EncCachedWs w = carve_enc_cached(workspace, enc, cache, T, max_new_len);
+  const KvBatch b{state_off, parent, max_new_len, T};
+  s = encoder_blocks(enc, h_in, T, h_out, w.e, st, [&](int l) -> bitrl_status {
+    const KvView c = kv_view(cache, l);
+    bitrl_status r = launch_kv_append(c, b, w.e.wide, enc->n_heads, theta, w.q, st);
+    if (r != BITRL_OK) return r;
+    if ((r = launch_attention_cached(c, b, w.q, enc->n_heads, accumulate_mass != 0, w.att, w.attn, st)) != BITRL_OK) return r;
+    return launch_rmsnorm_quant(w.att, T, enc->d, w.e.xq, w.e.absmax, w.e.rowsum, nullptr, st);
+  });
+  if (s != BITRL_OK) return s;
+  return pooled ? launch_kv_pool_last(kv_view(cache, 0), b, h_out, enc->d, pooled, st) : BITRL_OK;
 }
 
 // ---- heads, GAE, PPO objective ----------------------------------------------------------------------------
