@@ -365,6 +365,7 @@ BITRL_API bitrl_status bitrl_bitlinear5_forward_multi(int32_t count, const bitrl
  * max_pages hold) makes a call skip that sequence, and the next bitrl_poll_status returns BITRL_ERR_SHAPE. */
 #define BITRL_TREE_MAX_TOKENS 256
 #define BITRL_KV_MAX_SLOTS (1 << 19) /* max_pages * page_tokens at most; beyond it BITRL_ERR_LIMIT */
+#define BITRL_KV_MAX_GROUP 64 /* query heads of a kv head at most; beyond it BITRL_ERR_LIMIT */
 #define BITRL_PARENT_PAST (-1)
 #define BITRL_PARENT_PAD (-2)
 typedef struct bitrl_kv_cache {

@@ -16,6 +16,11 @@ namespace bitrl {
 
 constexpr int AC_TREE_WORDS = BITRL_TREE_MAX_TOKENS / 32;
 
+// Where a cut item of the tile kernels was left: two per CTA (0: the item began in an earlier CTA, 1: it begins here); s < 0: none.
+struct AtCut {
+  int s, x, h, ends;
+};
+
 struct AcArgs {
   KvView c;  // this layer
   KvBatch b;
@@ -28,6 +33,9 @@ struct AcArgs {
   float* part_o;           // [splits][T * n_heads][HD] unnormalised partial results (splits > 1)
   float2* part_ml;         // [splits][T * n_heads]: running maximum and sum
   float* lse;              // [T * n_heads]: maximum + log2(sum); +inf where a row sees nothing
+  const uint32_t* anc;     // trees: [T][AC_TREE_WORDS]
+  const int* tree_ok;      // trees: [n_seq], else nullptr
+  AtCut* cuts;             // tiles: [CTAs][2]
 };
 
 __device__ __forceinline__ float ac_exp2(float x) {
@@ -55,19 +63,26 @@ __device__ __forceinline__ void cp_async_wait() {
   asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
 }
 
-// Ancestors of every new token as bits, anc[token][AC_TREE_WORDS]: bit j is set when token j is the token itself or above
-// it; padding has no bits.  All threads of the CTA call it.
-__device__ __forceinline__ bool ac_load_tree(const KvBatch& b, const KvSeq& q, int* par, uint32_t* anc, int n_threads) {
-  if (!kv_load_tree(b, q, par, n_threads)) return false;
-  for (int i = threadIdx.x; i < q.m; i += n_threads) {
-    uint32_t* w = anc + i * AC_TREE_WORDS;
+// Ancestors of every new token as bits, anc[row][AC_TREE_WORDS]: bit j is set when token j of the sequence is the token
+// itself or above it; padding has no bits.  ok[s]: the sequence's tree is one.  One CTA per sequence.
+__global__ void __launch_bounds__(BITRL_TREE_MAX_TOKENS) attn_tree_kernel(const KvView c, const KvBatch b, uint32_t* anc, int* ok) {
+  __shared__ int par[BITRL_TREE_MAX_TOKENS];
+  pdl_enter();
+  const int s = blockIdx.x, i = threadIdx.x;
+  KvSeq q;
+  const bool good = kv_seq(c, b, s, q) && kv_load_tree(b, q, par, BITRL_TREE_MAX_TOKENS);
+  if (i == 0) ok[s] = good;
+  if (!good || i >= q.m) return;
+  uint32_t w[AC_TREE_WORDS];
 #pragma unroll
-    for (int k = 0; k < AC_TREE_WORDS; ++k) w[k] = 0u;
-    if (par[i] != BITRL_PARENT_PAD)
-      for (int j = i; j >= 0; j = par[j]) w[j >> 5] |= 1u << (j & 31);
+  for (int k = 0; k < AC_TREE_WORDS; ++k) w[k] = 0u;
+  for (int j = par[i] == BITRL_PARENT_PAD ? -1 : i; j >= 0; j = par[j]) {
+#pragma unroll
+    for (int k = 0; k < AC_TREE_WORDS; ++k) w[k] |= (j >> 5) == k ? 1u << (j & 31) : 0u;
   }
-  __syncthreads();
-  return true;
+  uint4* out = reinterpret_cast<uint4*>(anc + (static_cast<long long>(q.t0) + i) * AC_TREE_WORDS);
+  out[0] = make_uint4(w[0], w[1], w[2], w[3]);
+  out[1] = make_uint4(w[4], w[5], w[6], w[7]);
 }
 // Does token `tok` see the slot of new token j (j >= 0)?
 __device__ __forceinline__ bool ac_sees_new(const uint32_t* anc, int tok, int j) {
@@ -92,17 +107,16 @@ constexpr int AR_ROWS = 16;
 constexpr int AR_KEYS = 16;  // slots per step of a warp
 
 template <int HD>
-constexpr uint32_t ar_smem_bytes(bool tree) {
+constexpr uint32_t ar_smem_bytes() {
   const uint32_t ring = AR_WARPS * AR_STAGES * 2 * AR_KEYS * HD * 2;
   const uint32_t join = AR_WARPS * AR_ROWS * (HD * 4 + 8);
-  return (ring > join ? ring : join) + (tree ? BITRL_TREE_MAX_TOKENS * (AC_TREE_WORDS + 1) * 4 : 0);
+  return ring > join ? ring : join;
 }
 
 template <int HD>
 __global__ void __launch_bounds__(AR_THREADS) attn_rows_kernel(const __grid_constant__ AcArgs a) {
   constexpr int KS = HD / 16, ND = HD / 8, CH = HD / 8;
   constexpr uint32_t KV_BYTES = AR_KEYS * HD * 2;  // keys (or values) of one step
-  constexpr uint32_t RING = AR_WARPS * AR_STAGES * 2 * KV_BYTES;
   extern __shared__ __align__(128) unsigned char ar_smem[];
   pdl_enter();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3, lm = lane >> 3, lr = lane & 7;
@@ -119,13 +133,8 @@ __global__ void __launch_bounds__(AR_THREADS) attn_rows_kernel(const __grid_cons
   const int end = ac_key_end(q, a.rep, a.b.parent != nullptr, x0, AR_ROWS);
   const int k0 = split * a.split_keys, k1 = min(end, k0 + a.split_keys);
   if (k0 >= end) return;
-  uint32_t* anc = nullptr;
-  if (a.b.parent) {
-    constexpr uint32_t JOIN = AR_WARPS * AR_ROWS * (HD * 4 + 8);
-    anc = reinterpret_cast<uint32_t*>(ar_smem + (RING > JOIN ? RING : JOIN));
-    int* par = reinterpret_cast<int*>(anc + BITRL_TREE_MAX_TOKENS * AC_TREE_WORDS);
-    if (!ac_load_tree(a.b, q, par, anc, AR_THREADS)) return;
-  }
+  if (a.tree_ok && !a.tree_ok[s]) return;
+  const uint32_t* anc = a.b.parent ? a.anc + static_cast<long long>(q.t0) * AC_TREE_WORDS : nullptr;
 
   // ---- queries of rows g and g + 8 of the tile
   uint32_t qa[KS][4];
@@ -405,8 +414,8 @@ constexpr int AM_KEYS = 64;
 constexpr int AM_ROWS = 64;  // rows per step
 
 template <int HD>
-constexpr uint32_t am_smem_bytes(bool tree) {
-  return AM_KEYS * HD * 2 + 2 * AM_ROWS * (HD * 2 + 4) + (tree ? BITRL_TREE_MAX_TOKENS * (AC_TREE_WORDS + 1) * 4 : 0);
+constexpr uint32_t am_smem_bytes() {
+  return AM_KEYS * HD * 2 + 2 * AM_ROWS * (HD * 2 + 4);
 }
 
 template <int HD>
@@ -425,13 +434,9 @@ __global__ void __launch_bounds__(AM_THREADS) attn_mass_kernel(const __grid_cons
   if (!kv_seq(a.c, a.b, s, q)) return;
   const int slot0 = kt * AM_KEYS, end = q.used + q.m;
   if (slot0 >= end || q.m == 0) return;
-  uint32_t* anc = nullptr;
   float* lse_s = reinterpret_cast<float*>(am_smem + K_BYTES + 2 * Q_BYTES);  // [2][AM_ROWS]
-  if (a.b.parent) {
-    anc = reinterpret_cast<uint32_t*>(lse_s + 2 * AM_ROWS);
-    int* par = reinterpret_cast<int*>(anc + BITRL_TREE_MAX_TOKENS * AC_TREE_WORDS);
-    if (!ac_load_tree(a.b, q, par, anc, AM_THREADS)) return;
-  }
+  if (a.tree_ok && !a.tree_ok[s]) return;
+  const uint32_t* anc = a.b.parent ? a.anc + static_cast<long long>(q.t0) * AC_TREE_WORDS : nullptr;
   const uint32_t k_addr = ptx::smem_u32(am_smem), q_addr = k_addr + K_BYTES;
   const int slot_mask = (1 << a.c.page_shift) - 1;
   for (int i = threadIdx.x; i < AM_KEYS * CH; i += AM_THREADS) {
@@ -521,95 +526,6 @@ __global__ void __launch_bounds__(AM_THREADS) attn_mass_kernel(const __grid_cons
       }
     }
   }
-}
-
-// ---- host --------------------------------------------------------------------------------------------------------------
-struct AcPlan {
-  int row_tiles, splits, split_keys;
-  size_t lse_bytes, ml_bytes, o_bytes;
-  size_t bytes() const { return lse_bytes + ml_bytes + o_bytes; }
-  // Does every grid of the call fit a launch?
-  bool launchable(const KvView& c) const {
-    const long long heads = static_cast<long long>(c.n_seq) * c.n_kv;
-    const long long key_tiles = ((c.max_pages << c.page_shift) + AM_KEYS - 1) / AM_KEYS;
-    return heads * row_tiles <= INT_MAX / splits && heads <= INT_MAX / key_tiles;
-  }
-};
-
-inline size_t ac_up(size_t v) { return (v + 255) / 256 * 256; }
-
-// Key ranges are made so that even one row tile per (sequence, kv head) fills the SMs several times over; they depend on
-// the sizes alone, not on the lengths, which only the device knows.
-inline AcPlan ac_plan(const KvView& c, int T, int max_new, int n_heads) {
-  AcPlan p;
-  const int rep = n_heads / c.n_kv;
-  p.row_tiles = static_cast<int>((static_cast<long long>(max_new) * rep + AR_ROWS - 1) / AR_ROWS);
-  const long long items = static_cast<long long>(c.n_seq) * c.n_kv * p.row_tiles;
-  const int room = c.max_pages << c.page_shift;
-  const long long most = (room + 255) / 256;  // no range below 256 slots
-  long long splits = (148LL * 8 + items - 1) / items;
-  if (splits > most) splits = most;
-  p.split_keys = static_cast<int>(((room + splits - 1) / splits + 63) / 64 * 64);
-  p.splits = (room + p.split_keys - 1) / p.split_keys;
-  p.lse_bytes = ac_up(static_cast<size_t>(T) * n_heads * 4);
-  p.ml_bytes = p.splits > 1 ? ac_up(static_cast<size_t>(p.splits) * T * n_heads * 8) : 0;
-  p.o_bytes = p.splits > 1 ? ac_up(static_cast<size_t>(p.splits) * T * n_heads * c.hd * 4) : 0;
-  return p;
-}
-
-template <class K>
-bitrl_status ac_smem(K kernel, size_t bytes, bool (&done)[64]) {
-  int dev = 0;
-  BITRL_CUDA(cudaGetDevice(&dev));
-  if (dev >= 0 && dev < 64 && !done[dev]) {
-    BITRL_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(bytes)));
-    done[dev] = true;
-  }
-  return BITRL_OK;
-}
-
-template <int HD>
-bitrl_status launch_attention_cached_hd(const AcArgs& a, const AcPlan& p, bool mass, cudaStream_t st) {
-  const bool tree = a.b.parent != nullptr;
-  bitrl_status s;
-  static bool rows_set[64] = {false}, mass_set[64] = {false};
-  if ((s = ac_smem(attn_rows_kernel<HD>, ar_smem_bytes<HD>(true), rows_set)) != BITRL_OK) return s;
-  BITRL_CUDA(launch_pdl(attn_rows_kernel<HD>, dim3(static_cast<unsigned>(static_cast<long long>(a.c.n_seq) * a.c.n_kv * p.row_tiles * p.splits)),
-                        dim3(AR_THREADS), ar_smem_bytes<HD>(tree), st, a));
-  count_launch(1);
-  if (p.splits > 1) {
-    const unsigned per_seq = static_cast<unsigned>((static_cast<long long>(a.b.max_new) * a.n_heads + 3) / 4);
-    BITRL_CUDA(launch_pdl(attn_join_kernel<HD>, dim3(per_seq * a.c.n_seq), dim3(128), 0, st, a));
-    count_launch(1);
-  }
-  if (mass) {
-    if ((s = ac_smem(attn_mass_kernel<HD>, am_smem_bytes<HD>(true), mass_set)) != BITRL_OK) return s;
-    const unsigned tiles = static_cast<unsigned>(((a.c.max_pages << a.c.page_shift) + AM_KEYS - 1) / AM_KEYS);
-    BITRL_CUDA(launch_pdl(attn_mass_kernel<HD>, dim3(tiles * a.c.n_kv * a.c.n_seq), dim3(AM_THREADS), am_smem_bytes<HD>(tree), st, a));
-    count_launch(1);
-  }
-  return BITRL_OK;
-}
-
-bitrl_status launch_attention_cached(const KvView& c, const KvBatch& b, const void* q, int n_heads, bool mass, void* att,
-                                     void* workspace, cudaStream_t st) {
-  const AcPlan p = ac_plan(c, b.T, b.max_new, n_heads);
-  unsigned char* w = static_cast<unsigned char*>(workspace);
-  AcArgs a;
-  a.c = c;
-  a.b = b;
-  a.q = static_cast<const unsigned short*>(q);
-  a.att = static_cast<unsigned short*>(att);
-  a.n_heads = n_heads;
-  a.rep = n_heads / c.n_kv;
-  a.scale2 = static_cast<float>(1.4426950408889634 / sqrt(static_cast<double>(c.hd)));
-  a.row_tiles = p.row_tiles;
-  a.splits = p.splits;
-  a.split_keys = p.split_keys;
-  a.lse = reinterpret_cast<float*>(w);
-  a.part_ml = reinterpret_cast<float2*>(w + p.lse_bytes);
-  a.part_o = reinterpret_cast<float*>(w + p.lse_bytes + p.ml_bytes);
-  return c.hd == 128 ? launch_attention_cached_hd<128>(a, p, mass, st) : launch_attention_cached_hd<64>(a, p, mass, st);
 }
 
 }  // namespace bitrl

@@ -1,0 +1,742 @@
+// Attention over the cache for more than 16 rows per sequence and kv head: tcgen05 tiles of 128 rows.
+#pragma once
+
+#include <cuda.h>
+
+#include "attention_cached.cuh"
+#include "gemm.cuh"
+#include "ptx.cuh"
+
+namespace bitrl {
+
+// ---- work lists ------------------------------------------------------------------------------------------------------
+// Lengths are known on the device alone, so the kernels cut their work there: pairs (sequence s, index x < nx), each
+// holding n_kv items (kv heads) of cost(s, x) units, form one list, and CTA c of G takes its units [N c / G, N (c+1) / G).
+// Every CTA then has the same share whatever the lengths are; an item may be cut between neighbours.
+struct AcRun {
+  int s, x, h, u;   // first unit: item (s, x, h), unit u of it
+  long long left;   // units of this CTA
+};
+
+// All `n_threads` threads call it; `part` holds n_threads / 32 + 1 numbers of shared memory.  cost(s, x) >= 0.
+template <class Cost>
+__device__ __forceinline__ void ac_run_start(Cost cost, int n_seq, int nx, int n_kv, int n_threads, long long* part, AcRun* out) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const long long pairs = static_cast<long long>(n_seq) * nx;
+  const long long per = (pairs + n_threads - 1) / n_threads;
+  const long long p0 = min(pairs, per * threadIdx.x), p1 = min(pairs, p0 + per);
+  long long sum = 0;
+  for (long long p = p0; p < p1; ++p) sum += cost(static_cast<int>(p / nx), static_cast<int>(p % nx));
+  long long incl = sum;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const long long v = __shfl_up_sync(0xffffffffu, incl, o);
+    if (lane >= o) incl += v;
+  }
+  if (lane == 31) part[warp] = incl;
+  __syncthreads();
+  long long before = 0, all = 0;
+  for (int w = 0; w < n_threads / 32; ++w) {
+    if (w < warp) before += part[w];
+    all += part[w];
+  }
+  const long long excl = (before + incl - sum) * n_kv, N = all * n_kv;
+  const long long w0 = N * blockIdx.x / gridDim.x, w1 = N * (blockIdx.x + 1) / gridDim.x;
+  if (threadIdx.x == 0 && w0 >= w1) out->left = 0;
+  if (w0 < w1 && w0 >= excl && w0 < excl + sum * n_kv) {
+    long long rem = w0 - excl;
+    for (long long p = p0; p < p1; ++p) {
+      const int c = cost(static_cast<int>(p / nx), static_cast<int>(p % nx));
+      if (rem < static_cast<long long>(c) * n_kv) {
+        *out = AcRun{static_cast<int>(p / nx), static_cast<int>(p % nx), static_cast<int>(rem / c), static_cast<int>(rem % c), w1 - w0};
+        break;
+      }
+      rem -= static_cast<long long>(c) * n_kv;
+    }
+  }
+  __syncthreads();
+}
+
+// Walks a run item by item: u0 .. u1 are the units of item (s, x, h) that belong to the run.
+struct AcWalk {
+  int s, x, h, u0, u1, units;
+  long long left;
+  int nx, n_kv, n_seq;
+  __device__ __forceinline__ AcWalk(const AcRun& r, int nx_, int n_kv_, int n_seq_)
+      : s(r.s), x(r.x), h(r.h), u0(r.u), u1(0), units(0), left(r.left), nx(nx_), n_kv(n_kv_), n_seq(n_seq_) {}
+  template <class Cost>
+  __device__ __forceinline__ bool start(Cost cost) {
+    if (left <= 0) return false;
+    units = cost(s, x);
+    u1 = static_cast<int>(min(static_cast<long long>(units), u0 + left));
+    return true;
+  }
+  template <class Cost>
+  __device__ __forceinline__ bool next(Cost cost) {
+    left -= u1 - u0;
+    if (left <= 0) return false;
+    u0 = 0;
+    if (++h == n_kv) {
+      h = 0;
+      do {
+        if (++x == nx) {
+          x = 0;
+          if (++s >= n_seq) return false;
+        }
+        units = cost(s, x);
+      } while (units == 0);
+    }
+    u1 = static_cast<int>(min(static_cast<long long>(units), left));
+    return true;
+  }
+};
+
+// ---- forward -----------------------------------------------------------------------------------------------------------
+// An item is 256 rows (two tiles of 128, whole tokens each) of one kv head; a unit is 128 slots of its keys.  One CTA per SM:
+//   warp 0      producer: queries of an item (3-D TMA: dims x heads of the group x tokens), then per unit the keys and the
+//               values, page by page, 128-byte swizzled, through a ring of four tiles
+//   warp 1      MMA: S_a = Q_a K^T (128 x 128) and O_a += P_a V for the two row tiles a in turn; the softmax of one tile runs
+//               beside the products of the other.  P replaces S in tensor memory (A operand); V is the MN-major B operand.
+//   warps 2,3   make a unit's values harmless where some row must not see them: rows behind the last slot and of padding
+//               become zero, and so do values that are not finite (rows that do see them get them back at the end)
+//   warps 4-7, 8-11   softmax of row tile 0 / 1, one row per thread: no exchange between threads.  The running maximum is
+//               followed only when it has grown by more than 2^8 (weights stay below 2^8, statistics and sums are fp32), so
+//               the result is rescaled rarely.  Weights are rounded to bf16 for the product (2^-9 relative each, of random
+//               sign over the keys: below the rounding of the result itself); their sum is taken before the rounding.
+// Bound: 2 * 512 tensor cycles and 1024 cycles of exponentials per 128 x 128 tile for long chunks; the reading of keys and
+// values for up to ~100 rows.  Every wait is bounded; on expiry the CTA records a status word and leaves normally.
+constexpr int AT_THREADS = 384;
+constexpr int AT_KEYS = 128;
+constexpr int AT_RING = 4;
+constexpr float AT_GROWTH = 8.0f;
+enum { AT_WAIT_LOAD = 131, AT_WAIT_MMA = 132, AT_WAIT_SOFTMAX = 133, AT_WAIT_FIX = 134 };
+
+template <int HD>
+struct AtSmem {
+  static constexpr uint32_t TILE = 128 * HD * 2, HALF = 128 * 128;  // HALF: one 64-dimension block of a tile
+  static constexpr uint32_t Q = 0, RING = 2 * TILE, BAR = RING + AT_RING * TILE;
+  static constexpr uint32_t KV_FULL = BAR, KV_EMPTY = KV_FULL + 8 * AT_RING, Q_FULL = KV_EMPTY + 8 * AT_RING, Q_EMPTY = Q_FULL + 8,
+                            S_FULL = Q_EMPTY + 8, P_FULL = S_FULL + 16, O_FULL = P_FULL + 16, V_READY = O_FULL + 16, DRAIN = V_READY + 16;
+  static constexpr uint32_t MISC = DRAIN + 8;  // tensor-memory base, failed, odd[4]
+  static constexpr uint32_t RUN = MISC + 32, PART = RUN + 32;
+  static constexpr uint32_t BYTES = PART + 8 * (AT_THREADS / 32 + 1) + 1024;  // + slack to align the base
+  // one CTA per SM: it takes all of tensor memory
+  static constexpr uint32_t LAUNCH = BYTES > 120 * 1024 ? BYTES : 120 * 1024;
+};
+
+struct AtArgs {
+  AcArgs a;
+  int tok_tile;  // whole tokens of a 128-row tile
+  int nx;        // items of the longest sequence
+  int rows_cap;  // rows kept for each cut item: min(256, max_new * rep)
+};
+
+// Units (key tiles) of item (s, x).
+__device__ __forceinline__ int at_units(const AtArgs& t, int s, int x, KvSeq& q) {
+  if (!kv_seq(t.a.c, t.a.b, s, q)) return 0;
+  const int tok0 = x * 2 * t.tok_tile;
+  if (tok0 >= q.m || (t.a.tree_ok && !t.a.tree_ok[s])) return 0;
+  const int end = q.used + (t.a.b.parent ? q.m : min(q.m, tok0 + 2 * t.tok_tile));
+  return (end + AT_KEYS - 1) / AT_KEYS;
+}
+// 32 bits: which of the slots slot0 .. slot0 + 31 does token `tok` see?
+__device__ __forceinline__ uint32_t at_seen(const AcArgs& a, const KvSeq& q, int tok, int slot0) {
+  const int j0 = slot0 - q.used;  // place of the first slot among the new tokens
+  if (j0 + 32 <= 0) return 0xffffffffu;
+  if (!a.b.parent) {
+    const int n = tok + 1 - j0;  // slots seen from slot0 on
+    return n >= 32 ? 0xffffffffu : n <= 0 ? 0u : (1u << n) - 1u;
+  }
+  const uint32_t* w = a.anc + static_cast<long long>(q.t0 + tok) * AC_TREE_WORDS;
+  if (j0 >= BITRL_TREE_MAX_TOKENS) return 0u;
+  if (j0 < 0) return ((w[0] << (-j0)) | ((1u << (-j0)) - 1u));
+  const uint32_t lo = w[j0 >> 5], hi = (j0 >> 5) + 1 < AC_TREE_WORDS ? w[(j0 >> 5) + 1] : 0u;
+  return __funnelshift_r(lo, hi, j0 & 31);
+}
+
+template <int HD>
+__global__ void __launch_bounds__(AT_THREADS, 1)
+attn_tiles_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_constant__ CUtensorMap tmap_k,
+                  const __grid_constant__ CUtensorMap tmap_v, const __grid_constant__ AtArgs t) {
+  using M = AtSmem<HD>;
+  constexpr int NH = HD / 64;
+  extern __shared__ unsigned char at_smem_raw[];
+  const uint32_t raw = ptx::smem_u32(at_smem_raw), base = (raw + 1023u) & ~1023u;
+  unsigned char* sm = at_smem_raw + (base - raw);
+  volatile uint32_t* misc = reinterpret_cast<volatile uint32_t*>(sm + M::MISC);
+  volatile uint32_t* failed = misc + 1;
+  volatile uint32_t* odd = misc + 4;
+  const uint32_t failed_addr = base + M::MISC + 4;
+  const AcArgs& a = t.a;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  auto wait = [&](uint32_t bar, uint32_t parity) { return ptx::mbar_wait_abortable(base + bar, parity, failed_addr); };
+  auto give_up = [&](int stage) {
+    report_timeout(stage);
+    *failed = 1u;
+  };
+
+  if (threadIdx.x == 0) {
+    *failed = 0u;
+    for (int i = 0; i < 4; ++i) odd[i] = 0u;
+    for (int i = 0; i < AT_RING; ++i) { ptx::mbar_init(base + M::KV_FULL + 8 * i, 1); ptx::mbar_init(base + M::KV_EMPTY + 8 * i, 1); }
+    ptx::mbar_init(base + M::Q_FULL, 1);
+    ptx::mbar_init(base + M::Q_EMPTY, 1);
+    for (int i = 0; i < 2; ++i) {
+      ptx::mbar_init(base + M::S_FULL + 8 * i, 1);
+      ptx::mbar_init(base + M::P_FULL + 8 * i, 4);
+      ptx::mbar_init(base + M::O_FULL + 8 * i, 1);
+      ptx::mbar_init(base + M::V_READY + 8 * i, 2);
+    }
+    ptx::mbar_init(base + M::DRAIN, 1);
+    ptx::mbar_init_fence();
+    ptx::tma_prefetch_desc(&tmap_q);
+    ptx::tma_prefetch_desc(&tmap_k);
+    ptx::tma_prefetch_desc(&tmap_v);
+  }
+  if (warp == 1) {
+    ptx::tmem_alloc(base + M::MISC, 512);
+    ptx::tmem_relinquish();
+  }
+  ptx::tc_fence_before_sync();
+  __syncthreads();
+  ptx::tc_fence_after_sync();
+  const uint32_t tmem = misc[0];
+  pdl_enter();
+  AtCut* cuts = a.cuts + 2 * blockIdx.x;
+  if (threadIdx.x < 2) cuts[threadIdx.x].s = -1;
+  KvSeq q;
+  auto cost = [&](int s, int x) { return at_units(t, s, x, q); };
+  AcRun* run = reinterpret_cast<AcRun*>(sm + M::RUN);
+  ac_run_start(cost, a.c.n_seq, t.nx, a.c.n_kv, AT_THREADS, reinterpret_cast<long long*>(sm + M::PART), run);
+
+  AcWalk w(*run, t.nx, a.c.n_kv, a.c.n_seq);
+  const int tok_tile = t.tok_tile, slots_mask = (1 << a.c.page_shift) - 1;
+  // Has unit `u` a slot that some row of the item does not see?
+  auto masked = [&](int u) {
+    return (u + 1) * AT_KEYS > q.used + (a.b.parent ? 0 : w.x * 2 * tok_tile + 1);
+  };
+  bool more = w.start(cost);
+  if (warp == 0) {
+    // ------------------------------------------------------------------ producer
+    uint32_t e = 0, qn = 0;  // tiles put into the ring; items
+    bool ok = true;
+    const int page = 1 << a.c.page_shift, pieces = AT_KEYS >> a.c.page_shift;
+    const int piece = lane / NH, half = lane % NH;  // this lane's copy of a tile
+    const int none = a.c.n_pages * a.c.n_kv * page;  // a row behind the pool: such a copy fills with zeros
+    while (ok && more) {
+      const int end = q.used + (a.b.parent ? q.m : min(q.m, (w.x + 1) * 2 * tok_tile));
+      const int na = w.x * 2 * tok_tile + tok_tile < q.m ? 2 : 1;
+      if (!__any_sync(0xffffffffu, wait(M::Q_EMPTY, (qn & 1) ^ 1))) { ok = false; break; }
+      if (lane == 0) ptx::mbar_arrive_expect_tx(base + M::Q_FULL, na * NH * 128 * a.rep * tok_tile);
+      __syncwarp();
+      if (lane < na * NH)
+        ptx::tma_load_3d(base + M::Q + (lane / NH) * M::TILE + (lane % NH) * M::HALF, &tmap_q, 64 * (lane % NH), w.h * a.rep,
+                         q.t0 + (w.x * 2 + lane / NH) * tok_tile, base + M::Q_FULL);
+      ++qn;
+      auto row_of = [&](int u) {  // first row of this lane's page of unit u
+        const int slot = u * AT_KEYS + piece * page;
+        if (piece >= pieces || slot >= end) return none;
+        const int p = kv_page(a.c, w.s, slot);
+        return p < 0 ? none : (p * a.c.n_kv + w.h) * page;
+      };
+      int row = row_of(w.u0);
+      for (int u = w.u0; u < w.u1; ++u) {
+        const int row_next = u + 1 < w.u1 ? row_of(u + 1) : 0;
+#pragma unroll
+        for (int kv = 0; kv < 2; ++kv, ++e) {
+          const uint32_t slot = e % AT_RING;
+          if (!__any_sync(0xffffffffu, wait(M::KV_EMPTY + 8 * slot, ((e / AT_RING) & 1) ^ 1))) { ok = false; break; }
+          if (lane == 0) ptx::mbar_arrive_expect_tx(base + M::KV_FULL + 8 * slot, M::TILE);
+          __syncwarp();
+          if (piece < pieces)
+            ptx::tma_load_2d(base + M::RING + slot * M::TILE + half * M::HALF + piece * page * 128, kv ? &tmap_v : &tmap_k, 64 * half,
+                             row, base + M::KV_FULL + 8 * slot);
+        }
+        if (!ok) break;
+        row = row_next;
+      }
+      more = w.next(cost);
+      __syncwarp();
+    }
+    if (!ok && lane == 0) give_up(AT_WAIT_LOAD);
+  } else if (warp == 1) {
+    // ------------------------------------------------------------------ MMA issuer
+    constexpr uint32_t id_s = ptx::idesc_bf16(128, AT_KEYS, false), id_o = ptx::idesc_bf16(128, HD, true);
+    uint32_t e = 0, qn = 0, pn[2] = {0, 0};
+    bool ok = true;
+    auto all_wait = [&](uint32_t bar, uint32_t parity) { return __any_sync(0xffffffffu, wait(bar, parity)); };
+    auto scores = [&](int x, uint32_t slot) {
+      if (ptx::elect_one()) {
+        const uint64_t qd = ptx::smem_desc_sw128(base + M::Q + x * M::TILE), kd = ptx::smem_desc_sw128(base + M::RING + slot * M::TILE);
+#pragma unroll
+        for (int k = 0; k < HD / 16; ++k) {
+          const uint32_t off = ((k / 4) * M::HALF + (k % 4) * 32) >> 4;
+          ptx::mma_bf16_ss(tmem + 128 * x, qd + off, kd + off, id_s, k != 0);
+        }
+        ptx::mma_commit(base + M::S_FULL + 8 * x);
+      }
+      __syncwarp();
+    };
+    auto commit = [&](uint32_t bar) {
+      if (ptx::elect_one()) ptx::mma_commit(base + bar);
+      __syncwarp();
+    };
+    while (ok && more) {
+      const int na = w.x * 2 * tok_tile + tok_tile < q.m ? 2 : 1;
+      ok = all_wait(M::Q_FULL, qn & 1) && all_wait(M::KV_FULL + 8 * (e % AT_RING), (e / AT_RING) & 1);
+      if (!ok) break;
+      ++qn;
+      ptx::tc_fence_after_sync();
+      for (int x = 0; x < na; ++x) scores(x, e % AT_RING);
+      commit(M::KV_EMPTY + 8 * (e % AT_RING));
+      if (w.u1 - w.u0 == 1) commit(M::Q_EMPTY);
+      ++e;
+      for (int u = w.u0; ok && u < w.u1; ++u) {
+        const uint32_t v_slot = e % AT_RING, v_par = (e / AT_RING) & 1, k_slot = (e + 1) % AT_RING;
+        const bool last = u + 1 == w.u1;
+        ok = all_wait(M::V_READY + 8 * (v_slot >> 1), v_par);
+        for (int x = 0; ok && x < na; ++x) {
+          ok = all_wait(M::P_FULL + 8 * x, pn[x] & 1);
+          if (!ok) break;
+          ++pn[x];
+          ptx::tc_fence_after_sync();
+          if (ptx::elect_one()) {
+            const uint64_t vd = ptx::smem_desc_mn_sw128(base + M::RING + v_slot * M::TILE, M::HALF);
+#pragma unroll
+            for (int k = 0; k < AT_KEYS / 16; ++k)
+              ptx::mma_bf16_ts(tmem + 256 + 128 * x, tmem + 128 * x + 8 * k, vd + k * (2048 >> 4), id_o, u != w.u0 || k != 0);
+            if (last) ptx::mma_commit(base + M::O_FULL + 8 * x);
+          }
+          __syncwarp();
+          if (!last) {
+            if (x == 0) ok = all_wait(M::KV_FULL + 8 * k_slot, ((e + 1) / AT_RING) & 1);
+            if (!ok) break;
+            scores(x, k_slot);
+          }
+        }
+        if (!ok) break;
+        commit(M::KV_EMPTY + 8 * v_slot);
+        ++e;
+        if (!last) {
+          commit(M::KV_EMPTY + 8 * k_slot);
+          ++e;
+          if (u + 2 == w.u1) commit(M::Q_EMPTY);
+        }
+      }
+      more = w.next(cost);
+      __syncwarp();
+    }
+    if (!ok && lane == 0) give_up(AT_WAIT_MMA);
+  } else if (warp < 4) {
+    // ------------------------------------------------------------------ values of masked units
+    uint32_t e = 1, item = 0;
+    bool ok = true;
+    while (ok && more) {
+      const int end = q.used + q.m;
+      for (int u = w.u0; u < w.u1; ++u, e += 2) {
+        const uint32_t slot = e % AT_RING;
+        if (!__any_sync(0xffffffffu, wait(M::KV_FULL + 8 * slot, (e / AT_RING) & 1))) { ok = false; break; }
+        if (masked(u)) {
+          const uint32_t tile = base + M::RING + slot * M::TILE;
+          bool found = false;
+          for (int i = (warp - 2) * 32 + lane; i < AT_KEYS * HD / 8; i += 64) {
+            const int r = i & 127, c16 = i >> 7;  // key, 16-byte piece of its row
+            const int at = u * AT_KEYS + r;
+            if (at < q.used) continue;
+            const uint32_t addr = tile + (c16 >> 3) * M::HALF + r * 128 + (c16 & 7) * 16;
+            bool drop = at >= end;
+            if (!drop && a.b.parent) drop = a.b.parent[q.t0 + at - q.used] == BITRL_PARENT_PAD;
+            uint4 v = ptx::lds128(addr);
+            uint32_t x[4] = {v.x, v.y, v.z, v.w};
+            bool touch = drop;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              const bool lo = (x[j] & 0x7f80u) == 0x7f80u, hi = (x[j] & 0x7f800000u) == 0x7f800000u;
+              if (!drop && (lo || hi)) { found = true; touch = true; }
+              if (drop || lo) x[j] &= 0xffff0000u;
+              if (drop || hi) x[j] &= 0x0000ffffu;
+            }
+            if (touch) ptx::sts128(addr, make_uint4(x[0], x[1], x[2], x[3]));
+          }
+          if (__any_sync(0xffffffffu, found) && lane == 0) odd[item & 3] = item + 1;
+          ptx::fence_proxy_async_smem();
+        }
+        __syncwarp();
+        if (lane == 0) ptx::mbar_arrive(base + M::V_READY + 8 * (slot >> 1));
+      }
+      ++item;
+      if (ok) more = w.next(cost);
+      __syncwarp();
+    }
+    if (!ok && lane == 0) give_up(AT_WAIT_FIX);
+  } else {
+    // ------------------------------------------------------------------ softmax, one row per thread
+    const int x = (warp - 4) >> 2;  // row tile
+    const uint32_t lane_base = static_cast<uint32_t>((warp & 3) * 32) << 16;
+    const int r = (warp & 3) * 32 + lane, r_tok = r / a.rep, r_head = r - r_tok * a.rep;
+    const uint32_t s_addr = tmem + 128 * x + lane_base, o_addr = tmem + 256 + 128 * x + lane_base;
+    uint32_t sn = 0, on = 0, item = 0;
+    bool ok = true;
+    while (ok && more) {
+      const int tok_first = (w.x * 2 + x) * tok_tile, tok = tok_first + r_tok;
+      if (tok_first < q.m) {
+        const bool exists = r_tok < tok_tile && tok < q.m;
+        const int tk = min(tok, q.m - 1);
+        float m_ref = -INFINITY, l = 0.0f;
+        for (int u = w.u0; u < w.u1; ++u, ++sn) {
+          if (!__any_sync(0xffffffffu, wait(M::S_FULL + 8 * x, sn & 1))) { ok = false; break; }
+          ptx::tc_fence_after_sync();
+          uint32_t s[4][32];
+#pragma unroll
+          for (int c = 0; c < 4; ++c) ptx::tmem_ld_32x32b_x32(s_addr + 32 * c, s[c]);
+          ptx::tmem_ld_wait();
+          if (masked(u)) {
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+              const uint32_t seen = at_seen(a, q, tk, u * AT_KEYS + 32 * c);
+#pragma unroll
+              for (int i = 0; i < 32; ++i) s[c][i] = (seen >> i) & 1u ? s[c][i] : 0xff800000u;
+            }
+          }
+          float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+          for (int c = 0; c < 4; ++c)
+#pragma unroll
+            for (int i = 0; i < 32; ++i) mx[i & 3] = fmaxf(mx[i & 3], __uint_as_float(s[c][i]));
+          const float m2 = __fmul_rn(fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])), a.scale2);
+          if (u == w.u0) {
+            m_ref = m2;
+          } else if (__any_sync(0xffffffffu, m2 > m_ref + AT_GROWTH || (m_ref == -INFINITY && m2 > m_ref))) {
+            const float m_new = fmaxf(m_ref, m2);
+            const float f = m_new == m_ref ? 1.0f : ac_exp2(m_ref - m_new);
+            m_ref = m_new;
+            l = __fmul_rn(l, f);
+#pragma unroll
+            for (int c = 0; c < HD / 32; ++c) {
+              uint32_t o[32];
+              ptx::tmem_ld_32x32b_x32(o_addr + 32 * c, o);
+              ptx::tmem_ld_wait();
+#pragma unroll
+              for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__fmul_rn(__uint_as_float(o[i]), f));
+              ptx::tmem_st_32x32b_x32(o_addr + 32 * c, o);
+            }
+          }
+          const float sub = m_ref == -INFINITY ? 0.0f : -m_ref;
+          float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+          for (int c = 0; c < 4; c += 2) {
+            uint32_t p[32];
+#pragma unroll
+            for (int i = 0; i < 32; ++i) {
+              const int cc = c + (i >> 4), j = 2 * (i & 15);
+              const float p0 = ac_exp2(fmaf(__uint_as_float(s[cc][j]), a.scale2, sub));
+              const float p1 = ac_exp2(fmaf(__uint_as_float(s[cc][j + 1]), a.scale2, sub));
+              sum[i & 1] += p0;
+              sum[2 + (i & 1)] += p1;
+              p[i] = pack_bf16x2(p0, p1);
+            }
+            ptx::tmem_st_32x32b_x32(s_addr + 16 * c, p);
+          }
+          l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+          ptx::tmem_st_wait();
+          ptx::tc_fence_before_sync();
+          __syncwarp();
+          if (lane == 0) ptx::mbar_arrive(base + M::P_FULL + 8 * x);
+        }
+        if (!ok) break;
+        if (!__any_sync(0xffffffffu, wait(M::O_FULL + 8 * x, on & 1))) { ok = false; break; }
+        ++on;
+        ptx::tc_fence_after_sync();
+        const bool whole = w.u0 == 0 && w.u1 == w.units;
+        const bool fix = odd[item & 3] == item + 1;
+        const bool pad = a.b.parent && exists && a.b.parent[q.t0 + tok] == BITRL_PARENT_PAD;
+        const bool none = l == 0.0f || pad;
+        const float inv = !whole ? 1.0f : none ? 0.0f : __fdiv_rn(1.0f, l);
+        const long long row = static_cast<long long>(q.t0 + tok) * a.n_heads + w.h * a.rep + r_head;
+        const int cut = 2 * blockIdx.x + (w.u0 == 0 ? 1 : 0);
+        const int cut_row = x * tok_tile * a.rep + r;
+        float* part = a.part_o + (static_cast<long long>(cut) * t.rows_cap + cut_row) * HD;
+#pragma unroll 1
+        for (int c = 0; c < HD / 32; ++c) {
+          uint32_t o[32];
+          ptx::tmem_ld_32x32b_x32(o_addr + 32 * c, o);
+          ptx::tmem_ld_wait();
+          if (fix && exists && !pad) {  // rare: values that are not finite, of masked units, for the rows that see them
+            for (int at = max(q.used, w.u0 * AT_KEYS); at < min(q.used + q.m, w.u1 * AT_KEYS); ++at) {
+              if (!masked(at / AT_KEYS) || !(at_seen(a, q, tok, at) & 1u)) continue;
+              const int pg = kv_page(a.c, w.s, at);
+              if (pg < 0) continue;
+              const unsigned short* v = a.c.v + (kv_row(a.c, 0, pg, w.h) + (at & slots_mask)) * HD + 32 * c;
+#pragma unroll
+              for (int i = 0; i < 32; ++i) {
+                const unsigned short b = v[i];
+                if ((b & 0x7f80u) == 0x7f80u) o[i] = __float_as_uint(__uint_as_float(o[i]) + bf16_bits_to_float(b));
+              }
+            }
+          }
+          if (!exists) continue;
+          if (whole) {
+            uint4* dst = reinterpret_cast<uint4*>(a.att + row * HD + 32 * c);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              uint32_t b[4];
+#pragma unroll
+              for (int j = 0; j < 4; ++j)
+                b[j] = none ? 0u : pack_bf16x2(__fmul_rn(__uint_as_float(o[8 * i + 2 * j]), inv), __fmul_rn(__uint_as_float(o[8 * i + 2 * j + 1]), inv));
+              dst[i] = make_uint4(b[0], b[1], b[2], b[3]);
+            }
+          } else {
+            uint4* dst = reinterpret_cast<uint4*>(part + 32 * c);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) dst[i] = make_uint4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
+          }
+        }
+        if (exists) {
+          if (whole) a.lse[row] = none ? INFINITY : m_ref + __log2f(l);
+          else a.part_ml[static_cast<long long>(cut) * t.rows_cap + cut_row] = make_float2(m_ref, l);
+        }
+        if (!whole && threadIdx.x == 128) cuts[w.u0 == 0 ? 1 : 0] = AtCut{w.s, w.x, w.h, w.u1 == w.units};
+        ptx::tc_fence_before_sync();
+      }
+      ++item;
+      more = w.next(cost);
+      __syncwarp();
+    }
+    if (!ok && lane == 0) give_up(AT_WAIT_SOFTMAX);
+  }
+
+  // ---- teardown: every role leaves through here, also after a timeout ----
+  __syncwarp();
+  ptx::tc_fence_before_sync();
+  __syncthreads();
+  if (*failed) {
+    // Failure path only: copies and MMAs that nobody waited for may still be in flight.
+    if (warp == 1) {
+      if (ptx::elect_one()) ptx::mma_commit(base + M::DRAIN);
+      __syncwarp();
+      ptx::mbar_wait(base + M::DRAIN, 0, 2000000LL);
+    }
+    const long long t0 = clock64();
+    while (clock64() - t0 < 2000000LL) {}
+    __syncthreads();
+  }
+  if (warp == 1) {
+    ptx::tc_fence_after_sync();
+    ptx::tmem_dealloc(tmem, 512);
+  }
+}
+
+// Joins the cut items: the CTA in which an item begins and those after it each left a part.  Block (c, y) takes 32 rows of the
+// item that begins in CTA c.
+template <int HD>
+__global__ void __launch_bounds__(256) attn_tiles_join_kernel(const __grid_constant__ AtArgs t, int n_ctas) {
+  pdl_enter();
+  const AcArgs& a = t.a;
+  const int c0 = blockIdx.x;
+  const AtCut head = a.cuts[2 * c0 + 1];
+  if (head.s < 0) return;
+  KvSeq q;
+  if (!kv_seq(a.c, a.b, head.s, q)) return;
+  constexpr int PER = HD / 8;  // dimensions of a thread
+  const int cut_row = blockIdx.y * 32 + threadIdx.x / 8, d0 = (threadIdx.x % 8) * PER;
+  const int tile_rows = t.tok_tile * a.rep;
+  const int x = cut_row / tile_rows, r = cut_row - x * tile_rows;
+  const int tok = (head.x * 2 + x) * t.tok_tile + r / a.rep;
+  if (x > 1 || tok >= q.m) return;
+  // the parts: slot 1 of this CTA, then slot 0 of the following ones up to the one in which the item ends (a CTA whose run is
+  // empty has none)
+  auto part_at = [&](int c) { return static_cast<long long>(c == c0 ? 2 * c0 + 1 : 2 * c) * t.rows_cap + cut_row; };
+  float m_all = a.part_ml[part_at(c0)].x;
+  int last = c0;
+  while (last + 1 < n_ctas) {
+    const AtCut cut = a.cuts[2 * ++last];
+    if (cut.s < 0) continue;
+    m_all = fmaxf(m_all, a.part_ml[part_at(last)].x);
+    if (cut.ends) break;
+  }
+  float l = 0.0f, acc[PER];
+#pragma unroll
+  for (int i = 0; i < PER; ++i) acc[i] = 0.0f;
+  for (int c = c0; c <= last; ++c) {
+    if (c != c0 && a.cuts[2 * c].s < 0) continue;
+    const float2 ml = a.part_ml[part_at(c)];
+    if (ml.x == -INFINITY) continue;
+    const float f = ac_exp2(ml.x - m_all);
+    l = fmaf(ml.y, f, l);
+    const float4* p = reinterpret_cast<const float4*>(a.part_o + part_at(c) * HD + d0);
+#pragma unroll
+    for (int i = 0; i < PER / 4; ++i) {
+      const float4 v = p[i];
+      acc[4 * i] = fmaf(v.x, f, acc[4 * i]);
+      acc[4 * i + 1] = fmaf(v.y, f, acc[4 * i + 1]);
+      acc[4 * i + 2] = fmaf(v.z, f, acc[4 * i + 2]);
+      acc[4 * i + 3] = fmaf(v.w, f, acc[4 * i + 3]);
+    }
+  }
+  const bool none = l == 0.0f || (a.b.parent && a.b.parent[q.t0 + tok] == BITRL_PARENT_PAD);
+  const float inv = none ? 0.0f : __fdiv_rn(1.0f, l);
+  const long long row = static_cast<long long>(q.t0 + tok) * a.n_heads + head.h * a.rep + r % a.rep;
+#pragma unroll
+  for (int i = 0; i < PER; i += 8) {
+    uint32_t b[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) b[j] = none ? 0u : pack_bf16x2(__fmul_rn(acc[i + 2 * j], inv), __fmul_rn(acc[i + 2 * j + 1], inv));
+    *reinterpret_cast<uint4*>(a.att + row * HD + d0 + i) = make_uint4(b[0], b[1], b[2], b[3]);
+  }
+  if (d0 == 0) a.lse[row] = none ? INFINITY : m_all + __log2f(l);
+}
+
+// ---- host --------------------------------------------------------------------------------------------------------------
+constexpr int AC_FEW_ROWS = AR_ROWS;  // at most so many rows per sequence and kv head take the few-rows kernel
+
+struct AcPlan {
+  bool few;                                // few rows: attn_rows_kernel; else tiles
+  int row_tiles, splits, split_keys;       // few rows
+  int tok_tile, nx, rows_cap, ctas;        // tiles
+  size_t lse_bytes, ml_bytes, o_bytes, cut_bytes, anc_bytes, ok_bytes;
+  size_t bytes() const { return lse_bytes + ml_bytes + o_bytes + cut_bytes + anc_bytes + ok_bytes; }
+  // Does every grid and every coordinate of the call fit?
+  bool launchable(const KvView& c) const {
+    const long long heads = static_cast<long long>(c.n_seq) * c.n_kv;
+    const long long key_tiles = ((c.max_pages << c.page_shift) + AM_KEYS - 1) / AM_KEYS;
+    return heads * row_tiles <= INT_MAX / splits && heads <= INT_MAX / key_tiles &&
+           (static_cast<long long>(c.n_pages) * c.n_kv + 1) << c.page_shift <= INT_MAX;
+  }
+};
+
+inline size_t ac_up(size_t v) { return (v + 255) / 256 * 256; }
+
+// Sizes alone decide: the lengths are known on the device only.
+inline AcPlan ac_plan(const KvView& c, int T, int max_new, int n_heads) {
+  AcPlan p = {};
+  const int rep = n_heads / c.n_kv;
+  const long long rows = static_cast<long long>(max_new) * rep;
+  p.few = rows <= AC_FEW_ROWS;
+  p.row_tiles = p.splits = 1;
+  p.lse_bytes = ac_up(static_cast<size_t>(T) * n_heads * 4);
+  p.anc_bytes = max_new <= BITRL_TREE_MAX_TOKENS ? ac_up(static_cast<size_t>(T) * AC_TREE_WORDS * 4) : 0;
+  p.ok_bytes = ac_up(static_cast<size_t>(c.n_seq) * 4);
+  if (p.few) {
+    // ranges of keys are made so that even one row tile per (sequence, kv head) fills the SMs several times over
+    const long long items = static_cast<long long>(c.n_seq) * c.n_kv;
+    const int room = c.max_pages << c.page_shift;
+    const long long most = (room + 255) / 256;  // no range below 256 slots
+    long long splits = (148LL * 8 + items - 1) / items;
+    if (splits > most) splits = most;
+    p.split_keys = static_cast<int>(((room + splits - 1) / splits + 63) / 64 * 64);
+    p.splits = (room + p.split_keys - 1) / p.split_keys;
+    p.ml_bytes = p.splits > 1 ? ac_up(static_cast<size_t>(p.splits) * T * n_heads * 8) : 0;
+    p.o_bytes = p.splits > 1 ? ac_up(static_cast<size_t>(p.splits) * T * n_heads * c.hd * 4) : 0;
+  } else {
+    p.tok_tile = 128 / rep;
+    p.nx = (max_new + 2 * p.tok_tile - 1) / (2 * p.tok_tile);
+    p.rows_cap = static_cast<int>(rows < 256 ? rows : 256);
+    p.ctas = sm_count();
+    p.ml_bytes = ac_up(static_cast<size_t>(2 * p.ctas) * p.rows_cap * 8);
+    p.o_bytes = ac_up(static_cast<size_t>(2 * p.ctas) * p.rows_cap * c.hd * 4);
+    p.cut_bytes = ac_up(static_cast<size_t>(2 * p.ctas) * sizeof(AtCut));
+  }
+  return p;
+}
+
+template <class K>
+bitrl_status ac_smem(K kernel, size_t bytes, bool (&done)[64]) {
+  int dev = 0;
+  BITRL_CUDA(cudaGetDevice(&dev));
+  if (dev >= 0 && dev < 64 && !done[dev]) {
+    BITRL_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(bytes)));
+    done[dev] = true;
+  }
+  return BITRL_OK;
+}
+
+// Tensor map over bf16 data, 128-byte swizzle, boxes of 64 innermost elements.
+inline bitrl_status ac_tensor_map(CUtensorMap* m, const void* p, int dims, const cuuint64_t* size, const cuuint64_t* stride,
+                                  const cuuint32_t* box) {
+  const encode_tiled_fn encode = get_encode_tiled();
+  if (!encode) return cuda_fail(cudaErrorNotSupported);
+  const cuuint32_t ones[3] = {1, 1, 1};
+  const CUresult r = encode(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, dims, const_cast<void*>(p), size, stride, box, ones,
+                            CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  return r == CUDA_SUCCESS ? BITRL_OK : cuda_fail(cudaErrorInvalidValue);
+}
+
+template <int HD>
+bitrl_status launch_attention_cached_hd(const AcArgs& a, const AcPlan& p, bool mass, cudaStream_t st) {
+  bitrl_status s;
+  if (p.few) {
+    static bool done[64] = {false};
+    if ((s = ac_smem(attn_rows_kernel<HD>, ar_smem_bytes<HD>(), done)) != BITRL_OK) return s;
+    BITRL_CUDA(launch_pdl(attn_rows_kernel<HD>, dim3(static_cast<unsigned>(static_cast<long long>(a.c.n_seq) * a.c.n_kv * p.splits)),
+                          dim3(AR_THREADS), ar_smem_bytes<HD>(), st, a));
+    count_launch(1);
+    if (p.splits > 1) {
+      const unsigned per_seq = static_cast<unsigned>((static_cast<long long>(a.b.max_new) * a.n_heads + 3) / 4);
+      BITRL_CUDA(launch_pdl(attn_join_kernel<HD>, dim3(per_seq * a.c.n_seq), dim3(128), 0, st, a));
+      count_launch(1);
+    }
+  } else {
+    CUtensorMap mq, mk, mv;
+    const int page = 1 << a.c.page_shift;
+    const cuuint64_t kv_size[2] = {HD, static_cast<cuuint64_t>(a.c.n_pages) * a.c.n_kv * page}, kv_stride[1] = {HD * 2};
+    const cuuint32_t kv_box[2] = {64, static_cast<cuuint32_t>(page)};
+    const cuuint64_t q_size[3] = {HD, static_cast<cuuint64_t>(a.n_heads), static_cast<cuuint64_t>(a.b.T)};
+    const cuuint64_t q_stride[2] = {HD * 2, static_cast<cuuint64_t>(a.n_heads) * HD * 2};
+    const cuuint32_t q_box[3] = {64, static_cast<cuuint32_t>(a.rep), static_cast<cuuint32_t>(p.tok_tile)};
+    if ((s = ac_tensor_map(&mq, a.q, 3, q_size, q_stride, q_box)) != BITRL_OK) return s;
+    if ((s = ac_tensor_map(&mk, a.c.k, 2, kv_size, kv_stride, kv_box)) != BITRL_OK) return s;
+    if ((s = ac_tensor_map(&mv, a.c.v, 2, kv_size, kv_stride, kv_box)) != BITRL_OK) return s;
+    static bool done[64] = {false};
+    if ((s = ac_smem(attn_tiles_kernel<HD>, AtSmem<HD>::LAUNCH, done)) != BITRL_OK) return s;
+    const AtArgs t{a, p.tok_tile, p.nx, p.rows_cap};
+    BITRL_CUDA(launch_pdl(attn_tiles_kernel<HD>, dim3(p.ctas), dim3(AT_THREADS), AtSmem<HD>::LAUNCH, st, mq, mk, mv, t));
+    BITRL_CUDA(launch_pdl(attn_tiles_join_kernel<HD>, dim3(p.ctas, (p.rows_cap + 31) / 32), dim3(256), 0, st, t, p.ctas));
+    count_launch(2);
+  }
+  if (mass) {
+    static bool done[64] = {false};
+    if ((s = ac_smem(attn_mass_kernel<HD>, am_smem_bytes<HD>(), done)) != BITRL_OK) return s;
+    const unsigned tiles = static_cast<unsigned>(((a.c.max_pages << a.c.page_shift) + AM_KEYS - 1) / AM_KEYS);
+    BITRL_CUDA(launch_pdl(attn_mass_kernel<HD>, dim3(tiles * a.c.n_kv * a.c.n_seq), dim3(AM_THREADS), am_smem_bytes<HD>(), st, a));
+    count_launch(1);
+  }
+  return BITRL_OK;
+}
+
+bitrl_status launch_attention_cached(const KvView& c, const KvBatch& b, const void* q, int n_heads, bool mass, void* att,
+                                     void* workspace, cudaStream_t st) {
+  const AcPlan p = ac_plan(c, b.T, b.max_new, n_heads);
+  unsigned char* w = static_cast<unsigned char*>(workspace);
+  auto take = [&](size_t bytes) {
+    unsigned char* at = w;
+    w += bytes;
+    return at;
+  };
+  AcArgs a;
+  a.c = c;
+  a.b = b;
+  a.q = static_cast<const unsigned short*>(q);
+  a.att = static_cast<unsigned short*>(att);
+  a.n_heads = n_heads;
+  a.rep = n_heads / c.n_kv;
+  a.scale2 = static_cast<float>(1.4426950408889634 / sqrt(static_cast<double>(c.hd)));
+  a.row_tiles = p.row_tiles;
+  a.splits = p.splits;
+  a.split_keys = p.split_keys;
+  a.lse = reinterpret_cast<float*>(take(p.lse_bytes));
+  a.part_ml = reinterpret_cast<float2*>(take(p.ml_bytes));
+  a.part_o = reinterpret_cast<float*>(take(p.o_bytes));
+  a.cuts = reinterpret_cast<AtCut*>(take(p.cut_bytes));
+  uint32_t* anc = reinterpret_cast<uint32_t*>(take(p.anc_bytes));
+  int* ok = reinterpret_cast<int*>(take(p.ok_bytes));
+  a.anc = b.parent ? anc : nullptr;
+  a.tree_ok = b.parent ? ok : nullptr;
+  if (b.parent) {
+    BITRL_CUDA(launch_pdl(attn_tree_kernel, dim3(c.n_seq), dim3(BITRL_TREE_MAX_TOKENS), 0, st, c, b, anc, ok));
+    count_launch(1);
+  }
+  return c.hd == 128 ? launch_attention_cached_hd<128>(a, p, mass, st) : launch_attention_cached_hd<64>(a, p, mass, st);
+}
+
+}  // namespace bitrl

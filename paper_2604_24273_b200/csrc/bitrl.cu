@@ -111,6 +111,7 @@ static bitrl_status check_arch() {
 #include "attention.cuh"
 #include "kv_cache.cuh"
 #include "attention_cached.cuh"
+#include "attention_cached_tc.cuh"
 #include "heads.cuh"
 #include "gemm_w8.cuh"
 #include "w4.cuh"
@@ -613,6 +614,7 @@ bitrl_status kv_check_batch(const bitrl_kv_cache_t* c, int32_t layer, int32_t T,
                             const int32_t* parent, int32_t n_heads) {
   if (layer < 0 || layer >= c->n_layers || T < 0 || max_new < 0) return BITRL_ERR_SHAPE;
   if (n_heads < 1 || n_heads % c->n_kv_heads != 0) return BITRL_ERR_SHAPE;
+  if (n_heads / c->n_kv_heads > BITRL_KV_MAX_GROUP) return BITRL_ERR_LIMIT;
   if (!state_off && static_cast<long long>(c->n_seq) * max_new != T) return BITRL_ERR_SHAPE;
   if (parent && max_new > BITRL_TREE_MAX_TOKENS) return BITRL_ERR_LIMIT;
   if (max_new > static_cast<long long>(c->max_pages) * c->page_tokens) return BITRL_ERR_SHAPE;
@@ -650,7 +652,9 @@ bitrl_status bitrl_kv_append(const bitrl_kv_cache_t* cache, int32_t layer, const
 }
 
 size_t bitrl_attention_cached_workspace_bytes(const bitrl_kv_cache_t* cache, int32_t T, int32_t max_new_len, int32_t n_heads) {
-  if (kv_check(cache) != BITRL_OK || T < 1 || max_new_len < 1 || n_heads < 1 || n_heads % cache->n_kv_heads != 0) return 0;
+  if (kv_check(cache) != BITRL_OK || T < 1 || max_new_len < 1 || n_heads < 1 || n_heads % cache->n_kv_heads != 0 ||
+      n_heads / cache->n_kv_heads > BITRL_KV_MAX_GROUP)
+    return 0;
   return ac_plan(kv_view(cache, 0), T, max_new_len, n_heads).bytes();
 }
 

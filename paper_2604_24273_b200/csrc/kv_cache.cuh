@@ -64,7 +64,7 @@ __device__ __forceinline__ bool kv_seq(const KvView& c, const KvBatch& b, int s,
   const long long room = static_cast<long long>(c.max_pages) << c.page_shift;
   if (q.t0 < 0 || q.m < 0 || q.m > b.max_new || static_cast<long long>(q.t0) + q.m > b.T || q.used < 0 ||
       static_cast<long long>(q.used) + q.m > room || (b.parent && q.m > BITRL_TREE_MAX_TOKENS)) {
-    if (threadIdx.x == 0) report_status(BITRL_ERR_SHAPE, KV_STAGE_BAD_SEQ);
+    report_status(BITRL_ERR_SHAPE, KV_STAGE_BAD_SEQ);
     return false;
   }
   return true;

@@ -133,6 +133,14 @@ __device__ __forceinline__ void tma_load_2d(uint32_t dst, const void* tmap, int3
       "l"(tmap), "r"(c0), "r"(c1), "r"(bar)
       : "memory");
 }
+// 3-D tiled TMA load (this CTA only).
+__device__ __forceinline__ void tma_load_3d(uint32_t dst, const void* tmap, int32_t c0, int32_t c1, int32_t c2, uint32_t bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::
+          "r"(dst),
+      "l"(tmap), "r"(c0), "r"(c1), "r"(c2), "r"(bar)
+      : "memory");
+}
 __device__ __forceinline__ void tma_prefetch_desc(const void* tmap) {
   asm volatile("prefetch.tensormap [%0];" ::"l"(tmap) : "memory");
 }
@@ -176,6 +184,24 @@ __device__ __forceinline__ void mma_i8_ss(uint32_t d_tmem, uint64_t adesc, uint6
       "setp.ne.b32 p, %4, 0;\n\t"
       "tcgen05.mma.cta_group::1.kind::i8 [%0], %1, %2, %3, p;\n\t}" ::"r"(d_tmem),
       "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+// D[tmem] (+)= A[smem desc] * B[smem desc], bf16 operands (both), fp32 accumulate, K = 16.  One thread issues.
+__device__ __forceinline__ void mma_bf16_ss(uint32_t d_tmem, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d_tmem),
+      "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+// The same with A in tensor memory: 128 rows, 16 k as eight 32-bit columns of two bf16 each.
+__device__ __forceinline__ void mma_bf16_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t bdesc, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d_tmem),
+      "r"(a_tmem), "l"(bdesc), "r"(idesc), "r"(accumulate)
       : "memory");
 }
 // Arrives on the mbarrier once all MMAs issued so far by this thread have completed.
@@ -377,6 +403,24 @@ __device__ __forceinline__ uint64_t smem_desc_sw128(uint32_t smem_addr) {
   d |= static_cast<uint64_t>(1) << 46;                      // descriptor version for sm_100
   d |= static_cast<uint64_t>(2) << 61;                      // layout type: 128-byte swizzle
   return d;
+}
+
+// The same for an operand whose M/N dimension is contiguous (rows of 64 16-bit elements per k, 128-byte swizzle): 8-row
+// groups of k are 1024 bytes apart, blocks of 64 elements of the M/N dimension `block_bytes`.
+__device__ __forceinline__ uint64_t smem_desc_mn_sw128(uint32_t smem_addr, uint32_t block_bytes) {
+  uint64_t d = smem_desc_sw128(smem_addr);
+  d &= ~(static_cast<uint64_t>(0x3FFF) << 16);
+  d |= static_cast<uint64_t>(block_bytes >> 4) << 16;  // leading byte offset: the next block of the M/N dimension
+  return d;
+}
+
+// Instruction descriptor for kind::f16 with bf16 operands and an fp32 accumulator; A is K-major.
+__host__ __device__ constexpr uint32_t idesc_bf16(int mma_m, int mma_n, bool b_mn_major) {
+  return (1u << 4)                                     // D format: F32
+         | (1u << 7) | (1u << 10)                      // A, B format: BF16
+         | ((b_mn_major ? 1u : 0u) << 16)              // B major
+         | (static_cast<uint32_t>(mma_n >> 3) << 17)   // N / 8
+         | (static_cast<uint32_t>(mma_m >> 4) << 24);  // M / 16
 }
 
 // Instruction descriptor for kind::i8: D int32, A unsigned 8-bit, B signed 8-bit, both K-major.

@@ -537,3 +537,64 @@ def test_an_episode_step_by_step(B):
                 p = after["pos"][0][pg, h, at].tolist()
                 assert len(set(p)) == len(p) and set(range(max(0, int(after["seen"][s]) - recent), int(after["seen"][s]))) <= set(p)
     B.poll_status()
+
+
+def dense(c, q, off, nh, parent=None):
+    """att and added mass in 64 bits on the GPU, one (sequence, kv head) at a time, with the tolerances of ref.attend."""
+    nkv, hd = c["k"].shape[2], c["k"].shape[4]
+    rep = nh // nkv
+    att, tol = (torch.zeros(q.shape[0], nh, hd, dtype=torch.float64, device="cuda") for _ in range(2))
+    add, mtol = (torch.zeros(c["mass"].shape[1:], dtype=torch.float64, device="cuda") for _ in range(2))
+    k0, v0, table, q = c["k"][0].cuda(), c["v"][0].cuda(), c["page_table"].cuda(), q.cuda()
+    page = k0.shape[2]
+    for s in range(len(off) - 1):
+        t0, m, u = int(off[s]), int(off[s + 1] - off[s]), int(c["used"][s])
+        if m == 0:
+            continue
+        slot = torch.arange(u + m, device="cuda")
+        pg, at = table[s, slot // page].long(), slot % page
+        sees = torch.ones(m, u + m, dtype=torch.bool, device="cuda").tril(u)
+        if parent is not None:
+            sees[:, u:] = False
+            for i in range(m):
+                chain = ref.above(parent[t0 : t0 + m].tolist(), i)
+                sees[i, : u] = bool(chain)
+                sees[i, [u + j for j in chain]] = True
+        for h in range(nkv):
+            k, v = k0[pg, h, at].double(), v0[pg, h, at].double()
+            v = torch.where(sees.any(0)[:, None], v, 0.0)
+            k = torch.where(sees.any(0)[:, None], k, 0.0)
+            x = q[t0 : t0 + m].double().reshape(m, nh, hd)[:, h * rep : (h + 1) * rep].transpose(0, 1)
+            sc = (x @ k.T / hd**0.5).masked_fill(~sees, -math.inf)
+            p = torch.where(sees, torch.softmax(sc, 2), 0.0)
+            d = 2 * hd * 2.0**-23 * float((x.abs() @ k.abs().T).max()) / hd**0.5 + 2.0**-21 + (u + m) * 2.0**-23
+            o = p @ v
+            att[t0 : t0 + m, h * rep : (h + 1) * rep] = o.transpose(0, 1)
+            tol[t0 : t0 + m, h * rep : (h + 1) * rep] = (2.0**-8 * o.abs() + (2.0**-8 + d) * (p @ v.abs())).transpose(0, 1)
+            add[pg, h, at] += p.sum((0, 1))
+            mtol[pg, h, at] += p.sum((0, 1)) * (d + m * rep * 2.0**-23)
+    return att, add, tol, mtol
+
+
+@pytest.mark.parametrize("nh,nkv,hd,page,used,news,is_tree", [
+    (20, 5, 128, 64, [4100], [1500], False), (7, 1, 64, 32, [900, 0, 3000], [700, 333, 40], False), (4, 4, 128, 128, [0], [2100], False),
+    (20, 5, 128, 64, [3000 + 41 * i for i in range(9)], [15 + 3 * i for i in range(9)], True),
+    (12, 4, 64, 16, [10 * i for i in range(150)], [7 + i % 30 for i in range(150)], False),
+    (20, 5, 128, 64, [9000, 100, 5000, 1], [1, 1, 1, 1], False), (16, 4, 64, 16, [33 * i for i in range(200)], [1 + i % 3 for i in range(200)], True),
+    (64, 1, 128, 64, [1000], [130], False), (33, 1, 64, 64, [70, 500], [50, 3], True), (3, 1, 128, 16, [20000], [20], False),
+    (8, 1, 128, 64, [60000], [1], False)])
+def test_long_and_many(B, nh, nkv, hd, page, used, news, is_tree):
+    """Items cut between thread blocks, many short sequences, groups that do not divide a tile."""
+    c = ref.make(71, used, news, nkv, hd, page)
+    par = torch.tensor([p for s, m in enumerate(news) for p in ref.tree(80 + s, m, m // 9)], dtype=torch.int32) if is_tree else None
+    q = fill_new(c, 72, news, par, nh)
+    off = ref.offsets(news)
+    g = on_gpu(B, c)
+    att = B.attention_cached(g, 0, q.cuda(), (off.cuda(), max(news)), nh, parent=None if par is None else par.cuda())
+    B.poll_status()
+    want, add, tol, mtol = dense(c, q, off, nh, par)
+    err = (att.double().reshape(want.shape) - want).abs() - tol
+    assert not att.isnan().any() and err.max() <= 0, float(err.max())
+    m0 = c["mass"][0].double().cuda()
+    bad = (g.mass[0].double() - m0 - add).abs() - (mtol + 2.0**-23 * (m0 + add))
+    assert bad.max() <= 0, float(bad.max())
