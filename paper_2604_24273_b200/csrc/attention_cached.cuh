@@ -409,37 +409,37 @@ __global__ void __launch_bounds__(128) attn_join_kernel(const __grid_constant__ 
 // A second pass over the keys: with the final maximum and sum of every row known, a CTA owns 64 slots of one kv head, forms
 // their scores with all rows of the sequence and adds up each slot's weights in registers; a slot belongs to one CTA, so
 // nothing is added atomically.
-constexpr int AM_THREADS = 128;
-constexpr int AM_KEYS = 64;
-constexpr int AM_ROWS = 64;  // rows per step
+constexpr int AS_THREADS = 128;
+constexpr int AS_KEYS = 64;
+constexpr int AS_ROWS = 64;  // rows per step
 
 template <int HD>
-constexpr uint32_t am_smem_bytes() {
-  return AM_KEYS * HD * 2 + 2 * AM_ROWS * (HD * 2 + 4);
+constexpr uint32_t as_smem_bytes() {
+  return AS_KEYS * HD * 2 + 2 * AS_ROWS * (HD * 2 + 4);
 }
 
 template <int HD>
-__global__ void __launch_bounds__(AM_THREADS) attn_mass_kernel(const __grid_constant__ AcArgs a) {
+__global__ void __launch_bounds__(AS_THREADS) attn_mass_few_kernel(const __grid_constant__ AcArgs a) {
   constexpr int KS = HD / 16, CH = HD / 8;
-  constexpr uint32_t K_BYTES = AM_KEYS * HD * 2, Q_BYTES = AM_ROWS * HD * 2;
+  constexpr uint32_t K_BYTES = AS_KEYS * HD * 2, Q_BYTES = AS_ROWS * HD * 2;
   extern __shared__ __align__(128) unsigned char am_smem[];
   pdl_enter();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3, lm = lane >> 3, lr = lane & 7;
-  const int tiles = (((a.c.max_pages << a.c.page_shift) + AM_KEYS - 1) / AM_KEYS);
+  const int tiles = (((a.c.max_pages << a.c.page_shift) + AS_KEYS - 1) / AS_KEYS);
   int idx = blockIdx.x;
   const int kt = idx % tiles;
   idx /= tiles;
   const int head = idx % a.c.n_kv, s = idx / a.c.n_kv;
   KvSeq q;
   if (!kv_seq(a.c, a.b, s, q)) return;
-  const int slot0 = kt * AM_KEYS, end = q.used + q.m;
+  const int slot0 = kt * AS_KEYS, end = q.used + q.m;
   if (slot0 >= end || q.m == 0) return;
-  float* lse_s = reinterpret_cast<float*>(am_smem + K_BYTES + 2 * Q_BYTES);  // [2][AM_ROWS]
+  float* lse_s = reinterpret_cast<float*>(am_smem + K_BYTES + 2 * Q_BYTES);  // [2][AS_ROWS]
   if (a.tree_ok && !a.tree_ok[s]) return;
   const uint32_t* anc = a.b.parent ? a.anc + static_cast<long long>(q.t0) * AC_TREE_WORDS : nullptr;
   const uint32_t k_addr = ptx::smem_u32(am_smem), q_addr = k_addr + K_BYTES;
   const int slot_mask = (1 << a.c.page_shift) - 1;
-  for (int i = threadIdx.x; i < AM_KEYS * CH; i += AM_THREADS) {
+  for (int i = threadIdx.x; i < AS_KEYS * CH; i += AS_THREADS) {
     const int r = i / CH, ch = i % CH, slot = slot0 + r;
     int page = -1;
     if (slot < end) page = kv_page(a.c, s, slot);
@@ -448,18 +448,18 @@ __global__ void __launch_bounds__(AM_THREADS) attn_mass_kernel(const __grid_cons
   }
   const int rows = q.m * a.rep;
   // rows below the first that can see this tile's slots
-  const int first = (!anc && slot0 > q.used ? min(q.m, slot0 - q.used) * a.rep : 0) / AM_ROWS * AM_ROWS;
+  const int first = (!anc && slot0 > q.used ? min(q.m, slot0 - q.used) * a.rep : 0) / AS_ROWS * AS_ROWS;
   auto load_q = [&](int x0, int buf) {
-    for (int i = threadIdx.x; i < AM_ROWS * CH; i += AM_THREADS) {
+    for (int i = threadIdx.x; i < AS_ROWS * CH; i += AS_THREADS) {
       const int r = i / CH, ch = i % CH, x = x0 + r;
       const int tk = x / a.rep;
       const long long row = static_cast<long long>(q.t0 + tk) * a.n_heads + head * a.rep + (x - tk * a.rep);
       cp_async16(q_addr + buf * Q_BYTES + r * (HD * 2) + ((ch ^ (r & 7)) << 4), a.q + (x < rows ? row * HD + ch * 8 : 0),
                  x < rows ? 16u : 0u);
     }
-    if (threadIdx.x < AM_ROWS) {
+    if (threadIdx.x < AS_ROWS) {
       const int x = x0 + threadIdx.x, tk = x / a.rep;
-      lse_s[buf * AM_ROWS + threadIdx.x] =
+      lse_s[buf * AS_ROWS + threadIdx.x] =
           x < rows ? a.lse[static_cast<long long>(q.t0 + tk) * a.n_heads + head * a.rep + (x - tk * a.rep)] : INFINITY;
     }
   };
@@ -468,12 +468,12 @@ __global__ void __launch_bounds__(AM_THREADS) attn_mass_kernel(const __grid_cons
   uint32_t ka[KS][4];
   float got[2] = {0.0f, 0.0f};  // slots g and g + 8 of the warp's 16
   const int key_lo = slot0 + warp * 16 + g;
-  const bool masked = slot0 + AM_KEYS > q.used;
+  const bool masked = slot0 + AS_KEYS > q.used;
   int buf = 0;
-  for (int x0 = first; x0 < rows; x0 += AM_ROWS, buf ^= 1) {
+  for (int x0 = first; x0 < rows; x0 += AS_ROWS, buf ^= 1) {
     cp_async_wait<0>();
     __syncthreads();
-    if (x0 + AM_ROWS < rows) load_q(x0 + AM_ROWS, buf ^ 1);
+    if (x0 + AS_ROWS < rows) load_q(x0 + AS_ROWS, buf ^ 1);
     cp_async_commit();
     if (x0 == first) {
 #pragma unroll
@@ -482,7 +482,7 @@ __global__ void __launch_bounds__(AM_THREADS) attn_mass_kernel(const __grid_cons
         ldmatrix_x4(k_addr + key * (HD * 2) + ((ch ^ (key & 7)) << 4), ka[ks]);
       }
     }
-    for (int n0 = 0; n0 < AM_ROWS; n0 += 16) {
+    for (int n0 = 0; n0 < AS_ROWS; n0 += 16) {
       if (x0 + n0 >= rows) break;
       float c[2][4];
 #pragma unroll
@@ -502,7 +502,7 @@ __global__ void __launch_bounds__(AM_THREADS) attn_mass_kernel(const __grid_cons
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           const int r = n0 + 8 * nt + 2 * t + (e & 1), x = x0 + r;
-          const float lse = lse_s[buf * AM_ROWS + r];
+          const float lse = lse_s[buf * AS_ROWS + r];
           bool see = lse != INFINITY;
           if (masked) {
             const int slot = key_lo + 8 * (e >> 1);

@@ -586,6 +586,338 @@ __global__ void __launch_bounds__(256) attn_tiles_join_kernel(const __grid_const
   if (d0 == 0) a.lse[row] = none ? INFINITY : m_all + __log2f(l);
 }
 
+// ---- weight received by every slot ---------------------------------------------------------------------------------
+// A second pass over the keys: the final maximum and sum of every row are known, so p = 2^(t - lse) directly.  The scores
+// are formed transposed, S^T = K Q^T: a thread then owns one slot and adds up its weights over the rows in registers, in a
+// fixed order and without a word to other threads.  An item is 256 slots (two tiles) of one kv head, a unit is one row tile;
+// an item that is cut between CTAs leaves partial sums that attn_mass_join_kernel adds in order.
+//   warp 0 producer (keys of an item, double-buffered; queries through a ring of two), warp 1 MMA (two accumulators per key
+//   tile), warp 2 row statistics, warps 4-7 and 8-11 the sums of key tile 0 and 1.
+// Bound: 1024 cycles of exponentials per 128 x 128 tile (the products take 512) for long chunks; reading for short ones.
+constexpr int AM_THREADS = 384;
+constexpr int AM_KEYS = 256;
+enum { AM_WAIT_LOAD = 141, AM_WAIT_MMA = 142, AM_WAIT_LSE = 143, AM_WAIT_SUM = 144 };
+
+template <int HD>
+struct AmSmem {
+  static constexpr uint32_t TILE = 128 * HD * 2, HALF = 128 * 128;
+  static constexpr uint32_t K = 0, Q = 4 * TILE, LSE = Q + 2 * TILE;  // K [2][2 tiles], Q [2], LSE [4][128]
+  static constexpr uint32_t LIVE = LSE + 4 * 512, COL = LIVE + 64;    // LIVE [4][4] bits, COL [128] token of a column
+  static constexpr uint32_t BAR = COL + 128;
+  static constexpr uint32_t K_FULL = BAR, K_EMPTY = K_FULL + 16, Q_FULL = K_EMPTY + 16, Q_EMPTY = Q_FULL + 16, S_FULL = Q_EMPTY + 16,
+                            S_EMPTY = S_FULL + 32, L_FULL = S_EMPTY + 32, L_EMPTY = L_FULL + 32, DRAIN = L_EMPTY + 32;
+  static constexpr uint32_t MISC = DRAIN + 8, RUN = MISC + 8, PART = RUN + 32;
+  static constexpr uint32_t BYTES = PART + 8 * (AM_THREADS / 32 + 1) + 1024;
+  static constexpr uint32_t LAUNCH = BYTES > 120 * 1024 ? BYTES : 120 * 1024;  // one CTA per SM: it takes all of tensor memory
+};
+
+struct AmArgs {
+  AcArgs a;
+  int tok_tile;
+  int nx;       // items of the longest sequence that the page table can hold
+  float* part;  // [CTAs][2][256] sums of cut items
+};
+
+// Row tiles that see some slot of item (s, x), from `first` on.
+__device__ __forceinline__ int am_units(const AmArgs& t, int s, int x, KvSeq& q, int& first) {
+  first = 0;
+  if (!kv_seq(t.a.c, t.a.b, s, q) || (t.a.tree_ok && !t.a.tree_ok[s])) return 0;
+  if (x * AM_KEYS >= q.used + q.m) return 0;
+  if (!t.a.b.parent) first = max(0, x * AM_KEYS - q.used) / t.tok_tile;
+  return (q.m + t.tok_tile - 1) / t.tok_tile - first;
+}
+
+template <int HD>
+__global__ void __launch_bounds__(AM_THREADS, 1)
+attn_mass_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_constant__ CUtensorMap tmap_k, const __grid_constant__ AmArgs t) {
+  using M = AmSmem<HD>;
+  constexpr int NH = HD / 64;
+  extern __shared__ unsigned char at_smem_raw[];
+  const uint32_t raw = ptx::smem_u32(at_smem_raw), base = (raw + 1023u) & ~1023u;
+  unsigned char* sm = at_smem_raw + (base - raw);
+  volatile uint32_t* misc = reinterpret_cast<volatile uint32_t*>(sm + M::MISC);
+  volatile uint32_t* failed = misc + 1;
+  const uint32_t failed_addr = base + M::MISC + 4;
+  const AcArgs& a = t.a;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  auto wait = [&](uint32_t bar, uint32_t parity) {
+    return __any_sync(0xffffffffu, ptx::mbar_wait_abortable(base + bar, parity, failed_addr));
+  };
+  auto give_up = [&](int stage) {
+    report_timeout(stage);
+    *failed = 1u;
+  };
+  if (threadIdx.x == 0) {
+    *failed = 0u;
+    for (int i = 0; i < 2; ++i) {
+      ptx::mbar_init(base + M::K_FULL + 8 * i, 1);
+      ptx::mbar_init(base + M::K_EMPTY + 8 * i, 1);
+      ptx::mbar_init(base + M::Q_FULL + 8 * i, 1);
+      ptx::mbar_init(base + M::Q_EMPTY + 8 * i, 1);
+    }
+    for (int i = 0; i < 4; ++i) {
+      ptx::mbar_init(base + M::S_FULL + 8 * i, 1);
+      ptx::mbar_init(base + M::S_EMPTY + 8 * i, 4);
+      ptx::mbar_init(base + M::L_FULL + 8 * i, 1);
+      ptx::mbar_init(base + M::L_EMPTY + 8 * i, 8);
+    }
+    ptx::mbar_init(base + M::DRAIN, 1);
+    ptx::mbar_init_fence();
+    ptx::tma_prefetch_desc(&tmap_q);
+    ptx::tma_prefetch_desc(&tmap_k);
+  }
+  if (warp == 1) {
+    ptx::tmem_alloc(base + M::MISC, 512);
+    ptx::tmem_relinquish();
+  }
+  if (threadIdx.x >= 64 && threadIdx.x < 192) sm[M::COL + threadIdx.x - 64] = static_cast<unsigned char>((threadIdx.x - 64) / a.rep);
+  ptx::tc_fence_before_sync();
+  __syncthreads();
+  ptx::tc_fence_after_sync();
+  const uint32_t tmem = misc[0];
+  pdl_enter();
+  AtCut* cuts = a.cuts + 2 * blockIdx.x;
+  if (threadIdx.x < 2) cuts[threadIdx.x].s = -1;
+  KvSeq q;
+  int first;
+  auto cost = [&](int s, int x) { return am_units(t, s, x, q, first); };
+  AcRun* run = reinterpret_cast<AcRun*>(sm + M::RUN);
+  ac_run_start(cost, a.c.n_seq, t.nx, a.c.n_kv, AM_THREADS, reinterpret_cast<long long*>(sm + M::PART), run);
+  AcWalk w(*run, t.nx, a.c.n_kv, a.c.n_seq);
+  const int tok_tile = t.tok_tile;
+  auto key_tiles = [&]() { return w.x * AM_KEYS + 128 < q.used + q.m ? 2 : 1; };
+  auto rows_of = [&](int u) { return min(tok_tile, q.m - (first + u) * tok_tile) * a.rep; };
+  bool more = w.start(cost), ok = true;
+  if (warp == 0) {
+    // ------------------------------------------------------------------ producer
+    uint32_t kn = 0, qn = 0;
+    const int page = 1 << a.c.page_shift, pieces = 128 >> a.c.page_shift;
+    const int tile = lane / (pieces * NH), piece = lane % (pieces * NH) / NH, half = lane % NH;
+    const int none = a.c.n_pages * a.c.n_kv * page;  // a row behind the pool: such a copy fills with zeros
+    while (ok && more) {
+      const int na = key_tiles(), end = q.used + q.m;
+      int row = none;
+      if (tile < na) {
+        const int slot = w.x * AM_KEYS + tile * 128 + piece * page;
+        const int p = slot < end ? kv_page(a.c, w.s, slot) : -1;
+        if (p >= 0) row = (p * a.c.n_kv + w.h) * page;
+      }
+      const uint32_t kb = kn & 1;
+      if (!(ok = wait(M::K_EMPTY + 8 * kb, ((kn >> 1) & 1) ^ 1))) break;
+      if (lane == 0) ptx::mbar_arrive_expect_tx(base + M::K_FULL + 8 * kb, na * M::TILE);
+      __syncwarp();
+      if (tile < na)
+        ptx::tma_load_2d(base + M::K + (2 * kb + tile) * M::TILE + half * M::HALF + piece * page * 128, &tmap_k, 64 * half, row,
+                         base + M::K_FULL + 8 * kb);
+      ++kn;
+      for (int u = w.u0; u < w.u1; ++u, ++qn) {
+        const uint32_t qb = qn & 1;
+        if (!(ok = wait(M::Q_EMPTY + 8 * qb, ((qn >> 1) & 1) ^ 1))) break;
+        if (lane == 0) ptx::mbar_arrive_expect_tx(base + M::Q_FULL + 8 * qb, NH * 128 * a.rep * tok_tile);
+        __syncwarp();
+        if (lane < NH)
+          ptx::tma_load_3d(base + M::Q + qb * M::TILE + lane * M::HALF, &tmap_q, 64 * lane, w.h * a.rep, q.t0 + (first + u) * tok_tile,
+                           base + M::Q_FULL + 8 * qb);
+      }
+      if (ok) more = w.next(cost);
+      __syncwarp();
+    }
+    if (!ok && lane == 0) give_up(AM_WAIT_LOAD);
+  } else if (warp == 1) {
+    // ------------------------------------------------------------------ MMA issuer
+    uint32_t kn = 0, qn = 0, un[2] = {0, 0};
+    while (ok && more) {
+      const int na = key_tiles();
+      const uint32_t kb = kn & 1;
+      if (!(ok = wait(M::K_FULL + 8 * kb, (kn >> 1) & 1))) break;
+      ++kn;
+      for (int u = w.u0; ok && u < w.u1; ++u, ++qn) {
+        const uint32_t qb = qn & 1;
+        if (!(ok = wait(M::Q_FULL + 8 * qb, (qn >> 1) & 1))) break;
+        const uint32_t idesc = ptx::idesc_bf16(128, (rows_of(u) + 15) & ~15, false);
+        for (int x = 0; x < na; ++x) {
+          const uint32_t b = un[x] & 1;
+          if (!(ok = wait(M::S_EMPTY + 8 * (2 * x + b), ((un[x] >> 1) & 1) ^ 1))) break;
+          ++un[x];
+          ptx::tc_fence_after_sync();
+          if (ptx::elect_one()) {
+            const uint64_t kd = ptx::smem_desc_sw128(base + M::K + (2 * kb + x) * M::TILE), qd = ptx::smem_desc_sw128(base + M::Q + qb * M::TILE);
+#pragma unroll
+            for (int k = 0; k < HD / 16; ++k) {
+              const uint32_t off = ((k / 4) * M::HALF + (k % 4) * 32) >> 4;
+              ptx::mma_bf16_ss(tmem + 256 * x + 128 * b, kd + off, qd + off, idesc, k != 0);
+            }
+            ptx::mma_commit(base + M::S_FULL + 8 * (2 * x + b));
+          }
+          __syncwarp();
+        }
+        if (!ok) break;
+        if (ptx::elect_one()) {
+          ptx::mma_commit(base + M::Q_EMPTY + 8 * qb);
+          if (u + 1 == w.u1) ptx::mma_commit(base + M::K_EMPTY + 8 * kb);
+        }
+        __syncwarp();
+      }
+      if (ok) more = w.next(cost);
+      __syncwarp();
+    }
+    if (!ok && lane == 0) give_up(AM_WAIT_MMA);
+  } else if (warp == 2) {
+    // ------------------------------------------------------------------ row statistics
+    uint32_t n = 0;
+    while (ok && more) {
+      for (int u = w.u0; u < w.u1; ++u, ++n) {
+        const uint32_t b = n & 3;
+        const int rows = rows_of(u);
+        float v[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int c = lane + 32 * i, tk = c / a.rep;
+          v[i] = c < rows ? a.lse[static_cast<long long>(q.t0 + (first + u) * tok_tile + tk) * a.n_heads + w.h * a.rep + c - tk * a.rep] : INFINITY;
+        }
+        if (!(ok = wait(M::L_EMPTY + 8 * b, ((n >> 2) & 1) ^ 1))) break;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          reinterpret_cast<float*>(sm + M::LSE)[128 * b + lane + 32 * i] = v[i];
+          const uint32_t live = __ballot_sync(0xffffffffu, v[i] != INFINITY);
+          if (lane == 0) reinterpret_cast<uint32_t*>(sm + M::LIVE)[4 * b + i] = live;
+        }
+        __syncwarp();
+        if (lane == 0) ptx::mbar_arrive(base + M::L_FULL + 8 * b);
+      }
+      if (ok) more = w.next(cost);
+      __syncwarp();
+    }
+    if (!ok && lane == 0) give_up(AM_WAIT_LSE);
+  } else if (warp >= 4) {
+    // ------------------------------------------------------------------ sums, one slot per thread
+    const int x = (warp - 4) >> 2;
+    const uint32_t lane_base = static_cast<uint32_t>((warp & 3) * 32) << 16;
+    const int r = (warp & 3) * 32 + lane;
+    uint32_t un = 0, n = 0;
+    while (ok && more) {
+      const bool active = x < key_tiles();
+      const int slot = w.x * AM_KEYS + 128 * x + r, j = slot - q.used;
+      float got[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+      for (int u = w.u0; u < w.u1; ++u, ++n) {
+        const uint32_t b = n & 3;
+        if (!(ok = wait(M::L_FULL + 8 * b, (n >> 2) & 1))) break;
+        if (active) {
+          const uint32_t sb = un & 1;
+          if (!(ok = wait(M::S_FULL + 8 * (2 * x + sb), (un >> 1) & 1))) break;
+          ++un;
+          ptx::tc_fence_after_sync();
+          uint32_t s[4][32];
+          const int rows = rows_of(u);
+#pragma unroll
+          for (int c = 0; c < 4; ++c)
+            if (32 * c < rows) ptx::tmem_ld_32x32b_x32(tmem + 256 * x + 128 * sb + 32 * c + lane_base, s[c]);
+          ptx::tmem_ld_wait();
+          ptx::tc_fence_before_sync();
+          __syncwarp();
+          if (lane == 0) ptx::mbar_arrive(base + M::S_EMPTY + 8 * (2 * x + sb));
+          const int tok0 = (first + u) * tok_tile, last_slot = w.x * AM_KEYS + 128 * x + 127;
+          const bool masked = last_slot >= q.used + (a.b.parent ? 0 : tok0 + 1);
+#pragma unroll
+          for (int c = 0; c < 4; ++c) {
+            if (32 * c >= rows) break;
+            uint32_t see = ptx::lds32(base + M::LIVE + 16 * b + 4 * c);
+            const uint32_t lse = base + M::LSE + 512 * b + 128 * c;
+            if (masked) {
+              if (j >= 0)
+                for (int i = 0; i < 32; ++i) {
+                  const int tok = tok0 + sm[M::COL + 32 * c + i];
+                  bool can = a.b.parent ? false : j <= tok;
+                  if (a.b.parent && ((see >> i) & 1u) && j < q.m)
+                    can = (a.anc[static_cast<long long>(q.t0 + tok) * AC_TREE_WORDS + (j >> 5)] >> (j & 31)) & 1u;
+                  if (!can) see &= ~(1u << i);
+                }
+            }
+            if (__all_sync(0xffffffffu, see == 0xffffffffu)) {
+#pragma unroll
+              for (int i = 0; i < 32; i += 4) {
+                const uint4 e = ptx::lds128(lse + 4 * i);
+                got[0] += ac_exp2(fmaf(__uint_as_float(s[c][i]), a.scale2, -__uint_as_float(e.x)));
+                got[1] += ac_exp2(fmaf(__uint_as_float(s[c][i + 1]), a.scale2, -__uint_as_float(e.y)));
+                got[2] += ac_exp2(fmaf(__uint_as_float(s[c][i + 2]), a.scale2, -__uint_as_float(e.z)));
+                got[3] += ac_exp2(fmaf(__uint_as_float(s[c][i + 3]), a.scale2, -__uint_as_float(e.w)));
+              }
+            } else {
+#pragma unroll
+              for (int i = 0; i < 32; i += 4) {
+                const uint4 e = ptx::lds128(lse + 4 * i);
+                const uint32_t ev[4] = {e.x, e.y, e.z, e.w};
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+                  if ((see >> (i + k)) & 1u) got[k] += ac_exp2(fmaf(__uint_as_float(s[c][i + k]), a.scale2, -__uint_as_float(ev[k])));
+              }
+            }
+          }
+        }
+        __syncwarp();
+        if (lane == 0) ptx::mbar_arrive(base + M::L_EMPTY + 8 * b);
+      }
+      if (!ok) break;
+      const float sum = (got[0] + got[1]) + (got[2] + got[3]);
+      if (w.u0 == 0 && w.u1 == w.units) {
+        if (slot < q.used + q.m) {
+          const int page = kv_page(a.c, w.s, slot);
+          if (page >= 0) a.c.mass[kv_row(a.c, 0, page, w.h) + (slot & ((1 << a.c.page_shift) - 1))] += sum;
+        }
+      } else {
+        const int cut = w.u0 == 0 ? 1 : 0;
+        t.part[(2 * static_cast<long long>(blockIdx.x) + cut) * AM_KEYS + 128 * x + r] = sum;
+        if (threadIdx.x == 128) cuts[cut] = AtCut{w.s, w.x, w.h, w.u1 == w.units};
+      }
+      more = w.next(cost);
+      __syncwarp();
+    }
+    if (!ok && lane == 0) give_up(AM_WAIT_SUM);
+  }
+
+  // ---- teardown: every role leaves through here, also after a timeout ----
+  __syncwarp();
+  ptx::tc_fence_before_sync();
+  __syncthreads();
+  if (*failed) {
+    // Failure path only: copies and MMAs that nobody waited for may still be in flight.
+    if (warp == 1) {
+      if (ptx::elect_one()) ptx::mma_commit(base + M::DRAIN);
+      __syncwarp();
+      ptx::mbar_wait(base + M::DRAIN, 0, 2000000LL);
+    }
+    const long long t0 = clock64();
+    while (clock64() - t0 < 2000000LL) {}
+    __syncthreads();
+  }
+  if (warp == 1) {
+    ptx::tc_fence_after_sync();
+    ptx::tmem_dealloc(tmem, 512);
+  }
+}
+
+// Adds the parts of the items that were cut, from the CTA in which an item begins onwards.
+__global__ void __launch_bounds__(AM_KEYS) attn_mass_join_kernel(const __grid_constant__ AmArgs t, int n_ctas) {
+  pdl_enter();
+  const AcArgs& a = t.a;
+  const int c0 = blockIdx.x;
+  const AtCut head = a.cuts[2 * c0 + 1];
+  if (head.s < 0) return;
+  KvSeq q;
+  if (!kv_seq(a.c, a.b, head.s, q)) return;
+  const int slot = head.x * AM_KEYS + threadIdx.x;
+  if (slot >= q.used + q.m) return;
+  float sum = t.part[(2 * static_cast<long long>(c0) + 1) * AM_KEYS + threadIdx.x];
+  for (int c = c0 + 1; c < n_ctas; ++c) {
+    const AtCut cut = a.cuts[2 * c];
+    if (cut.s < 0) continue;  // a CTA whose run is empty
+    sum += t.part[2 * static_cast<long long>(c) * AM_KEYS + threadIdx.x];
+    if (cut.ends) break;
+  }
+  const int page = kv_page(a.c, head.s, slot);
+  if (page >= 0) a.c.mass[kv_row(a.c, 0, page, head.h) + (slot & ((1 << a.c.page_shift) - 1))] += sum;
+}
+
 // ---- host --------------------------------------------------------------------------------------------------------------
 constexpr int AC_FEW_ROWS = AR_ROWS;  // at most so many rows per sequence and kv head take the few-rows kernel
 
@@ -593,12 +925,12 @@ struct AcPlan {
   bool few;                                // few rows: attn_rows_kernel; else tiles
   int row_tiles, splits, split_keys;       // few rows
   int tok_tile, nx, rows_cap, ctas;        // tiles
-  size_t lse_bytes, ml_bytes, o_bytes, cut_bytes, anc_bytes, ok_bytes;
-  size_t bytes() const { return lse_bytes + ml_bytes + o_bytes + cut_bytes + anc_bytes + ok_bytes; }
+  size_t lse_bytes, ml_bytes, o_bytes, cut_bytes, sum_bytes, anc_bytes, ok_bytes;
+  size_t bytes() const { return lse_bytes + ml_bytes + o_bytes + cut_bytes + sum_bytes + anc_bytes + ok_bytes; }
   // Does every grid and every coordinate of the call fit?
   bool launchable(const KvView& c) const {
     const long long heads = static_cast<long long>(c.n_seq) * c.n_kv;
-    const long long key_tiles = ((c.max_pages << c.page_shift) + AM_KEYS - 1) / AM_KEYS;
+    const long long key_tiles = ((c.max_pages << c.page_shift) + AS_KEYS - 1) / AS_KEYS;
     return heads * row_tiles <= INT_MAX / splits && heads <= INT_MAX / key_tiles &&
            (static_cast<long long>(c.n_pages) * c.n_kv + 1) << c.page_shift <= INT_MAX;
   }
@@ -635,6 +967,7 @@ inline AcPlan ac_plan(const KvView& c, int T, int max_new, int n_heads) {
     p.ml_bytes = ac_up(static_cast<size_t>(2 * p.ctas) * p.rows_cap * 8);
     p.o_bytes = ac_up(static_cast<size_t>(2 * p.ctas) * p.rows_cap * c.hd * 4);
     p.cut_bytes = ac_up(static_cast<size_t>(2 * p.ctas) * sizeof(AtCut));
+    p.sum_bytes = ac_up(static_cast<size_t>(2 * p.ctas) * AM_KEYS * 4);
   }
   return p;
 }
@@ -663,7 +996,7 @@ inline bitrl_status ac_tensor_map(CUtensorMap* m, const void* p, int dims, const
 }
 
 template <int HD>
-bitrl_status launch_attention_cached_hd(const AcArgs& a, const AcPlan& p, bool mass, cudaStream_t st) {
+bitrl_status launch_attention_cached_hd(const AcArgs& a, const AcPlan& p, bool mass, float* sums, cudaStream_t st) {
   bitrl_status s;
   if (p.few) {
     static bool done[64] = {false};
@@ -674,6 +1007,13 @@ bitrl_status launch_attention_cached_hd(const AcArgs& a, const AcPlan& p, bool m
     if (p.splits > 1) {
       const unsigned per_seq = static_cast<unsigned>((static_cast<long long>(a.b.max_new) * a.n_heads + 3) / 4);
       BITRL_CUDA(launch_pdl(attn_join_kernel<HD>, dim3(per_seq * a.c.n_seq), dim3(128), 0, st, a));
+      count_launch(1);
+    }
+    if (mass) {
+      static bool mass_done[64] = {false};
+      if ((s = ac_smem(attn_mass_few_kernel<HD>, as_smem_bytes<HD>(), mass_done)) != BITRL_OK) return s;
+      const unsigned tiles = static_cast<unsigned>(((a.c.max_pages << a.c.page_shift) + AS_KEYS - 1) / AS_KEYS);
+      BITRL_CUDA(launch_pdl(attn_mass_few_kernel<HD>, dim3(tiles * a.c.n_kv * a.c.n_seq), dim3(AS_THREADS), as_smem_bytes<HD>(), st, a));
       count_launch(1);
     }
   } else {
@@ -693,13 +1033,14 @@ bitrl_status launch_attention_cached_hd(const AcArgs& a, const AcPlan& p, bool m
     BITRL_CUDA(launch_pdl(attn_tiles_kernel<HD>, dim3(p.ctas), dim3(AT_THREADS), AtSmem<HD>::LAUNCH, st, mq, mk, mv, t));
     BITRL_CUDA(launch_pdl(attn_tiles_join_kernel<HD>, dim3(p.ctas, (p.rows_cap + 31) / 32), dim3(256), 0, st, t, p.ctas));
     count_launch(2);
-  }
-  if (mass) {
-    static bool done[64] = {false};
-    if ((s = ac_smem(attn_mass_kernel<HD>, am_smem_bytes<HD>(), done)) != BITRL_OK) return s;
-    const unsigned tiles = static_cast<unsigned>(((a.c.max_pages << a.c.page_shift) + AM_KEYS - 1) / AM_KEYS);
-    BITRL_CUDA(launch_pdl(attn_mass_kernel<HD>, dim3(tiles * a.c.n_kv * a.c.n_seq), dim3(AM_THREADS), am_smem_bytes<HD>(), st, a));
-    count_launch(1);
+    if (mass) {
+      static bool mass_done[64] = {false};
+      if ((s = ac_smem(attn_mass_kernel<HD>, AmSmem<HD>::LAUNCH, mass_done)) != BITRL_OK) return s;
+      const AmArgs m{a, p.tok_tile, ((a.c.max_pages << a.c.page_shift) + AM_KEYS - 1) / AM_KEYS, sums};
+      BITRL_CUDA(launch_pdl(attn_mass_kernel<HD>, dim3(p.ctas), dim3(AM_THREADS), AmSmem<HD>::LAUNCH, st, mq, mk, m));
+      BITRL_CUDA(launch_pdl(attn_mass_join_kernel, dim3(p.ctas), dim3(AM_KEYS), 0, st, m, p.ctas));
+      count_launch(2);
+    }
   }
   return BITRL_OK;
 }
@@ -728,6 +1069,7 @@ bitrl_status launch_attention_cached(const KvView& c, const KvBatch& b, const vo
   a.part_ml = reinterpret_cast<float2*>(take(p.ml_bytes));
   a.part_o = reinterpret_cast<float*>(take(p.o_bytes));
   a.cuts = reinterpret_cast<AtCut*>(take(p.cut_bytes));
+  float* sums = reinterpret_cast<float*>(take(p.sum_bytes));
   uint32_t* anc = reinterpret_cast<uint32_t*>(take(p.anc_bytes));
   int* ok = reinterpret_cast<int*>(take(p.ok_bytes));
   a.anc = b.parent ? anc : nullptr;
@@ -736,7 +1078,7 @@ bitrl_status launch_attention_cached(const KvView& c, const KvBatch& b, const vo
     BITRL_CUDA(launch_pdl(attn_tree_kernel, dim3(c.n_seq), dim3(BITRL_TREE_MAX_TOKENS), 0, st, c, b, anc, ok));
     count_launch(1);
   }
-  return c.hd == 128 ? launch_attention_cached_hd<128>(a, p, mass, st) : launch_attention_cached_hd<64>(a, p, mass, st);
+  return c.hd == 128 ? launch_attention_cached_hd<128>(a, p, mass, sums, st) : launch_attention_cached_hd<64>(a, p, mass, sums, st);
 }
 
 }  // namespace bitrl
