@@ -33,7 +33,8 @@ struct AcArgs {
   float* part_o;           // [splits][T * n_heads][HD] unnormalised partial results (splits > 1)
   float2* part_ml;         // [splits][T * n_heads]: running maximum and sum
   float* lse;              // [T * n_heads]: maximum + log2(sum); +inf where a row sees nothing
-  const uint32_t* anc;     // trees: [T][AC_TREE_WORDS]
+  const uint32_t* anc;     // trees: [T][AC_TREE_WORDS], the tokens that a token sees
+  const uint32_t* desc;    // trees: [T][AC_TREE_WORDS], the tokens that see a token
   const int* tree_ok;      // trees: [n_seq], else nullptr
   AtCut* cuts;             // tiles: [CTAs][2]
 };
@@ -64,25 +65,37 @@ __device__ __forceinline__ void cp_async_wait() {
 }
 
 // Ancestors of every new token as bits, anc[row][AC_TREE_WORDS]: bit j is set when token j of the sequence is the token
-// itself or above it; padding has no bits.  ok[s]: the sequence's tree is one.  One CTA per sequence.
-__global__ void __launch_bounds__(BITRL_TREE_MAX_TOKENS) attn_tree_kernel(const KvView c, const KvBatch b, uint32_t* anc, int* ok) {
+// itself or above it; padding has no bits.  desc is the transpose.  ok[s]: the sequence's tree is one.  One CTA per sequence.
+__global__ void __launch_bounds__(BITRL_TREE_MAX_TOKENS)
+attn_tree_kernel(const KvView c, const KvBatch b, uint32_t* anc, uint32_t* desc, int* ok) {
   __shared__ int par[BITRL_TREE_MAX_TOKENS];
+  __shared__ uint32_t below[BITRL_TREE_MAX_TOKENS][AC_TREE_WORDS + 1];
   pdl_enter();
   const int s = blockIdx.x, i = threadIdx.x;
   KvSeq q;
   const bool good = kv_seq(c, b, s, q) && kv_load_tree(b, q, par, BITRL_TREE_MAX_TOKENS);
   if (i == 0) ok[s] = good;
-  if (!good || i >= q.m) return;
+  if (!good) return;
   uint32_t w[AC_TREE_WORDS];
 #pragma unroll
-  for (int k = 0; k < AC_TREE_WORDS; ++k) w[k] = 0u;
-  for (int j = par[i] == BITRL_PARENT_PAD ? -1 : i; j >= 0; j = par[j]) {
+  for (int k = 0; k < AC_TREE_WORDS; ++k) w[k] = below[i][k] = 0u;
+  __syncthreads();
+  if (i < q.m)
+    for (int j = par[i] == BITRL_PARENT_PAD ? -1 : i; j >= 0; j = par[j]) {
 #pragma unroll
-    for (int k = 0; k < AC_TREE_WORDS; ++k) w[k] |= (j >> 5) == k ? 1u << (j & 31) : 0u;
-  }
-  uint4* out = reinterpret_cast<uint4*>(anc + (static_cast<long long>(q.t0) + i) * AC_TREE_WORDS);
+      for (int k = 0; k < AC_TREE_WORDS; ++k) w[k] |= (j >> 5) == k ? 1u << (j & 31) : 0u;
+      atomicOr(&below[j][i >> 5], 1u << (i & 31));
+    }
+  __syncthreads();
+  if (i >= q.m) return;
+  const long long at = (static_cast<long long>(q.t0) + i) * AC_TREE_WORDS;
+  uint4* out = reinterpret_cast<uint4*>(anc + at);
   out[0] = make_uint4(w[0], w[1], w[2], w[3]);
   out[1] = make_uint4(w[4], w[5], w[6], w[7]);
+  const uint32_t* d = below[i];
+  out = reinterpret_cast<uint4*>(desc + at);
+  out[0] = make_uint4(d[0], d[1], d[2], d[3]);
+  out[1] = make_uint4(d[4], d[5], d[6], d[7]);
 }
 // Does token `tok` see the slot of new token j (j >= 0)?
 __device__ __forceinline__ bool ac_sees_new(const uint32_t* anc, int tok, int j) {

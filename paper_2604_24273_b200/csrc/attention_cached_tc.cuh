@@ -216,6 +216,9 @@ attn_tiles_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
     return (u + 1) * AT_KEYS > q.used + (a.b.parent ? 0 : w.x * 2 * tok_tile + 1);
   };
   bool more = w.start(cost);
+  if (warp < 4) {
+  // 128 threads at 88 registers and 256 at 208: the launch's 384 at 168
+  ptx::regs_dec<88>();
   if (warp == 0) {
     // ------------------------------------------------------------------ producer
     uint32_t e = 0, qn = 0;  // tiles put into the ring; items
@@ -327,7 +330,7 @@ attn_tiles_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
       __syncwarp();
     }
     if (!ok && lane == 0) give_up(AT_WAIT_MMA);
-  } else if (warp < 4) {
+  } else {
     // ------------------------------------------------------------------ values of masked units
     uint32_t e = 1, item = 0;
     bool ok = true;
@@ -369,8 +372,10 @@ attn_tiles_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
       __syncwarp();
     }
     if (!ok && lane == 0) give_up(AT_WAIT_FIX);
+  }
   } else {
     // ------------------------------------------------------------------ softmax, one row per thread
+    ptx::regs_inc<208>();
     const int x = (warp - 4) >> 2;  // row tile
     const uint32_t lane_base = static_cast<uint32_t>((warp & 3) * 32) << 16;
     const int r = (warp & 3) * 32 + lane, r_tok = r / a.rep, r_head = r - r_tok * a.rep;
@@ -402,7 +407,8 @@ attn_tiles_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
 #pragma unroll
           for (int c = 0; c < 4; ++c)
 #pragma unroll
-            for (int i = 0; i < 32; ++i) mx[i & 3] = fmaxf(mx[i & 3], __uint_as_float(s[c][i]));
+            for (int i = 0; i < 32; i += 2)
+              mx[(i >> 1) & 3] = fmaxf(mx[(i >> 1) & 3], fmaxf(__uint_as_float(s[c][i]), __uint_as_float(s[c][i + 1])));
           const float m2 = __fmul_rn(fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])), a.scale2);
           if (u == w.u0) {
             m_ref = m2;
@@ -422,22 +428,29 @@ attn_tiles_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
             }
           }
           const float sub = m_ref == -INFINITY ? 0.0f : -m_ref;
-          float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+          const uint64_t scale_x2 = ptx::pack_f32x2(__float_as_uint(a.scale2), __float_as_uint(a.scale2));
+          const uint64_t sub_x2 = ptx::pack_f32x2(__float_as_uint(sub), __float_as_uint(sub));
+          uint64_t sum[2] = {0ull, 0ull};
 #pragma unroll
           for (int c = 0; c < 4; c += 2) {
             uint32_t p[32];
 #pragma unroll
             for (int i = 0; i < 32; ++i) {
               const int cc = c + (i >> 4), j = 2 * (i & 15);
-              const float p0 = ac_exp2(fmaf(__uint_as_float(s[cc][j]), a.scale2, sub));
-              const float p1 = ac_exp2(fmaf(__uint_as_float(s[cc][j + 1]), a.scale2, sub));
-              sum[i & 1] += p0;
-              sum[2 + (i & 1)] += p1;
+              float p0, p1;
+              ptx::unpack_f32x2(ptx::fma_f32x2(ptx::pack_f32x2(s[cc][j], s[cc][j + 1]), scale_x2, sub_x2), p0, p1);
+              p0 = ac_exp2(p0);
+              p1 = ac_exp2(p1);
+              sum[i & 1] = ptx::add_f32x2(sum[i & 1], ptx::pack_f32x2(__float_as_uint(p0), __float_as_uint(p1)));
               p[i] = pack_bf16x2(p0, p1);
             }
             ptx::tmem_st_32x32b_x32(s_addr + 16 * c, p);
           }
-          l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+          {
+            float l0, l1;
+            ptx::unpack_f32x2(ptx::add_f32x2(sum[0], sum[1]), l0, l1);
+            l += l0 + l1;
+          }
           ptx::tmem_st_wait();
           ptx::tc_fence_before_sync();
           __syncwarp();
@@ -602,8 +615,7 @@ template <int HD>
 struct AmSmem {
   static constexpr uint32_t TILE = 128 * HD * 2, HALF = 128 * 128;
   static constexpr uint32_t K = 0, Q = 4 * TILE, LSE = Q + 2 * TILE;  // K [2][2 tiles], Q [2], LSE [4][128]
-  static constexpr uint32_t LIVE = LSE + 4 * 512, COL = LIVE + 64;    // LIVE [4][4] bits, COL [128] token of a column
-  static constexpr uint32_t BAR = COL + 128;
+  static constexpr uint32_t LIVE = LSE + 4 * 512, BAR = LIVE + 64;    // LIVE [4][4] bits: columns that hold a row
   static constexpr uint32_t K_FULL = BAR, K_EMPTY = K_FULL + 16, Q_FULL = K_EMPTY + 16, Q_EMPTY = Q_FULL + 16, S_FULL = Q_EMPTY + 16,
                             S_EMPTY = S_FULL + 32, L_FULL = S_EMPTY + 32, L_EMPTY = L_FULL + 32, DRAIN = L_EMPTY + 32;
   static constexpr uint32_t MISC = DRAIN + 8, RUN = MISC + 8, PART = RUN + 32;
@@ -670,7 +682,6 @@ attn_mass_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_consta
     ptx::tmem_alloc(base + M::MISC, 512);
     ptx::tmem_relinquish();
   }
-  if (threadIdx.x >= 64 && threadIdx.x < 192) sm[M::COL + threadIdx.x - 64] = static_cast<unsigned char>((threadIdx.x - 64) / a.rep);
   ptx::tc_fence_before_sync();
   __syncthreads();
   ptx::tc_fence_after_sync();
@@ -778,7 +789,7 @@ attn_mass_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_consta
         if (!(ok = wait(M::L_EMPTY + 8 * b, ((n >> 2) & 1) ^ 1))) break;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          reinterpret_cast<float*>(sm + M::LSE)[128 * b + lane + 32 * i] = v[i];
+          reinterpret_cast<float*>(sm + M::LSE)[128 * b + lane + 32 * i] = -v[i];  // what the sums add
           const uint32_t live = __ballot_sync(0xffffffffu, v[i] != INFINITY);
           if (lane == 0) reinterpret_cast<uint32_t*>(sm + M::LIVE)[4 * b + i] = live;
         }
@@ -794,6 +805,7 @@ attn_mass_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_consta
     const int x = (warp - 4) >> 2;
     const uint32_t lane_base = static_cast<uint32_t>((warp & 3) * 32) << 16;
     const int r = (warp & 3) * 32 + lane;
+    const uint64_t scale_x2 = ptx::pack_f32x2(__float_as_uint(a.scale2), __float_as_uint(a.scale2));
     uint32_t un = 0, n = 0;
     while (ok && more) {
       const bool active = x < key_tiles();
@@ -823,24 +835,33 @@ attn_mass_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_consta
             if (32 * c >= rows) break;
             uint32_t see = ptx::lds32(base + M::LIVE + 16 * b + 4 * c);
             const uint32_t lse = base + M::LSE + 512 * b + 128 * c;
-            if (masked) {
-              if (j >= 0)
-                for (int i = 0; i < 32; ++i) {
-                  const int tok = tok0 + sm[M::COL + 32 * c + i];
-                  bool can = a.b.parent ? false : j <= tok;
-                  if (a.b.parent && ((see >> i) & 1u) && j < q.m)
-                    can = (a.anc[static_cast<long long>(q.t0 + tok) * AC_TREE_WORDS + (j >> 5)] >> (j & 31)) & 1u;
-                  if (!can) see &= ~(1u << i);
+            if (masked && j >= 0) {
+              // columns of this chunk whose token sees the slot of new token j
+              uint32_t can = 0u;
+              if (!a.b.parent) {
+                const int from = (j - tok0) * a.rep - 32 * c;  // rows from token j on
+                can = from >= 32 ? 0u : from <= 0 ? 0xffffffffu : 0xffffffffu << from;
+              } else if (j < q.m) {
+                const uint32_t* who = a.desc + static_cast<long long>(q.t0 + j) * AC_TREE_WORDS;
+                for (int tk = 32 * c / a.rep; tk * a.rep < 32 * c + 32; ++tk) {
+                  const int tok = tok0 + tk, lo = tk * a.rep - 32 * c;
+                  if (tk >= tok_tile || tok >= q.m) break;
+                  if (((who[tok >> 5] >> (tok & 31)) & 1u) == 0) continue;
+                  const int from = max(lo, 0), n = min(lo + a.rep, 32) - from;
+                  can |= (n >= 32 ? 0xffffffffu : (1u << n) - 1u) << from;
                 }
+              }
+              see &= can;
             }
             if (__all_sync(0xffffffffu, see == 0xffffffffu)) {
 #pragma unroll
               for (int i = 0; i < 32; i += 4) {
                 const uint4 e = ptx::lds128(lse + 4 * i);
-                got[0] += ac_exp2(fmaf(__uint_as_float(s[c][i]), a.scale2, -__uint_as_float(e.x)));
-                got[1] += ac_exp2(fmaf(__uint_as_float(s[c][i + 1]), a.scale2, -__uint_as_float(e.y)));
-                got[2] += ac_exp2(fmaf(__uint_as_float(s[c][i + 2]), a.scale2, -__uint_as_float(e.z)));
-                got[3] += ac_exp2(fmaf(__uint_as_float(s[c][i + 3]), a.scale2, -__uint_as_float(e.w)));
+                float p[4];
+                ptx::unpack_f32x2(ptx::fma_f32x2(ptx::pack_f32x2(s[c][i], s[c][i + 1]), scale_x2, ptx::pack_f32x2(e.x, e.y)), p[0], p[1]);
+                ptx::unpack_f32x2(ptx::fma_f32x2(ptx::pack_f32x2(s[c][i + 2], s[c][i + 3]), scale_x2, ptx::pack_f32x2(e.z, e.w)), p[2], p[3]);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) got[k] += ac_exp2(p[k]);
               }
             } else {
 #pragma unroll
@@ -849,7 +870,7 @@ attn_mass_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_consta
                 const uint32_t ev[4] = {e.x, e.y, e.z, e.w};
 #pragma unroll
                 for (int k = 0; k < 4; ++k)
-                  if ((see >> (i + k)) & 1u) got[k] += ac_exp2(fmaf(__uint_as_float(s[c][i + k]), a.scale2, -__uint_as_float(ev[k])));
+                  if ((see >> (i + k)) & 1u) got[k] += ac_exp2(fmaf(__uint_as_float(s[c][i + k]), a.scale2, __uint_as_float(ev[k])));
               }
             }
           }
@@ -926,7 +947,7 @@ struct AcPlan {
   int row_tiles, splits, split_keys;       // few rows
   int tok_tile, nx, rows_cap, ctas;        // tiles
   size_t lse_bytes, ml_bytes, o_bytes, cut_bytes, sum_bytes, anc_bytes, ok_bytes;
-  size_t bytes() const { return lse_bytes + ml_bytes + o_bytes + cut_bytes + sum_bytes + anc_bytes + ok_bytes; }
+  size_t bytes() const { return lse_bytes + ml_bytes + o_bytes + cut_bytes + sum_bytes + 2 * anc_bytes + ok_bytes; }
   // Does every grid and every coordinate of the call fit?
   bool launchable(const KvView& c) const {
     const long long heads = static_cast<long long>(c.n_seq) * c.n_kv;
@@ -946,7 +967,7 @@ inline AcPlan ac_plan(const KvView& c, int T, int max_new, int n_heads) {
   p.few = rows <= AC_FEW_ROWS;
   p.row_tiles = p.splits = 1;
   p.lse_bytes = ac_up(static_cast<size_t>(T) * n_heads * 4);
-  p.anc_bytes = max_new <= BITRL_TREE_MAX_TOKENS ? ac_up(static_cast<size_t>(T) * AC_TREE_WORDS * 4) : 0;
+  p.anc_bytes = max_new <= BITRL_TREE_MAX_TOKENS ? ac_up(static_cast<size_t>(T) * AC_TREE_WORDS * 4) : 0;  // twice
   p.ok_bytes = ac_up(static_cast<size_t>(c.n_seq) * 4);
   if (p.few) {
     // ranges of keys are made so that even one row tile per (sequence, kv head) fills the SMs several times over
@@ -1071,11 +1092,13 @@ bitrl_status launch_attention_cached(const KvView& c, const KvBatch& b, const vo
   a.cuts = reinterpret_cast<AtCut*>(take(p.cut_bytes));
   float* sums = reinterpret_cast<float*>(take(p.sum_bytes));
   uint32_t* anc = reinterpret_cast<uint32_t*>(take(p.anc_bytes));
+  uint32_t* desc = reinterpret_cast<uint32_t*>(take(p.anc_bytes));
   int* ok = reinterpret_cast<int*>(take(p.ok_bytes));
   a.anc = b.parent ? anc : nullptr;
+  a.desc = b.parent ? desc : nullptr;
   a.tree_ok = b.parent ? ok : nullptr;
   if (b.parent) {
-    BITRL_CUDA(launch_pdl(attn_tree_kernel, dim3(c.n_seq), dim3(BITRL_TREE_MAX_TOKENS), 0, st, c, b, anc, ok));
+    BITRL_CUDA(launch_pdl(attn_tree_kernel, dim3(c.n_seq), dim3(BITRL_TREE_MAX_TOKENS), 0, st, c, b, anc, desc, ok));
     count_launch(1);
   }
   return c.hd == 128 ? launch_attention_cached_hd<128>(a, p, mass, sums, st) : launch_attention_cached_hd<64>(a, p, mass, sums, st);
