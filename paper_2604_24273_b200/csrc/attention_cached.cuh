@@ -7,6 +7,8 @@
 // row x = token * rep + j.  Everything works on logarithms to base two: t = score * log2(e), p = 2^(t - lse).
 #pragma once
 
+#include <cuda.h>
+
 #include "attention.cuh"
 #include "common.cuh"
 #include "kv_cache.cuh"
@@ -28,15 +30,13 @@ struct AcArgs {
   unsigned short* att;      // the same
   int n_heads, rep;
   float scale2;            // log2(e) / sqrt(head_dim)
-  int row_tiles;           // row tiles of the longest sequence
-  int splits, split_keys;  // key ranges per row tile, slots per range (a multiple of 64)
-  float* part_o;           // [splits][T * n_heads][HD] unnormalised partial results (splits > 1)
-  float2* part_ml;         // [splits][T * n_heads]: running maximum and sum
+  float* part_o;           // [parts][rows][HD] unnormalised results of cut items
+  float2* part_ml;         // [parts][rows]: running maximum and sum
   float* lse;              // [T * n_heads]: maximum + log2(sum); +inf where a row sees nothing
   const uint32_t* anc;     // trees: [T][AC_TREE_WORDS], the tokens that a token sees
   const uint32_t* desc;    // trees: [T][AC_TREE_WORDS], the tokens that see a token
   const int* tree_ok;      // trees: [n_seq], else nullptr
-  AtCut* cuts;             // tiles: [CTAs][2]
+  AtCut* cuts;             // tile kernels: [CTAs][2]
 };
 
 __device__ __forceinline__ float ac_exp2(float x) {
@@ -54,16 +54,6 @@ __device__ __forceinline__ uint32_t pack_bf16x2(float x0, float x1) {
   const __nv_bfloat162 p = __floats2bfloat162_rn(x0, x1);
   return *reinterpret_cast<const uint32_t*>(&p);
 }
-// 16-byte asynchronous copy; bytes = 0 fills the destination with zeros and reads nothing.
-__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, uint32_t bytes) {
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
-}
-__device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int N>
-__device__ __forceinline__ void cp_async_wait() {
-  asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
-}
-
 // Ancestors of every new token as bits, anc[row][AC_TREE_WORDS]: bit j is set when token j of the sequence is the token
 // itself or above it; padding has no bits.  desc is the transpose.  ok[s]: the sequence's tree is one.  One CTA per sequence.
 __global__ void __launch_bounds__(BITRL_TREE_MAX_TOKENS)
@@ -103,400 +93,198 @@ __device__ __forceinline__ bool ac_sees_new(const uint32_t* anc, int tok, int j)
 }
 __device__ __forceinline__ bool ac_is_pad(const uint32_t* anc, int tok) { return anc && !ac_sees_new(anc, tok, tok); }
 
-// First slot that no row of the tile of `rows` rows starting at row x0 sees.
-__device__ __forceinline__ int ac_key_end(const KvSeq& q, int rep, bool tree, int x0, int rows) {
-  return q.used + (tree ? q.m : min(q.m, (x0 + rows - 1) / rep + 1));
+// ---- few rows (at most 16 per sequence and kv head) ------------------------------------------------------------------
+// Bound by the reading of keys and values.  Lengths are known on the device alone, so the work is cut there: the units (16
+// slots of one sequence and kv head) of the whole batch form one list, sequence by sequence and head by head, and every
+// warp of the grid takes an equal run of it, whatever the lengths are.  A warp needs nothing from the others: it brings its
+// units in by TMA through a ring of its own, keeps a running maximum, sum and 16 x HD result, and leaves one result per
+// (sequence, head) that it met.  Results of items that lie within one run are final; the others are joined by
+// attn_few_join_kernel, which also turns the scores that this kernel leaves behind (fp32, 4 to 64 bytes per slot beside
+// the 4 HD bytes of its key and value) into the weight of every slot, so that keys are read once.
+// Scores come from mma.sync (a 16-row tile fills its M; a tcgen05 tile has 128 rows).  The weights are split into two bf16
+// halves (16 significant bits), which costs nothing where reading bounds the kernel.
+constexpr int AF_WARPS = 8;
+constexpr int AF_THREADS = 32 * AF_WARPS;
+constexpr int AF_STAGES = 3;
+constexpr int AF_ROWS = 16;
+constexpr int AF_SLOTS = 16;   // slots of a unit
+constexpr int AF_MIN_RUN = 2;  // units of a run at least (short lists use fewer warps)
+enum { AF_WAIT_LOAD = 151 };
+
+struct AfRun {
+  int s, h, u, left;  // first unit (unit u of item (s, h)) and number of units
+};
+struct AfHead {
+  long long units;  // of the whole list
+  int runs;         // in use
+};
+
+struct AfArgs {
+  AcArgs a;
+  int rows_cap;    // rows of a sequence and head at most: max_new * rep
+  int score_rows;  // rows_cap rounded up to 4, 8 or 16
+  int max_runs;
+  float* scores;   // [pages][kv heads][page][score_rows] or nullptr: scores in base-two units, -inf where unseen
+  AfHead* head;
+  AfRun* run;      // [max_runs]
+};
+
+// First unit of run r.
+__device__ __forceinline__ long long af_start(const AfHead& h, int r) { return h.units * r / h.runs; }
+// The run that holds unit g.
+__device__ __forceinline__ int af_run_of(const AfHead& h, long long g) {
+  int r = static_cast<int>(g * h.runs / h.units);
+  while (r + 1 < h.runs && af_start(h, r + 1) <= g) ++r;
+  while (r > 0 && af_start(h, r) > g) --r;
+  return r;
+}
+// Units of one kv head of sequence s.
+__device__ __forceinline__ int af_units(const AcArgs& a, int s, KvSeq& q) {
+  if (!kv_seq(a.c, a.b, s, q) || q.m == 0 || (a.tree_ok && !a.tree_ok[s])) return 0;
+  return (q.used + q.m + AF_SLOTS - 1) / AF_SLOTS;
 }
 
-// ---- few rows: one 16-row tile per CTA -----------------------------------------------------------------------------
-// Bound by the reading of keys and values.  The warps of a CTA share the rows and take different keys, 16 at a time, each
-// through a ring of its own, so no barrier stands in the loop; every warp keeps its own running maximum, sum and 16 x HD
-// result, and these are joined at the end.  Scores come from mma.sync (a 16-row tile fills its M; a tcgen05 tile has 128).
-// The weights are split into two bf16 halves (16 significant bits), which costs nothing where reading bounds the kernel.
-constexpr int AR_THREADS = 128;
-constexpr int AR_WARPS = AR_THREADS / 32;
-constexpr int AR_STAGES = 3;
-constexpr int AR_ROWS = 16;
-constexpr int AR_KEYS = 16;  // slots per step of a warp
-
 template <int HD>
-constexpr uint32_t ar_smem_bytes() {
-  const uint32_t ring = AR_WARPS * AR_STAGES * 2 * AR_KEYS * HD * 2;
-  const uint32_t join = AR_WARPS * AR_ROWS * (HD * 4 + 8);
-  return ring > join ? ring : join;
+constexpr uint32_t af_smem_bytes() {
+  return AF_WARPS * AF_STAGES * 2 * AF_SLOTS * HD * 2 + 1024;
 }
 
 template <int HD>
-__global__ void __launch_bounds__(AR_THREADS) attn_rows_kernel(const __grid_constant__ AcArgs a) {
-  constexpr int KS = HD / 16, ND = HD / 8, CH = HD / 8;
-  constexpr uint32_t KV_BYTES = AR_KEYS * HD * 2;  // keys (or values) of one step
-  extern __shared__ __align__(128) unsigned char ar_smem[];
-  pdl_enter();
+__global__ void __launch_bounds__(AF_THREADS, 1)
+attn_few_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constant__ CUtensorMap tmap_v, const __grid_constant__ AfArgs f) {
+  constexpr int KS = HD / 16, ND = HD / 8, NH = HD / 64;
+  constexpr uint32_t HALF = AF_SLOTS * 128, TILE = NH * HALF;  // a 64-dimension block of the keys (or values) of a unit
+  extern __shared__ unsigned char af_smem_raw[];
+  __shared__ __align__(8) unsigned long long bars[AF_WARPS * AF_STAGES];
+  __shared__ long long part[AF_WARPS], first_of[AF_THREADS + 1];
+  const AcArgs& a = f.a;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3, lm = lane >> 3, lr = lane & 7;
-  int idx = blockIdx.x;
-  const int split = idx % a.splits;
-  idx /= a.splits;
-  const int rt = idx % a.row_tiles;
-  idx /= a.row_tiles;
-  const int head = idx % a.c.n_kv, s = idx / a.c.n_kv;
+  const uint32_t bar = ptx::smem_u32(bars + warp * AF_STAGES);
+  if (threadIdx.x < AF_WARPS * AF_STAGES) ptx::mbar_init(ptx::smem_u32(bars + threadIdx.x), 1);
+  if (threadIdx.x == 0) {
+    ptx::tma_prefetch_desc(&tmap_k);
+    ptx::tma_prefetch_desc(&tmap_v);
+  }
+  ptx::mbar_init_fence();
+  pdl_enter();
+
+  // ---- this warp's run: units before every block of sequences, then a search
   KvSeq q;
-  if (!kv_seq(a.c, a.b, s, q)) return;
-  const int x0 = rt * AR_ROWS;
-  if (x0 >= q.m * a.rep) return;
-  const int end = ac_key_end(q, a.rep, a.b.parent != nullptr, x0, AR_ROWS);
-  const int k0 = split * a.split_keys, k1 = min(end, k0 + a.split_keys);
-  if (k0 >= end) return;
-  if (a.tree_ok && !a.tree_ok[s]) return;
-  const uint32_t* anc = a.b.parent ? a.anc + static_cast<long long>(q.t0) * AC_TREE_WORDS : nullptr;
-
-  // ---- queries of rows g and g + 8 of the tile
-  uint32_t qa[KS][4];
-  int tok[2];
+  const int per = (a.c.n_seq + AF_THREADS - 1) / AF_THREADS, sb = min(a.c.n_seq, per * static_cast<int>(threadIdx.x));
+  long long sum = 0;
+  for (int s = sb; s < min(a.c.n_seq, sb + per); ++s) sum += af_units(a, s, q);
+  sum *= a.c.n_kv;
+  long long incl = sum;
 #pragma unroll
-  for (int rr = 0; rr < 2; ++rr) {
-    const int x = x0 + g + 8 * rr;
-    const bool live = x < q.m * a.rep;
-    tok[rr] = live ? x / a.rep : 0;
-    const unsigned short* row =
-        a.q + (static_cast<long long>(q.t0 + tok[rr]) * a.n_heads + head * a.rep + (live ? x - tok[rr] * a.rep : 0)) * HD + 2 * t;
-#pragma unroll
-    for (int ks = 0; ks < KS; ++ks) {
-      qa[ks][rr] = live ? *reinterpret_cast<const uint32_t*>(row + 16 * ks) : 0u;
-      qa[ks][2 + rr] = live ? *reinterpret_cast<const uint32_t*>(row + 16 * ks + 8) : 0u;
-    }
+  for (int o = 1; o < 32; o <<= 1) {
+    const long long v = __shfl_up_sync(0xffffffffu, incl, o);
+    if (lane >= o) incl += v;
   }
-
-  const uint32_t ring = ptx::smem_u32(ar_smem) + warp * (AR_STAGES * 2 * KV_BYTES);
-  const int slot_mask = (1 << a.c.page_shift) - 1;
-  auto load = [&](int slot0, int stage) {  // slots [slot0, slot0 + 16) of one page
-    const int page = kv_page(a.c, s, slot0);
-    const long long row0 = kv_row(a.c, 0, page < 0 ? 0 : page, head) + (slot0 & slot_mask);
-    const uint32_t dk = ring + stage * 2 * KV_BYTES;
-#pragma unroll
-    for (int u = 0; u < AR_KEYS * CH / 32; ++u) {
-      const int i = lane + 32 * u, r = i / CH, ch = i % CH;
-      const int slot = slot0 + r;
-      const bool have = page >= 0 && slot < k1 && !(anc && slot >= q.used && ac_is_pad(anc, slot - q.used));
-      const uint32_t off = r * (HD * 2) + ((ch ^ (r & 7)) << 4);
-      const long long src = have ? (row0 + r) * HD + ch * 8 : 0;
-      cp_async16(dk + off, a.c.k + src, have ? 16u : 0u);
-      cp_async16(dk + KV_BYTES + off, a.c.v + src, have ? 16u : 0u);
-    }
-  };
-
-  float o[ND][4];
-#pragma unroll
-  for (int nd = 0; nd < ND; ++nd)
-#pragma unroll
-    for (int e = 0; e < 4; ++e) o[nd][e] = 0.0f;
-  float m_run[2] = {-INFINITY, -INFINITY}, l_run[2] = {0.0f, 0.0f};
-
-  const int step = AR_WARPS * AR_KEYS;
-  int slot0 = k0 + warp * AR_KEYS;
-#pragma unroll
-  for (int i = 0; i < AR_STAGES - 1; ++i) {
-    if (slot0 + i * step < k1) load(slot0 + i * step, i);
-    cp_async_commit();
-  }
-  int stage = 0;
-  for (; slot0 < k1; slot0 += step) {
-    cp_async_wait<AR_STAGES - 2>();
-    __syncwarp();
-    {
-      const int ahead = slot0 + (AR_STAGES - 1) * step, st = stage == 0 ? AR_STAGES - 1 : stage - 1;
-      if (ahead < k1) load(ahead, st);
-      cp_async_commit();
-    }
-    const uint32_t ks_addr = ring + stage * 2 * KV_BYTES, vs_addr = ks_addr + KV_BYTES;
-    float c[2][4];
-#pragma unroll
-    for (int nt = 0; nt < 2; ++nt)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) c[nt][e] = 0.0f;
-#pragma unroll
-    for (int ks = 0; ks < KS; ++ks) {
-      const int key = 8 * (lm >> 1) + lr, ch = 2 * ks + (lm & 1);
-      uint32_t kb[4];
-      ldmatrix_x4(ks_addr + key * (HD * 2) + ((ch ^ (key & 7)) << 4), kb);
-      mma_bf16(c[0], qa[ks], kb[0], kb[1]);
-      mma_bf16(c[1], qa[ks], kb[2], kb[3]);
-    }
-    // ---- scale, mask; slots below used are seen by every row
-    const bool masked = slot0 + AR_KEYS > q.used || slot0 + AR_KEYS > k1;
-    float mx[2] = {-INFINITY, -INFINITY};
-#pragma unroll
-    for (int nt = 0; nt < 2; ++nt)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        float v = __fmul_rn(c[nt][e], a.scale2);
-        if (masked) {
-          const int slot = slot0 + 8 * nt + 2 * t + (e & 1);
-          const bool see = slot < k1 && (slot < q.used || ac_sees_new(anc, tok[e >> 1], slot - q.used));
-          v = see ? v : -INFINITY;
-        }
-        c[nt][e] = v;
-        mx[e >> 1] = fmaxf(mx[e >> 1], v);
-      }
-    float alpha[2];
-#pragma unroll
-    for (int rr = 0; rr < 2; ++rr) {
-      mx[rr] = fmaxf(mx[rr], __shfl_xor_sync(0xffffffffu, mx[rr], 1));
-      mx[rr] = fmaxf(mx[rr], __shfl_xor_sync(0xffffffffu, mx[rr], 2));
-      const float m_new = fmaxf(m_run[rr], mx[rr]);
-      alpha[rr] = m_new == m_run[rr] ? 1.0f : ac_exp2(m_run[rr] - m_new);
-      m_run[rr] = m_new;
-    }
-    float sum[2] = {0.0f, 0.0f};
-#pragma unroll
-    for (int nt = 0; nt < 2; ++nt)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const float mm = m_run[e >> 1];
-        c[nt][e] = c[nt][e] == -INFINITY ? 0.0f : ac_exp2(c[nt][e] - mm);
-        sum[e >> 1] += c[nt][e];
-      }
-    l_run[0] = fmaf(l_run[0], alpha[0], sum[0]);
-    l_run[1] = fmaf(l_run[1], alpha[1], sum[1]);
-    if (__any_sync(0xffffffffu, alpha[0] != 1.0f || alpha[1] != 1.0f)) {
-#pragma unroll
-      for (int nd = 0; nd < ND; ++nd) {
-        o[nd][0] = __fmul_rn(o[nd][0], alpha[0]);
-        o[nd][1] = __fmul_rn(o[nd][1], alpha[0]);
-        o[nd][2] = __fmul_rn(o[nd][2], alpha[1]);
-        o[nd][3] = __fmul_rn(o[nd][3], alpha[1]);
-      }
-    }
-    // A value that is not finite in a slot that some row does not see must not reach that row as 0 * inf: such a step
-    // (new tokens only) goes through scalar sums over the seen slots.
-    bool odd = false;
-    if (masked) {
-#pragma unroll
-      for (int u = 0; u < AR_KEYS * CH / 32; ++u) {
-        const uint4 x = ptx::lds128(vs_addr + (lane + 32 * u) * 16);
-        const uint32_t w[4] = {x.x, x.y, x.z, x.w};
-#pragma unroll
-        for (int j = 0; j < 4; ++j) odd |= (w[j] & 0x7f80u) == 0x7f80u || (w[j] & 0x7f800000u) == 0x7f800000u;
-      }
-      odd = __any_sync(0xffffffffu, odd);
-    }
-    if (!odd) {
-      uint32_t ph[4], pl[4];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const float p0 = c[i >> 1][2 * (i & 1)], p1 = c[i >> 1][2 * (i & 1) + 1];
-        ph[i] = pack_bf16x2(p0, p1);
-        pl[i] = pack_bf16x2(p0 - __uint_as_float(ph[i] << 16), p1 - __uint_as_float(ph[i] & 0xffff0000u));
-      }
-#pragma unroll
-      for (int nd = 0; nd < ND; nd += 2) {
-        const int key = 8 * (lm & 1) + lr, ch = nd + (lm >> 1);
-        uint32_t vb[4];
-        ldmatrix_x4_trans(vs_addr + key * (HD * 2) + ((ch ^ (key & 7)) << 4), vb);
-        mma_bf16(o[nd], ph, vb[0], vb[1]);
-        mma_bf16(o[nd + 1], ph, vb[2], vb[3]);
-        mma_bf16(o[nd], pl, vb[0], vb[1]);
-        mma_bf16(o[nd + 1], pl, vb[2], vb[3]);
-      }
-    } else {
-      for (int key = 0; key < AR_KEYS; ++key) {
-        const int from = (lane & ~3) | ((key & 7) >> 1);  // the lane of this row group that holds the key's weight
-        float p[2];
-#pragma unroll
-        for (int rr = 0; rr < 2; ++rr) {
-          const float w00 = __shfl_sync(0xffffffffu, c[0][2 * rr], from), w01 = __shfl_sync(0xffffffffu, c[0][2 * rr + 1], from);
-          const float w10 = __shfl_sync(0xffffffffu, c[1][2 * rr], from), w11 = __shfl_sync(0xffffffffu, c[1][2 * rr + 1], from);
-          p[rr] = key < 8 ? ((key & 1) ? w01 : w00) : ((key & 1) ? w11 : w10);
-        }
-        const int slot = slot0 + key;
-        bool see[2];
-#pragma unroll
-        for (int rr = 0; rr < 2; ++rr) see[rr] = slot < k1 && (slot < q.used || ac_sees_new(anc, tok[rr], slot - q.used));
-#pragma unroll
-        for (int nd = 0; nd < ND; ++nd) {
-          const uint32_t w = ptx::lds32(vs_addr + key * (HD * 2) + ((nd ^ (key & 7)) << 4) + 4 * t);
-          const float v0 = __uint_as_float(w << 16), v1 = __uint_as_float(w & 0xffff0000u);
-          if (see[0]) { o[nd][0] = fmaf(p[0], v0, o[nd][0]); o[nd][1] = fmaf(p[0], v1, o[nd][1]); }
-          if (see[1]) { o[nd][2] = fmaf(p[1], v0, o[nd][2]); o[nd][3] = fmaf(p[1], v1, o[nd][3]); }
-        }
-      }
-    }
-    __syncwarp();
-    stage = stage == AR_STAGES - 1 ? 0 : stage + 1;
-  }
-  cp_async_wait<0>();
-
-  // ---- join the warps
+  if (lane == 31) part[warp] = incl;
   __syncthreads();
-  float* jo = reinterpret_cast<float*>(ar_smem);                                  // [warp][row][HD]
-  float2* jml = reinterpret_cast<float2*>(jo + AR_WARPS * AR_ROWS * HD);          // [warp][row]
-#pragma unroll
-  for (int rr = 0; rr < 2; ++rr) {
-    l_run[rr] += __shfl_xor_sync(0xffffffffu, l_run[rr], 1);
-    l_run[rr] += __shfl_xor_sync(0xffffffffu, l_run[rr], 2);
-    const int r = warp * AR_ROWS + g + 8 * rr;
-    if (t == 0) jml[r] = make_float2(m_run[rr], l_run[rr]);
-#pragma unroll
-    for (int nd = 0; nd < ND; ++nd)
-      *reinterpret_cast<float2*>(jo + r * HD + 8 * nd + 2 * t) = make_float2(o[nd][2 * rr], o[nd][2 * rr + 1]);
-  }
+  for (int w = 0; w < warp; ++w) incl += part[w];
+  first_of[threadIdx.x + 1] = incl;
+  if (threadIdx.x == 0) first_of[0] = 0;
   __syncthreads();
-  constexpr int PER = AR_ROWS * HD / AR_THREADS;  // consecutive dimensions of one row per thread
-  const int r = threadIdx.x / (HD / PER), d0 = (threadIdx.x % (HD / PER)) * PER;
-  const int x = x0 + r;
-  if (x >= q.m * a.rep) return;
-  float m_all = -INFINITY, l_all = 0.0f, acc[PER];
-#pragma unroll
-  for (int w = 0; w < AR_WARPS; ++w) m_all = fmaxf(m_all, jml[w * AR_ROWS + r].x);
-#pragma unroll
-  for (int i = 0; i < PER; ++i) acc[i] = 0.0f;
-#pragma unroll
-  for (int w = 0; w < AR_WARPS; ++w) {
-    const float2 ml = jml[w * AR_ROWS + r];
-    const float f = ml.x == -INFINITY ? 0.0f : ac_exp2(ml.x - m_all);
-    if (ml.x == -INFINITY) continue;
-    l_all = fmaf(ml.y, f, l_all);
-#pragma unroll
-    for (int i = 0; i < PER; ++i) acc[i] = fmaf(jo[(w * AR_ROWS + r) * HD + d0 + i], f, acc[i]);
-  }
-  const int tk = x / a.rep;
-  const long long row = static_cast<long long>(q.t0 + tk) * a.n_heads + head * a.rep + (x - tk * a.rep);
-  if (a.splits > 1) {
-    const long long at = static_cast<long long>(split) * a.b.T * a.n_heads + row;
-#pragma unroll
-    for (int i = 0; i < PER; i += 4)
-      *reinterpret_cast<float4*>(a.part_o + at * HD + d0 + i) = make_float4(acc[i], acc[i + 1], acc[i + 2], acc[i + 3]);
-    if (d0 == 0) a.part_ml[at] = make_float2(m_all, l_all);
+  AfHead head;
+  head.units = first_of[AF_THREADS];
+  head.runs = static_cast<int>(min(static_cast<long long>(f.max_runs), (head.units + AF_MIN_RUN - 1) / AF_MIN_RUN));
+  // neighbouring runs go to different CTAs, so that a short list spreads over all SMs
+  const int r = warp * gridDim.x + blockIdx.x;
+  if (blockIdx.x == 0 && threadIdx.x == 0) *f.head = head;
+  if (r >= head.runs) {
+    if (lane == 0) f.run[r].left = 0;
     return;
   }
-  const bool none = l_all == 0.0f || ac_is_pad(anc, tk);
-  const float inv = none ? 0.0f : __fdiv_rn(1.0f, l_all);
-#pragma unroll
-  for (int i = 0; i < PER; i += 2)
-    *reinterpret_cast<uint32_t*>(a.att + row * HD + d0 + i) = none ? 0u : pack_bf16x2(__fmul_rn(acc[i], inv), __fmul_rn(acc[i + 1], inv));
-  if (d0 == 0) a.lse[row] = none ? INFINITY : m_all + __log2f(l_all);
-}
-
-// Joins the key ranges of every row; one warp per row, ranges in ascending order.
-template <int HD>
-__global__ void __launch_bounds__(128) attn_join_kernel(const __grid_constant__ AcArgs a) {
-  pdl_enter();
-  const int lane = threadIdx.x & 31;
-  // rows of a sequence: blockIdx = sequence * blocks per sequence + block, four rows each
-  const int per_seq = (a.b.max_new * a.n_heads + 3) / 4;
-  const int s = blockIdx.x / per_seq, i = (blockIdx.x - s * per_seq) * 4 + (threadIdx.x >> 5);
-  KvSeq q;
-  if (!kv_seq(a.c, a.b, s, q)) return;
-  const int tok = i / a.n_heads, h = i - tok * a.n_heads;
-  if (tok >= q.m) return;
-  bool pad = false;
-  if (a.b.parent) pad = a.b.parent[q.t0 + tok] == BITRL_PARENT_PAD;
-  const int x = tok * a.rep + h % a.rep;
-  const int end = ac_key_end(q, a.rep, a.b.parent != nullptr, x / AR_ROWS * AR_ROWS, AR_ROWS);
-  const int n = (end + a.split_keys - 1) / a.split_keys;
-  const long long row = static_cast<long long>(q.t0) * a.n_heads + i, stride = static_cast<long long>(a.b.T) * a.n_heads;
-  float m_all = -INFINITY;
-  for (int k = lane; k < n; k += 32) m_all = fmaxf(m_all, a.part_ml[k * stride + row].x);
-  m_all = warp_max(m_all);
-  constexpr int PER = HD / 32;
-  float l_all = 0.0f, acc[PER];
-#pragma unroll
-  for (int e = 0; e < PER; ++e) acc[e] = 0.0f;
-  for (int k = 0; k < n; ++k) {
-    const float2 ml = a.part_ml[k * stride + row];
-    if (ml.x == -INFINITY) continue;
-    const float f = ac_exp2(ml.x - m_all);
-    l_all = fmaf(ml.y, f, l_all);
-    const float* po = a.part_o + (k * stride + row) * HD + lane * PER;
-#pragma unroll
-    for (int e = 0; e < PER; ++e) acc[e] = fmaf(po[e], f, acc[e]);
+  const long long w0 = af_start(head, r);
+  int left = static_cast<int>(af_start(head, r + 1) - w0), s = 0, h = 0, u0 = 0;
+  {
+    int block = 0;  // the last block that begins at or before w0: blocks without units do not count
+    for (int i = lane; i < AF_THREADS; i += 32)
+      if (first_of[i] <= w0 && w0 < first_of[i + 1]) block = i;
+    block = __reduce_max_sync(0xffffffffu, block);
+    long long rem = w0 - first_of[block];
+    for (s = block * per;; ++s) {
+      const long long n = static_cast<long long>(af_units(a, s, q)) * a.c.n_kv;
+      if (rem < n || s + 1 >= a.c.n_seq) break;
+      rem -= n;
+    }
+    const int n = af_units(a, s, q);
+    h = static_cast<int>(rem / n);
+    u0 = static_cast<int>(rem % n);
   }
-  const bool none = pad || l_all == 0.0f;
-  const float inv = none ? 0.0f : __fdiv_rn(1.0f, l_all);
-#pragma unroll
-  for (int e = 0; e < PER; e += 2)
-    *reinterpret_cast<uint32_t*>(a.att + row * HD + lane * PER + e) = none ? 0u : pack_bf16x2(__fmul_rn(acc[e], inv), __fmul_rn(acc[e + 1], inv));
-  if (lane == 0) a.lse[row] = none ? INFINITY : m_all + __log2f(l_all);
-}
+  if (lane == 0) f.run[r] = AfRun{s, h, u0, left};
 
-// ---- weight received by every slot ---------------------------------------------------------------------------------
-// A second pass over the keys: with the final maximum and sum of every row known, a CTA owns 64 slots of one kv head, forms
-// their scores with all rows of the sequence and adds up each slot's weights in registers; a slot belongs to one CTA, so
-// nothing is added atomically.
-constexpr int AS_THREADS = 128;
-constexpr int AS_KEYS = 64;
-constexpr int AS_ROWS = 64;  // rows per step
-
-template <int HD>
-constexpr uint32_t as_smem_bytes() {
-  return AS_KEYS * HD * 2 + 2 * AS_ROWS * (HD * 2 + 4);
-}
-
-template <int HD>
-__global__ void __launch_bounds__(AS_THREADS) attn_mass_few_kernel(const __grid_constant__ AcArgs a) {
-  constexpr int KS = HD / 16, CH = HD / 8;
-  constexpr uint32_t K_BYTES = AS_KEYS * HD * 2, Q_BYTES = AS_ROWS * HD * 2;
-  extern __shared__ __align__(128) unsigned char am_smem[];
-  pdl_enter();
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3, lm = lane >> 3, lr = lane & 7;
-  const int tiles = (((a.c.max_pages << a.c.page_shift) + AS_KEYS - 1) / AS_KEYS);
-  int idx = blockIdx.x;
-  const int kt = idx % tiles;
-  idx /= tiles;
-  const int head = idx % a.c.n_kv, s = idx / a.c.n_kv;
-  KvSeq q;
-  if (!kv_seq(a.c, a.b, s, q)) return;
-  const int slot0 = kt * AS_KEYS, end = q.used + q.m;
-  if (slot0 >= end || q.m == 0) return;
-  float* lse_s = reinterpret_cast<float*>(am_smem + K_BYTES + 2 * Q_BYTES);  // [2][AS_ROWS]
-  if (a.tree_ok && !a.tree_ok[s]) return;
-  const uint32_t* anc = a.b.parent ? a.anc + static_cast<long long>(q.t0) * AC_TREE_WORDS : nullptr;
-  const uint32_t k_addr = ptx::smem_u32(am_smem), q_addr = k_addr + K_BYTES;
+  // ---- loads, ahead of the arithmetic: a position of their own in the list
+  const uint32_t raw = ptx::smem_u32(af_smem_raw), ring = ((raw + 1023u) & ~1023u) + warp * (AF_STAGES * 2 * TILE);
   const int slot_mask = (1 << a.c.page_shift) - 1;
-  for (int i = threadIdx.x; i < AS_KEYS * CH; i += AS_THREADS) {
-    const int r = i / CH, ch = i % CH, slot = slot0 + r;
-    int page = -1;
-    if (slot < end) page = kv_page(a.c, s, slot);
-    const long long src = page < 0 ? 0 : (kv_row(a.c, 0, page, head) + (slot & slot_mask)) * HD + ch * 8;
-    cp_async16(k_addr + r * (HD * 2) + ((ch ^ (r & 7)) << 4), a.c.k + src, page < 0 ? 0u : 16u);
-  }
-  const int rows = q.m * a.rep;
-  // rows below the first that can see this tile's slots
-  const int first = (!anc && slot0 > q.used ? min(q.m, slot0 - q.used) * a.rep : 0) / AS_ROWS * AS_ROWS;
-  auto load_q = [&](int x0, int buf) {
-    for (int i = threadIdx.x; i < AS_ROWS * CH; i += AS_THREADS) {
-      const int r = i / CH, ch = i % CH, x = x0 + r;
-      const int tk = x / a.rep;
-      const long long row = static_cast<long long>(q.t0 + tk) * a.n_heads + head * a.rep + (x - tk * a.rep);
-      cp_async16(q_addr + buf * Q_BYTES + r * (HD * 2) + ((ch ^ (r & 7)) << 4), a.q + (x < rows ? row * HD + ch * 8 : 0),
-                 x < rows ? 16u : 0u);
-    }
-    if (threadIdx.x < AS_ROWS) {
-      const int x = x0 + threadIdx.x, tk = x / a.rep;
-      lse_s[buf * AS_ROWS + threadIdx.x] =
-          x < rows ? a.lse[static_cast<long long>(q.t0 + tk) * a.n_heads + head * a.rep + (x - tk * a.rep)] : INFINITY;
-    }
-  };
-  load_q(first, 0);
-  cp_async_commit();
-  uint32_t ka[KS][4];
-  float got[2] = {0.0f, 0.0f};  // slots g and g + 8 of the warp's 16
-  const int key_lo = slot0 + warp * 16 + g;
-  const bool masked = slot0 + AS_KEYS > q.used;
-  int buf = 0;
-  for (int x0 = first; x0 < rows; x0 += AS_ROWS, buf ^= 1) {
-    cp_async_wait<0>();
-    __syncthreads();
-    if (x0 + AS_ROWS < rows) load_q(x0 + AS_ROWS, buf ^ 1);
-    cp_async_commit();
-    if (x0 == first) {
+  int ls = s, lh = h, lu = u0, l_left = left;
+  KvSeq lq = q;
+  int l_units = af_units(a, ls, lq);
+  auto load = [&](int stage) {
+    if (l_left <= 0) return;
+    if (lane == 0) {
+      const int slot0 = lu * AF_SLOTS;
+      const int page = kv_page(a.c, ls, slot0);
+      // a page that the table does not have: a row behind the pool, which fills with zeros
+      const int row = page < 0 ? a.c.n_pages * a.c.n_kv << a.c.page_shift
+                               : static_cast<int>(((page * a.c.n_kv + lh) << a.c.page_shift) + (slot0 & slot_mask));
+      const uint32_t dst = ring + stage * 2 * TILE;
+      ptx::mbar_arrive_expect_tx(bar + 8 * stage, 2 * TILE);
 #pragma unroll
-      for (int ks = 0; ks < KS; ++ks) {
-        const int key = warp * 16 + 8 * (lm & 1) + lr, ch = 2 * ks + (lm >> 1);
-        ldmatrix_x4(k_addr + key * (HD * 2) + ((ch ^ (key & 7)) << 4), ka[ks]);
+      for (int i = 0; i < NH; ++i) {
+        ptx::tma_load_2d(dst + i * HALF, &tmap_k, 64 * i, row, bar + 8 * stage);
+        ptx::tma_load_2d(dst + TILE + i * HALF, &tmap_v, 64 * i, row, bar + 8 * stage);
       }
     }
-    for (int n0 = 0; n0 < AS_ROWS; n0 += 16) {
-      if (x0 + n0 >= rows) break;
+    --l_left;
+    if (++lu == l_units && l_left > 0) {
+      lu = 0;
+      if (++lh == a.c.n_kv) {
+        lh = 0;
+        do l_units = af_units(a, ++ls, lq);
+        while (l_units == 0 && ls + 1 < a.c.n_seq);
+      }
+    }
+  };
+  for (int i = 0; i < AF_STAGES; ++i) load(i);
+  uint32_t stage = 0, phase = 0;
+  bool ok = true;
+
+  while (ok && left > 0) {
+    const int units = af_units(a, s, q);
+    const int u1 = min(units, u0 + left), end = q.used + q.m, rows = q.m * a.rep;
+    const uint32_t* anc = a.b.parent ? a.anc + static_cast<long long>(q.t0) * AC_TREE_WORDS : nullptr;
+    // queries of rows g and g + 8
+    uint32_t qa[KS][4];
+    int tok[2];
+#pragma unroll
+    for (int rr = 0; rr < 2; ++rr) {
+      const int x = g + 8 * rr;
+      const bool live = x < rows;
+      tok[rr] = live ? x / a.rep : 0;
+      const unsigned short* row =
+          a.q + (static_cast<long long>(q.t0 + tok[rr]) * a.n_heads + h * a.rep + (live ? x - tok[rr] * a.rep : 0)) * HD + 2 * t;
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) {
+        qa[ks][rr] = live ? *reinterpret_cast<const uint32_t*>(row + 16 * ks) : 0u;
+        qa[ks][2 + rr] = live ? *reinterpret_cast<const uint32_t*>(row + 16 * ks + 8) : 0u;
+      }
+    }
+    float o[ND][4];
+#pragma unroll
+    for (int nd = 0; nd < ND; ++nd)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[nd][e] = 0.0f;
+    float m_run[2] = {-INFINITY, -INFINITY}, l_run[2] = {0.0f, 0.0f};
+
+    for (int u = u0; u < u1; ++u) {
+      const int slot0 = u * AF_SLOTS;
+      if (!__any_sync(0xffffffffu, ptx::mbar_wait(bar + 8 * stage, phase))) {
+        ok = false;
+        break;
+      }
+      const uint32_t ks_addr = ring + stage * 2 * TILE, vs_addr = ks_addr + TILE;
       float c[2][4];
 #pragma unroll
       for (int nt = 0; nt < 2; ++nt)
@@ -504,39 +292,263 @@ __global__ void __launch_bounds__(AS_THREADS) attn_mass_few_kernel(const __grid_
         for (int e = 0; e < 4; ++e) c[nt][e] = 0.0f;
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks) {
-        const int r = n0 + 8 * (lm >> 1) + lr, ch = 2 * ks + (lm & 1);
-        uint32_t qb[4];
-        ldmatrix_x4(q_addr + buf * Q_BYTES + r * (HD * 2) + ((ch ^ (r & 7)) << 4), qb);
-        mma_bf16(c[0], ka[ks], qb[0], qb[1]);
-        mma_bf16(c[1], ka[ks], qb[2], qb[3]);
+        const int key = 8 * (lm >> 1) + lr, ch = 2 * ks + (lm & 1);
+        uint32_t kb[4];
+        ldmatrix_x4(ks_addr + (ch >> 3) * HALF + key * 128 + (((ch ^ key) & 7) << 4), kb);
+        mma_bf16(c[0], qa[ks], kb[0], kb[1]);
+        mma_bf16(c[1], qa[ks], kb[2], kb[3]);
       }
+      // ---- scale, mask; slots below used are seen by every row
+      const bool masked = slot0 + AF_SLOTS > q.used;
+      float mx[2] = {-INFINITY, -INFINITY};
 #pragma unroll
       for (int nt = 0; nt < 2; ++nt)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          const int r = n0 + 8 * nt + 2 * t + (e & 1), x = x0 + r;
-          const float lse = lse_s[buf * AS_ROWS + r];
-          bool see = lse != INFINITY;
+          float v = __fmul_rn(c[nt][e], a.scale2);
           if (masked) {
-            const int slot = key_lo + 8 * (e >> 1);
-            see = see && slot < end && (slot < q.used || ac_sees_new(anc, x / a.rep, slot - q.used));
+            const int slot = slot0 + 8 * nt + 2 * t + (e & 1);
+            const bool see = slot < end && (slot < q.used || ac_sees_new(anc, tok[e >> 1], slot - q.used));
+            v = see ? v : -INFINITY;
           }
-          if (see) got[e >> 1] += ac_exp2(fmaf(c[nt][e], a.scale2, -lse));
+          c[nt][e] = v;
+          mx[e >> 1] = fmaxf(mx[e >> 1], v);
         }
-    }
-    __syncthreads();
-  }
+      if (f.scores) {
+        const int page = kv_page(a.c, s, slot0);
+        if (page >= 0) {
+          float* at = f.scores + ((kv_row(a.c, 0, page, h) + (slot0 & slot_mask)) + 2 * t) * f.score_rows;
 #pragma unroll
-  for (int rr = 0; rr < 2; ++rr) {
-    got[rr] += __shfl_xor_sync(0xffffffffu, got[rr], 1);
-    got[rr] += __shfl_xor_sync(0xffffffffu, got[rr], 2);
-    const int slot = key_lo + 8 * rr;
-    if (t == 0 && slot < end) {
-      const int page = kv_page(a.c, s, slot);
-      if (page >= 0) {
-        float* w = a.c.mass + kv_row(a.c, 0, page, head) + (slot & slot_mask);
-        *w += got[rr];
+          for (int nt = 0; nt < 2; ++nt)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const int x = g + 8 * (e >> 1);
+              if (x < f.score_rows) at[(8 * nt + (e & 1)) * f.score_rows + x] = c[nt][e];
+            }
+        }
       }
+      float alpha[2];
+#pragma unroll
+      for (int rr = 0; rr < 2; ++rr) {
+        mx[rr] = fmaxf(mx[rr], __shfl_xor_sync(0xffffffffu, mx[rr], 1));
+        mx[rr] = fmaxf(mx[rr], __shfl_xor_sync(0xffffffffu, mx[rr], 2));
+        const float m_new = fmaxf(m_run[rr], mx[rr]);
+        alpha[rr] = m_new == m_run[rr] ? 1.0f : ac_exp2(m_run[rr] - m_new);
+        m_run[rr] = m_new;
+      }
+      float add[2] = {0.0f, 0.0f};
+#pragma unroll
+      for (int nt = 0; nt < 2; ++nt)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          c[nt][e] = c[nt][e] == -INFINITY ? 0.0f : ac_exp2(c[nt][e] - m_run[e >> 1]);
+          add[e >> 1] += c[nt][e];
+        }
+      l_run[0] = fmaf(l_run[0], alpha[0], add[0]);
+      l_run[1] = fmaf(l_run[1], alpha[1], add[1]);
+      if (__any_sync(0xffffffffu, alpha[0] != 1.0f || alpha[1] != 1.0f)) {
+#pragma unroll
+        for (int nd = 0; nd < ND; ++nd) {
+          o[nd][0] = __fmul_rn(o[nd][0], alpha[0]);
+          o[nd][1] = __fmul_rn(o[nd][1], alpha[0]);
+          o[nd][2] = __fmul_rn(o[nd][2], alpha[1]);
+          o[nd][3] = __fmul_rn(o[nd][3], alpha[1]);
+        }
+      }
+      // A value that is not finite in a slot that some row does not see (or behind the last slot) must not reach that row
+      // as 0 * inf: such a unit goes through scalar sums over the seen slots.
+      bool odd = false;
+      if (masked) {
+#pragma unroll
+        for (int i = 0; i < static_cast<int>(TILE / 512); ++i) {
+          const uint4 x = ptx::lds128(vs_addr + (lane + 32 * i) * 16);
+          const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+          for (int j = 0; j < 4; ++j) odd |= (w[j] & 0x7f80u) == 0x7f80u || (w[j] & 0x7f800000u) == 0x7f800000u;
+        }
+        odd = __any_sync(0xffffffffu, odd);
+      }
+      if (!odd) {
+        uint32_t ph[4], pl[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float p0 = c[i >> 1][2 * (i & 1)], p1 = c[i >> 1][2 * (i & 1) + 1];
+          ph[i] = pack_bf16x2(p0, p1);
+          pl[i] = pack_bf16x2(p0 - __uint_as_float(ph[i] << 16), p1 - __uint_as_float(ph[i] & 0xffff0000u));
+        }
+#pragma unroll
+        for (int nd = 0; nd < ND; nd += 2) {
+          const int key = 8 * (lm & 1) + lr, ch = nd + (lm >> 1);
+          uint32_t vb[4];
+          ldmatrix_x4_trans(vs_addr + (ch >> 3) * HALF + key * 128 + (((ch ^ key) & 7) << 4), vb);
+          mma_bf16(o[nd], ph, vb[0], vb[1]);
+          mma_bf16(o[nd + 1], ph, vb[2], vb[3]);
+          mma_bf16(o[nd], pl, vb[0], vb[1]);
+          mma_bf16(o[nd + 1], pl, vb[2], vb[3]);
+        }
+      } else {
+        for (int key = 0; key < AF_SLOTS; ++key) {
+          const int from = (lane & ~3) | ((key & 7) >> 1);  // the lane of this row group that holds the key's weight
+          float p[2];
+          bool see[2];
+          const int slot = slot0 + key;
+#pragma unroll
+          for (int rr = 0; rr < 2; ++rr) {
+            const float w00 = __shfl_sync(0xffffffffu, c[0][2 * rr], from), w01 = __shfl_sync(0xffffffffu, c[0][2 * rr + 1], from);
+            const float w10 = __shfl_sync(0xffffffffu, c[1][2 * rr], from), w11 = __shfl_sync(0xffffffffu, c[1][2 * rr + 1], from);
+            p[rr] = key < 8 ? ((key & 1) ? w01 : w00) : ((key & 1) ? w11 : w10);
+            see[rr] = slot < end && (slot < q.used || ac_sees_new(anc, tok[rr], slot - q.used));
+          }
+#pragma unroll
+          for (int nd = 0; nd < ND; ++nd) {
+            const uint32_t w = ptx::lds32(vs_addr + (nd >> 3) * HALF + key * 128 + (((nd ^ key) & 7) << 4) + 4 * t);
+            const float v0 = __uint_as_float(w << 16), v1 = __uint_as_float(w & 0xffff0000u);
+            if (see[0]) { o[nd][0] = fmaf(p[0], v0, o[nd][0]); o[nd][1] = fmaf(p[0], v1, o[nd][1]); }
+            if (see[1]) { o[nd][2] = fmaf(p[1], v0, o[nd][2]); o[nd][3] = fmaf(p[1], v1, o[nd][3]); }
+          }
+        }
+      }
+      __syncwarp();
+      load(stage);  // the unit AF_STAGES ahead takes this one's place
+      if (++stage == AF_STAGES) {
+        stage = 0;
+        phase ^= 1u;
+      }
+    }
+    if (!ok) break;
+
+    // ---- the item, or this run's part of it
+    const bool whole = u0 == 0 && u1 == units;
+    const int cut = 2 * r + (u0 == 0 ? 1 : 0);
+#pragma unroll
+    for (int rr = 0; rr < 2; ++rr) {
+      l_run[rr] += __shfl_xor_sync(0xffffffffu, l_run[rr], 1);
+      l_run[rr] += __shfl_xor_sync(0xffffffffu, l_run[rr], 2);
+      const int x = g + 8 * rr;
+      if (x >= rows) continue;
+      if (whole) {
+        const bool none = l_run[rr] == 0.0f || ac_is_pad(anc, tok[rr]);
+        const float inv = none ? 0.0f : __fdiv_rn(1.0f, l_run[rr]);
+        const long long row = static_cast<long long>(q.t0 + tok[rr]) * a.n_heads + h * a.rep + x - tok[rr] * a.rep;
+#pragma unroll
+        for (int nd = 0; nd < ND; ++nd)
+          *reinterpret_cast<uint32_t*>(a.att + row * HD + 8 * nd + 2 * t) =
+              none ? 0u : pack_bf16x2(__fmul_rn(o[nd][2 * rr], inv), __fmul_rn(o[nd][2 * rr + 1], inv));
+        if (t == 0) a.lse[row] = none ? INFINITY : m_run[rr] + __log2f(l_run[rr]);
+      } else {
+        float* to = a.part_o + (static_cast<long long>(cut) * f.rows_cap + x) * HD;
+#pragma unroll
+        for (int nd = 0; nd < ND; ++nd) *reinterpret_cast<float2*>(to + 8 * nd + 2 * t) = make_float2(o[nd][2 * rr], o[nd][2 * rr + 1]);
+        if (t == 0) a.part_ml[static_cast<long long>(cut) * f.rows_cap + x] = make_float2(m_run[rr], l_run[rr]);
+      }
+    }
+    left -= u1 - u0;
+    u0 = 0;
+    if (left > 0 && ++h == a.c.n_kv) {
+      h = 0;
+      while (++s + 1 < a.c.n_seq && af_units(a, s, q) == 0) {}
+    }
+  }
+  if (!ok) {
+    // failure path only: a copy that did not arrive in time may still be in flight
+    if (lane == 0) report_timeout(AF_WAIT_LOAD);
+    const long long t0 = clock64();
+    while (clock64() - t0 < 2000000LL) {}
+  }
+}
+
+// The runs again, without the keys: joins the items that were cut (in run order) and adds every slot's weights, p = 2^(score
+// - lse), to mass.  A warp takes the slots of its run; of the results of a cut item it joins its share, 8 dimensions of a
+// row at a time.
+template <int HD, int SR>
+__global__ void __launch_bounds__(AF_THREADS) attn_few_join_kernel(const __grid_constant__ AfArgs f) {
+  pdl_enter();
+  const AcArgs& a = f.a;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  __shared__ float lse_s[AF_WARPS][AF_ROWS], max_s[AF_WARPS][AF_ROWS], inv_s[AF_WARPS][AF_ROWS];
+  const int r = warp * gridDim.x + blockIdx.x;
+  const AfRun run = f.run[r];
+  const AfHead head = *f.head;
+  int left = run.left, s = run.s, h = run.h, u0 = run.u;
+  long long at = left > 0 ? af_start(head, r) : 0;  // place in the list
+  KvSeq q;
+  while (left > 0) {
+    const int units = af_units(a, s, q);
+    const int u1 = min(units, u0 + left), end = q.used + q.m, rows = q.m * a.rep;
+    const bool whole = u0 == 0 && u1 == units;
+    const uint32_t* anc = a.b.parent ? a.anc + static_cast<long long>(q.t0) * AC_TREE_WORDS : nullptr;
+    auto row_at = [&](int x) { return static_cast<long long>(q.t0 + x / a.rep) * a.n_heads + h * a.rep + x % a.rep; };
+    if (whole) {
+      if (lane < AF_ROWS) lse_s[warp][lane] = lane < rows ? a.lse[row_at(lane)] : INFINITY;
+      __syncwarp();
+    } else {
+      const int ra = af_run_of(head, at - u0), rb = af_run_of(head, at - u0 + units - 1), n = rb - ra + 1, me = r - ra;
+      auto part = [&](int k) { return static_cast<long long>(2 * (ra + k) + (k == 0 ? 1 : 0)) * f.rows_cap; };
+      for (int x = 0; x < AF_ROWS; ++x) {
+        float m = -INFINITY, l = 0.0f;
+        if (x < rows) {
+          for (int k = lane; k < n; k += 32) m = fmaxf(m, a.part_ml[part(k) + x].x);
+          m = warp_max(m);
+          for (int k = lane; k < n; k += 32) {
+            const float2 ml = a.part_ml[part(k) + x];
+            if (ml.x != -INFINITY) l = fmaf(ml.y, ac_exp2(ml.x - m), l);
+          }
+          l = warp_sum(l);
+        }
+        const bool none = x >= rows || l == 0.0f || ac_is_pad(anc, x / a.rep);
+        if (lane == 0) {
+          lse_s[warp][x] = none ? INFINITY : m + __log2f(l);
+          max_s[warp][x] = m;
+          inv_s[warp][x] = none ? 0.0f : __fdiv_rn(1.0f, l);
+        }
+      }
+      __syncwarp();
+      // results: pieces of 8 dimensions, piece i to the (i mod n)-th run of the item; lanes: 4 parts side by side x 8 dimensions
+      const int k0 = lane >> 3, d = lane & 7;
+      for (int i = me; i < rows * (HD / 8); i += n) {
+        const int x = i / (HD / 8), dim = (i - x * (HD / 8)) * 8 + d;
+        const float m = max_s[warp][x];
+        float acc = 0.0f;
+        for (int k = k0; k < n; k += 4) {
+          const float mk = a.part_ml[part(k) + x].x;
+          if (mk != -INFINITY) acc = fmaf(a.part_o[(part(k) + x) * HD + dim], ac_exp2(mk - m), acc);
+        }
+        acc += __shfl_xor_sync(0xffffffffu, acc, 8);
+        acc += __shfl_xor_sync(0xffffffffu, acc, 16);
+        const float v = lse_s[warp][x] == INFINITY ? 0.0f : __fmul_rn(acc, inv_s[warp][x]);
+        const float w = __shfl_down_sync(0xffffffffu, v, 1);
+        if (k0 == 0 && (d & 1) == 0) *reinterpret_cast<uint32_t*>(a.att + row_at(x) * HD + dim) = pack_bf16x2(v, w);
+      }
+    }
+    if (f.scores) {
+      float lse[SR];
+#pragma unroll
+      for (int x = 0; x < SR; ++x) lse[x] = lse_s[warp][x];
+      const int slot1 = min(end, u1 * AF_SLOTS);
+#pragma unroll 4
+      for (int slot = u0 * AF_SLOTS + lane; slot < slot1; slot += 32) {
+        const int page = kv_page(a.c, s, slot);
+        if (page < 0) continue;
+        const long long row = kv_row(a.c, 0, page, h) + (slot & ((1 << a.c.page_shift) - 1));
+        const float4* sc = reinterpret_cast<const float4*>(f.scores + row * SR);
+        float got = 0.0f;
+#pragma unroll
+        for (int x = 0; x < SR; x += 4) {
+          const float4 v = sc[x / 4];
+          const float vv[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+          for (int e = 0; e < 4; ++e) got += lse[x + e] == INFINITY ? 0.0f : ac_exp2(vv[e] - lse[x + e]);
+        }
+        a.c.mass[row] += got;
+      }
+    }
+    __syncwarp();
+    left -= u1 - u0;
+    at += u1 - u0;
+    u0 = 0;
+    if (left > 0 && ++h == a.c.n_kv) {
+      h = 0;
+      while (++s + 1 < a.c.n_seq && af_units(a, s, q) == 0) {}
     }
   }
 }

@@ -940,20 +940,17 @@ __global__ void __launch_bounds__(AM_KEYS) attn_mass_join_kernel(const __grid_co
 }
 
 // ---- host --------------------------------------------------------------------------------------------------------------
-constexpr int AC_FEW_ROWS = AR_ROWS;  // at most so many rows per sequence and kv head take the few-rows kernel
-
 struct AcPlan {
-  bool few;                                // few rows: attn_rows_kernel; else tiles
-  int row_tiles, splits, split_keys;       // few rows
-  int tok_tile, nx, rows_cap, ctas;        // tiles
-  size_t lse_bytes, ml_bytes, o_bytes, cut_bytes, sum_bytes, anc_bytes, ok_bytes;
-  size_t bytes() const { return lse_bytes + ml_bytes + o_bytes + cut_bytes + sum_bytes + 2 * anc_bytes + ok_bytes; }
-  // Does every grid and every coordinate of the call fit?
+  bool few;                                    // few rows: attn_few_kernel; else tiles
+  int rows_cap;                                // rows kept of a cut item
+  int score_rows, runs;                        // few rows
+  int tok_tile, nx, ctas;                      // tiles
+  size_t lse_bytes, ml_bytes, o_bytes, cut_bytes, sum_bytes, score_bytes, anc_bytes, ok_bytes, run_bytes;
+  size_t bytes() const { return lse_bytes + ml_bytes + o_bytes + cut_bytes + sum_bytes + score_bytes + 2 * anc_bytes + ok_bytes + run_bytes; }
+  // Does every coordinate of the call fit?
   bool launchable(const KvView& c) const {
-    const long long heads = static_cast<long long>(c.n_seq) * c.n_kv;
-    const long long key_tiles = ((c.max_pages << c.page_shift) + AS_KEYS - 1) / AS_KEYS;
-    return heads * row_tiles <= INT_MAX / splits && heads <= INT_MAX / key_tiles &&
-           (static_cast<long long>(c.n_pages) * c.n_kv + 1) << c.page_shift <= INT_MAX;
+    return (static_cast<long long>(c.n_pages) * c.n_kv + 1) << c.page_shift <= INT_MAX &&
+           static_cast<long long>(c.n_seq) * ((static_cast<long long>(c.max_pages) << c.page_shift) / AF_SLOTS + 1) * c.n_kv <= INT_MAX;
   }
 };
 
@@ -964,22 +961,18 @@ inline AcPlan ac_plan(const KvView& c, int T, int max_new, int n_heads) {
   AcPlan p = {};
   const int rep = n_heads / c.n_kv;
   const long long rows = static_cast<long long>(max_new) * rep;
-  p.few = rows <= AC_FEW_ROWS;
-  p.row_tiles = p.splits = 1;
+  p.few = rows <= AF_ROWS;
   p.lse_bytes = ac_up(static_cast<size_t>(T) * n_heads * 4);
   p.anc_bytes = max_new <= BITRL_TREE_MAX_TOKENS ? ac_up(static_cast<size_t>(T) * AC_TREE_WORDS * 4) : 0;  // twice
   p.ok_bytes = ac_up(static_cast<size_t>(c.n_seq) * 4);
   if (p.few) {
-    // ranges of keys are made so that even one row tile per (sequence, kv head) fills the SMs several times over
-    const long long items = static_cast<long long>(c.n_seq) * c.n_kv;
-    const int room = c.max_pages << c.page_shift;
-    const long long most = (room + 255) / 256;  // no range below 256 slots
-    long long splits = (148LL * 8 + items - 1) / items;
-    if (splits > most) splits = most;
-    p.split_keys = static_cast<int>(((room + splits - 1) / splits + 63) / 64 * 64);
-    p.splits = (room + p.split_keys - 1) / p.split_keys;
-    p.ml_bytes = p.splits > 1 ? ac_up(static_cast<size_t>(p.splits) * T * n_heads * 8) : 0;
-    p.o_bytes = p.splits > 1 ? ac_up(static_cast<size_t>(p.splits) * T * n_heads * c.hd * 4) : 0;
+    p.rows_cap = static_cast<int>(rows);
+    p.score_rows = rows <= 4 ? 4 : rows <= 8 ? 8 : 16;
+    p.runs = sm_count() * AF_WARPS;
+    p.ml_bytes = ac_up(static_cast<size_t>(2 * p.runs) * p.rows_cap * 8);
+    p.o_bytes = ac_up(static_cast<size_t>(2 * p.runs) * p.rows_cap * c.hd * 4);
+    p.run_bytes = 256 + ac_up(static_cast<size_t>(p.runs) * sizeof(AfRun));
+    p.score_bytes = c.mass ? ac_up((static_cast<size_t>(c.n_pages) * c.n_kv << c.page_shift) * p.score_rows * 4) : 0;
   } else {
     p.tok_tile = 128 / rep;
     p.nx = (max_new + 2 * p.tok_tile - 1) / (2 * p.tok_tile);
@@ -1017,37 +1010,29 @@ inline bitrl_status ac_tensor_map(CUtensorMap* m, const void* p, int dims, const
 }
 
 template <int HD>
-bitrl_status launch_attention_cached_hd(const AcArgs& a, const AcPlan& p, bool mass, float* sums, cudaStream_t st) {
+bitrl_status launch_attention_cached_hd(const AcArgs& a, const AcPlan& p, bool mass, float* sums, const AfArgs& f, cudaStream_t st) {
   bitrl_status s;
+  CUtensorMap mk, mv;
+  const int page = 1 << a.c.page_shift;
+  const cuuint64_t kv_size[2] = {HD, static_cast<cuuint64_t>(a.c.n_pages) * a.c.n_kv * page}, kv_stride[1] = {HD * 2};
+  const cuuint32_t kv_box[2] = {64, static_cast<cuuint32_t>(p.few ? AF_SLOTS : page)};
+  if ((s = ac_tensor_map(&mk, a.c.k, 2, kv_size, kv_stride, kv_box)) != BITRL_OK) return s;
+  if ((s = ac_tensor_map(&mv, a.c.v, 2, kv_size, kv_stride, kv_box)) != BITRL_OK) return s;
   if (p.few) {
     static bool done[64] = {false};
-    if ((s = ac_smem(attn_rows_kernel<HD>, ar_smem_bytes<HD>(), done)) != BITRL_OK) return s;
-    BITRL_CUDA(launch_pdl(attn_rows_kernel<HD>, dim3(static_cast<unsigned>(static_cast<long long>(a.c.n_seq) * a.c.n_kv * p.splits)),
-                          dim3(AR_THREADS), ar_smem_bytes<HD>(), st, a));
-    count_launch(1);
-    if (p.splits > 1) {
-      const unsigned per_seq = static_cast<unsigned>((static_cast<long long>(a.b.max_new) * a.n_heads + 3) / 4);
-      BITRL_CUDA(launch_pdl(attn_join_kernel<HD>, dim3(per_seq * a.c.n_seq), dim3(128), 0, st, a));
-      count_launch(1);
-    }
-    if (mass) {
-      static bool mass_done[64] = {false};
-      if ((s = ac_smem(attn_mass_few_kernel<HD>, as_smem_bytes<HD>(), mass_done)) != BITRL_OK) return s;
-      const unsigned tiles = static_cast<unsigned>(((a.c.max_pages << a.c.page_shift) + AS_KEYS - 1) / AS_KEYS);
-      BITRL_CUDA(launch_pdl(attn_mass_few_kernel<HD>, dim3(tiles * a.c.n_kv * a.c.n_seq), dim3(AS_THREADS), as_smem_bytes<HD>(), st, a));
-      count_launch(1);
-    }
+    if ((s = ac_smem(attn_few_kernel<HD>, af_smem_bytes<HD>(), done)) != BITRL_OK) return s;
+    const dim3 grid(p.runs / AF_WARPS);
+    BITRL_CUDA(launch_pdl(attn_few_kernel<HD>, grid, dim3(AF_THREADS), af_smem_bytes<HD>(), st, mk, mv, f));
+    BITRL_CUDA(p.score_rows == 4   ? launch_pdl(attn_few_join_kernel<HD, 4>, grid, dim3(AF_THREADS), 0, st, f)
+               : p.score_rows == 8 ? launch_pdl(attn_few_join_kernel<HD, 8>, grid, dim3(AF_THREADS), 0, st, f)
+                                   : launch_pdl(attn_few_join_kernel<HD, 16>, grid, dim3(AF_THREADS), 0, st, f));
+    count_launch(2);
   } else {
-    CUtensorMap mq, mk, mv;
-    const int page = 1 << a.c.page_shift;
-    const cuuint64_t kv_size[2] = {HD, static_cast<cuuint64_t>(a.c.n_pages) * a.c.n_kv * page}, kv_stride[1] = {HD * 2};
-    const cuuint32_t kv_box[2] = {64, static_cast<cuuint32_t>(page)};
+    CUtensorMap mq;
     const cuuint64_t q_size[3] = {HD, static_cast<cuuint64_t>(a.n_heads), static_cast<cuuint64_t>(a.b.T)};
     const cuuint64_t q_stride[2] = {HD * 2, static_cast<cuuint64_t>(a.n_heads) * HD * 2};
     const cuuint32_t q_box[3] = {64, static_cast<cuuint32_t>(a.rep), static_cast<cuuint32_t>(p.tok_tile)};
     if ((s = ac_tensor_map(&mq, a.q, 3, q_size, q_stride, q_box)) != BITRL_OK) return s;
-    if ((s = ac_tensor_map(&mk, a.c.k, 2, kv_size, kv_stride, kv_box)) != BITRL_OK) return s;
-    if ((s = ac_tensor_map(&mv, a.c.v, 2, kv_size, kv_stride, kv_box)) != BITRL_OK) return s;
     static bool done[64] = {false};
     if ((s = ac_smem(attn_tiles_kernel<HD>, AtSmem<HD>::LAUNCH, done)) != BITRL_OK) return s;
     const AtArgs t{a, p.tok_tile, p.nx, p.rows_cap};
@@ -1083,25 +1068,26 @@ bitrl_status launch_attention_cached(const KvView& c, const KvBatch& b, const vo
   a.n_heads = n_heads;
   a.rep = n_heads / c.n_kv;
   a.scale2 = static_cast<float>(1.4426950408889634 / sqrt(static_cast<double>(c.hd)));
-  a.row_tiles = p.row_tiles;
-  a.splits = p.splits;
-  a.split_keys = p.split_keys;
   a.lse = reinterpret_cast<float*>(take(p.lse_bytes));
   a.part_ml = reinterpret_cast<float2*>(take(p.ml_bytes));
   a.part_o = reinterpret_cast<float*>(take(p.o_bytes));
   a.cuts = reinterpret_cast<AtCut*>(take(p.cut_bytes));
   float* sums = reinterpret_cast<float*>(take(p.sum_bytes));
+  float* scores = reinterpret_cast<float*>(take(p.score_bytes));
+  unsigned char* runs = take(p.run_bytes);
   uint32_t* anc = reinterpret_cast<uint32_t*>(take(p.anc_bytes));
   uint32_t* desc = reinterpret_cast<uint32_t*>(take(p.anc_bytes));
   int* ok = reinterpret_cast<int*>(take(p.ok_bytes));
   a.anc = b.parent ? anc : nullptr;
   a.desc = b.parent ? desc : nullptr;
   a.tree_ok = b.parent ? ok : nullptr;
+  const AfArgs f{a, p.rows_cap, p.score_rows, p.runs, mass ? scores : nullptr, reinterpret_cast<AfHead*>(runs),
+                 reinterpret_cast<AfRun*>(runs + 256)};
   if (b.parent) {
     BITRL_CUDA(launch_pdl(attn_tree_kernel, dim3(c.n_seq), dim3(BITRL_TREE_MAX_TOKENS), 0, st, c, b, anc, desc, ok));
     count_launch(1);
   }
-  return c.hd == 128 ? launch_attention_cached_hd<128>(a, p, mass, sums, st) : launch_attention_cached_hd<64>(a, p, mass, sums, st);
+  return c.hd == 128 ? launch_attention_cached_hd<128>(a, p, mass, sums, f, st) : launch_attention_cached_hd<64>(a, p, mass, sums, f, st);
 }
 
 }  // namespace bitrl
