@@ -108,15 +108,15 @@ constexpr int AF_THREADS = 32 * AF_WARPS;
 constexpr int AF_STAGES = 3;
 constexpr int AF_ROWS = 16;
 constexpr int AF_SLOTS = 16;   // slots of a unit
-constexpr int AF_MIN_RUN = 2;  // units of a run at least (short lists use fewer warps)
+constexpr int AF_MIN_RUN = 4;  // units of a run at least (short lists use fewer warps)
 enum { AF_WAIT_LOAD = 151 };
 
 struct AfRun {
   int s, h, u, left;  // first unit (unit u of item (s, h)) and number of units
 };
 struct AfHead {
-  long long units;  // of the whole list
-  int runs;         // in use
+  int units, runs;  // of the whole list; runs in use
+  int per, more;    // units of a run; the first `more` runs have one more
 };
 
 struct AfArgs {
@@ -130,13 +130,11 @@ struct AfArgs {
 };
 
 // First unit of run r.
-__device__ __forceinline__ long long af_start(const AfHead& h, int r) { return h.units * r / h.runs; }
+__device__ __forceinline__ int af_start(const AfHead& h, int r) { return r * h.per + min(r, h.more); }
 // The run that holds unit g.
-__device__ __forceinline__ int af_run_of(const AfHead& h, long long g) {
-  int r = static_cast<int>(g * h.runs / h.units);
-  while (r + 1 < h.runs && af_start(h, r + 1) <= g) ++r;
-  while (r > 0 && af_start(h, r) > g) --r;
-  return r;
+__device__ __forceinline__ int af_run_of(const AfHead& h, int g) {
+  const int longer = h.more * (h.per + 1);
+  return g < longer ? g / (h.per + 1) : h.more + (g - longer) / h.per;
 }
 // Units of one kv head of sequence s.
 __device__ __forceinline__ int af_units(const AcArgs& a, int s, KvSeq& q) {
@@ -156,7 +154,7 @@ attn_few_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constan
   constexpr uint32_t HALF = AF_SLOTS * 128, TILE = NH * HALF;  // a 64-dimension block of the keys (or values) of a unit
   extern __shared__ unsigned char af_smem_raw[];
   __shared__ __align__(8) unsigned long long bars[AF_WARPS * AF_STAGES];
-  __shared__ long long part[AF_WARPS], first_of[AF_THREADS + 1];
+  __shared__ int part[AF_WARPS], first_of[AF_THREADS + 1];
   const AcArgs& a = f.a;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3, lm = lane >> 3, lr = lane & 7;
   const uint32_t bar = ptx::smem_u32(bars + warp * AF_STAGES);
@@ -171,13 +169,13 @@ attn_few_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constan
   // ---- this warp's run: units before every block of sequences, then a search
   KvSeq q;
   const int per = (a.c.n_seq + AF_THREADS - 1) / AF_THREADS, sb = min(a.c.n_seq, per * static_cast<int>(threadIdx.x));
-  long long sum = 0;
+  int sum = 0;
   for (int s = sb; s < min(a.c.n_seq, sb + per); ++s) sum += af_units(a, s, q);
   sum *= a.c.n_kv;
-  long long incl = sum;
+  int incl = sum;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
-    const long long v = __shfl_up_sync(0xffffffffu, incl, o);
+    const int v = __shfl_up_sync(0xffffffffu, incl, o);
     if (lane >= o) incl += v;
   }
   if (lane == 31) part[warp] = incl;
@@ -187,8 +185,10 @@ attn_few_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constan
   if (threadIdx.x == 0) first_of[0] = 0;
   __syncthreads();
   AfHead head;
-  head.units = first_of[AF_THREADS];
-  head.runs = static_cast<int>(min(static_cast<long long>(f.max_runs), (head.units + AF_MIN_RUN - 1) / AF_MIN_RUN));
+  head.units = static_cast<int>(first_of[AF_THREADS]);
+  head.runs = min(f.max_runs, (head.units + AF_MIN_RUN - 1) / AF_MIN_RUN);
+  head.per = head.runs > 0 ? head.units / head.runs : 0;
+  head.more = head.units - head.per * head.runs;
   // neighbouring runs go to different CTAs, so that a short list spreads over all SMs
   const int r = warp * gridDim.x + blockIdx.x;
   if (blockIdx.x == 0 && threadIdx.x == 0) *f.head = head;
@@ -196,22 +196,22 @@ attn_few_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constan
     if (lane == 0) f.run[r].left = 0;
     return;
   }
-  const long long w0 = af_start(head, r);
-  int left = static_cast<int>(af_start(head, r + 1) - w0), s = 0, h = 0, u0 = 0;
+  const int w0 = af_start(head, r);
+  int left = af_start(head, r + 1) - w0, s = 0, h = 0, u0 = 0;
   {
     int block = 0;  // the last block that begins at or before w0: blocks without units do not count
     for (int i = lane; i < AF_THREADS; i += 32)
       if (first_of[i] <= w0 && w0 < first_of[i + 1]) block = i;
     block = __reduce_max_sync(0xffffffffu, block);
-    long long rem = w0 - first_of[block];
+    int rem = w0 - first_of[block];
     for (s = block * per;; ++s) {
-      const long long n = static_cast<long long>(af_units(a, s, q)) * a.c.n_kv;
+      const int n = af_units(a, s, q) * a.c.n_kv;
       if (rem < n || s + 1 >= a.c.n_seq) break;
       rem -= n;
     }
     const int n = af_units(a, s, q);
-    h = static_cast<int>(rem / n);
-    u0 = static_cast<int>(rem % n);
+    h = rem / n;
+    u0 = rem % n;
   }
   if (lane == 0) f.run[r] = AfRun{s, h, u0, left};
 
@@ -458,19 +458,30 @@ attn_few_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constan
 }
 
 // The runs again, without the keys: joins the items that were cut (in run order) and adds every slot's weights, p = 2^(score
-// - lse), to mass.  A warp takes the slots of its run; of the results of a cut item it joins its share, 8 dimensions of a
-// row at a time.
+// - lse), to mass.  The AJ_SPLIT warps of a run take its slots in turn, and of the results of a cut item each joins its share,
+// 8 dimensions of a row at a time.  Everything here is short chains of loads, so several are kept in flight: four rows of
+// statistics, four parts of a result, four slots per lane.
+constexpr int AJ_SPLIT = 4;
+
+// (maximum, sum) of two disjoint sets of keys.
+__device__ __forceinline__ float2 aj_merge(float2 x, float2 y) {
+  const float m = fmaxf(x.x, y.x);
+  const float lx = x.x == -INFINITY ? 0.0f : __fmul_rn(x.y, ac_exp2(x.x - m)), ly = y.x == -INFINITY ? 0.0f : __fmul_rn(y.y, ac_exp2(y.x - m));
+  return make_float2(m, lx + ly);
+}
+
 template <int HD, int SR>
 __global__ void __launch_bounds__(AF_THREADS) attn_few_join_kernel(const __grid_constant__ AfArgs f) {
   pdl_enter();
   const AcArgs& a = f.a;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, sub = blockIdx.y;
   __shared__ float lse_s[AF_WARPS][AF_ROWS], max_s[AF_WARPS][AF_ROWS], inv_s[AF_WARPS][AF_ROWS];
   const int r = warp * gridDim.x + blockIdx.x;
   const AfRun run = f.run[r];
   const AfHead head = *f.head;
   int left = run.left, s = run.s, h = run.h, u0 = run.u;
-  long long at = left > 0 ? af_start(head, r) : 0;  // place in the list
+  int at = left > 0 ? af_start(head, r) : 0;  // place in the list
+  const int slot_mask = (1 << a.c.page_shift) - 1;
   KvSeq q;
   while (left > 0) {
     const int units = af_units(a, s, q);
@@ -484,40 +495,68 @@ __global__ void __launch_bounds__(AF_THREADS) attn_few_join_kernel(const __grid_
     } else {
       const int ra = af_run_of(head, at - u0), rb = af_run_of(head, at - u0 + units - 1), n = rb - ra + 1, me = r - ra;
       auto part = [&](int k) { return static_cast<long long>(2 * (ra + k) + (k == 0 ? 1 : 0)) * f.rows_cap; };
-      for (int x = 0; x < AF_ROWS; ++x) {
-        float m = -INFINITY, l = 0.0f;
-        if (x < rows) {
-          for (int k = lane; k < n; k += 32) m = fmaxf(m, a.part_ml[part(k) + x].x);
-          m = warp_max(m);
+      for (int x0 = 0; x0 < AF_ROWS; x0 += 4) {
+        float2 ml[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) ml[i] = make_float2(-INFINITY, 0.0f);
+        if (x0 < rows) {
           for (int k = lane; k < n; k += 32) {
-            const float2 ml = a.part_ml[part(k) + x];
-            if (ml.x != -INFINITY) l = fmaf(ml.y, ac_exp2(ml.x - m), l);
+            float2 v[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[i] = x0 + i < rows ? a.part_ml[part(k) + x0 + i] : make_float2(-INFINITY, 0.0f);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) ml[i] = aj_merge(ml[i], v[i]);
           }
-          l = warp_sum(l);
+#pragma unroll
+          for (int o = 16; o > 0; o >>= 1)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              ml[i] = aj_merge(ml[i], make_float2(__shfl_xor_sync(0xffffffffu, ml[i].x, o), __shfl_xor_sync(0xffffffffu, ml[i].y, o)));
         }
-        const bool none = x >= rows || l == 0.0f || ac_is_pad(anc, x / a.rep);
-        if (lane == 0) {
-          lse_s[warp][x] = none ? INFINITY : m + __log2f(l);
-          max_s[warp][x] = m;
-          inv_s[warp][x] = none ? 0.0f : __fdiv_rn(1.0f, l);
+        if (lane < 4) {
+          const float2 v = lane == 0 ? ml[0] : lane == 1 ? ml[1] : lane == 2 ? ml[2] : ml[3];
+          const int x = x0 + lane;
+          const bool none = x >= rows || v.y == 0.0f || ac_is_pad(anc, x / a.rep);
+          lse_s[warp][x] = none ? INFINITY : v.x + __log2f(v.y);
+          max_s[warp][x] = v.x;
+          inv_s[warp][x] = none ? 0.0f : __fdiv_rn(1.0f, v.y);
         }
       }
       __syncwarp();
-      // results: pieces of 8 dimensions, piece i to the (i mod n)-th run of the item; lanes: 4 parts side by side x 8 dimensions
-      const int k0 = lane >> 3, d = lane & 7;
-      for (int i = me; i < rows * (HD / 8); i += n) {
-        const int x = i / (HD / 8), dim = (i - x * (HD / 8)) * 8 + d;
-        const float m = max_s[warp][x];
-        float acc = 0.0f;
-        for (int k = k0; k < n; k += 4) {
-          const float mk = a.part_ml[part(k) + x].x;
-          if (mk != -INFINITY) acc = fmaf(a.part_o[(part(k) + x) * HD + dim], ac_exp2(mk - m), acc);
+      // results: pieces of 8 dimensions, dealt to the warps of the item in turn; lanes: 4 parts side by side x 8 dimensions.
+      // Eight loads of a lane are under way together: parts of one piece, or pieces where an item has few parts.
+      const int k0 = lane >> 3, d = lane & 7, pieces = rows * (HD / 8), step = n * AJ_SPLIT;
+      const int kn = n > 4 ? 8 : 1, pn = n > 4 ? 1 : 8;
+      for (int i0 = me * AJ_SPLIT + sub; i0 < pieces; i0 += pn * step) {
+        float acc[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) acc[j] = 0.0f;
+        for (int kb = k0; kb < n; kb += 4 * kn) {
+          float v[8], m[8];
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            const int i = kn == 8 ? i0 : i0 + j * step, k = kn == 8 ? kb + 4 * j : kb, x = i / (HD / 8);
+            const bool have = i < pieces && k < n;
+            v[j] = have ? a.part_o[(part(k) + x) * HD + (i - x * (HD / 8)) * 8 + d] : 0.0f;
+            m[j] = have ? a.part_ml[part(k) + x].x - max_s[warp][x] : -INFINITY;
+          }
+#pragma unroll
+          for (int j = 0; j < 8; ++j)
+            if (m[j] > -INFINITY || m[j] != m[j]) acc[j] = fmaf(v[j], ac_exp2(m[j]), acc[j]);
         }
-        acc += __shfl_xor_sync(0xffffffffu, acc, 8);
-        acc += __shfl_xor_sync(0xffffffffu, acc, 16);
-        const float v = lse_s[warp][x] == INFINITY ? 0.0f : __fmul_rn(acc, inv_s[warp][x]);
-        const float w = __shfl_down_sync(0xffffffffu, v, 1);
-        if (k0 == 0 && (d & 1) == 0) *reinterpret_cast<uint32_t*>(a.att + row_at(x) * HD + dim) = pack_bf16x2(v, w);
+        if (kn == 8) acc[0] = ((acc[0] + acc[1]) + (acc[2] + acc[3])) + ((acc[4] + acc[5]) + (acc[6] + acc[7]));
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          if (j >= pn) break;
+          acc[j] += __shfl_xor_sync(0xffffffffu, acc[j], 8);
+          acc[j] += __shfl_xor_sync(0xffffffffu, acc[j], 16);
+          const int i = i0 + j * step, x = i / (HD / 8);
+          const bool none = i >= pieces || lse_s[warp][x & (AF_ROWS - 1)] == INFINITY;
+          const float v = none ? 0.0f : __fmul_rn(acc[j], inv_s[warp][x]);
+          const float w = __shfl_down_sync(0xffffffffu, v, 1);
+          if (i < pieces && k0 == 0 && (d & 1) == 0)
+            *reinterpret_cast<uint32_t*>(a.att + row_at(x) * HD + (i - x * (HD / 8)) * 8 + d) = pack_bf16x2(v, w);
+        }
       }
     }
     if (f.scores) {
@@ -525,21 +564,36 @@ __global__ void __launch_bounds__(AF_THREADS) attn_few_join_kernel(const __grid_
 #pragma unroll
       for (int x = 0; x < SR; ++x) lse[x] = lse_s[warp][x];
       const int slot1 = min(end, u1 * AF_SLOTS);
-#pragma unroll 4
-      for (int slot = u0 * AF_SLOTS + lane; slot < slot1; slot += 32) {
-        const int page = kv_page(a.c, s, slot);
-        if (page < 0) continue;
-        const long long row = kv_row(a.c, 0, page, h) + (slot & ((1 << a.c.page_shift) - 1));
-        const float4* sc = reinterpret_cast<const float4*>(f.scores + row * SR);
-        float got = 0.0f;
+      const int* pages = a.c.page_table + static_cast<long long>(s) * a.c.max_pages;
+      for (int base = u0 * AF_SLOTS + 128 * sub + lane; base < slot1; base += 128 * AJ_SPLIT) {
+        int page[4];
+        long long row[4];
+        float4 sc[4][SR / 4];
+        float old[4];
 #pragma unroll
-        for (int x = 0; x < SR; x += 4) {
-          const float4 v = sc[x / 4];
-          const float vv[4] = {v.x, v.y, v.z, v.w};
+        for (int i = 0; i < 4; ++i) page[i] = base + 32 * i < slot1 ? pages[(base + 32 * i) >> a.c.page_shift] : -1;
 #pragma unroll
-          for (int e = 0; e < 4; ++e) got += lse[x + e] == INFINITY ? 0.0f : ac_exp2(vv[e] - lse[x + e]);
+        for (int i = 0; i < 4; ++i) {
+          if (page[i] >= a.c.n_pages) page[i] = -1;  // reported by the kernel that read the keys
+          row[i] = page[i] < 0 ? 0 : kv_row(a.c, 0, page[i], h) + ((base + 32 * i) & slot_mask);
+          if (page[i] >= 0) {
+            old[i] = a.c.mass[row[i]];
+#pragma unroll
+            for (int x = 0; x < SR / 4; ++x) sc[i][x] = reinterpret_cast<const float4*>(f.scores + row[i] * SR)[x];
+          }
         }
-        a.c.mass[row] += got;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          if (page[i] < 0) continue;
+          float got = 0.0f;
+#pragma unroll
+          for (int x = 0; x < SR / 4; ++x) {
+            const float v[4] = {sc[i][x].x, sc[i][x].y, sc[i][x].z, sc[i][x].w};
+#pragma unroll
+            for (int e = 0; e < 4; ++e) got += lse[4 * x + e] == INFINITY ? 0.0f : ac_exp2(v[e] - lse[4 * x + e]);
+          }
+          a.c.mass[row[i]] = old[i] + got;
+        }
       }
     }
     __syncwarp();

@@ -1023,9 +1023,9 @@ bitrl_status launch_attention_cached_hd(const AcArgs& a, const AcPlan& p, bool m
     if ((s = ac_smem(attn_few_kernel<HD>, af_smem_bytes<HD>(), done)) != BITRL_OK) return s;
     const dim3 grid(p.runs / AF_WARPS);
     BITRL_CUDA(launch_pdl(attn_few_kernel<HD>, grid, dim3(AF_THREADS), af_smem_bytes<HD>(), st, mk, mv, f));
-    BITRL_CUDA(p.score_rows == 4   ? launch_pdl(attn_few_join_kernel<HD, 4>, grid, dim3(AF_THREADS), 0, st, f)
-               : p.score_rows == 8 ? launch_pdl(attn_few_join_kernel<HD, 8>, grid, dim3(AF_THREADS), 0, st, f)
-                                   : launch_pdl(attn_few_join_kernel<HD, 16>, grid, dim3(AF_THREADS), 0, st, f));
+    BITRL_CUDA(p.score_rows == 4   ? launch_pdl(attn_few_join_kernel<HD, 4>, dim3(grid.x, AJ_SPLIT), dim3(AF_THREADS), 0, st, f)
+               : p.score_rows == 8 ? launch_pdl(attn_few_join_kernel<HD, 8>, dim3(grid.x, AJ_SPLIT), dim3(AF_THREADS), 0, st, f)
+                                   : launch_pdl(attn_few_join_kernel<HD, 16>, dim3(grid.x, AJ_SPLIT), dim3(AF_THREADS), 0, st, f));
     count_launch(2);
   } else {
     CUtensorMap mq;
