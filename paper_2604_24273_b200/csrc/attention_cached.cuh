@@ -49,6 +49,12 @@ __device__ __forceinline__ void mma_bf16(float (&d)[4], const uint32_t (&a)[4], 
                : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
                : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
+// Transposes an 8 x 8 matrix of 16-bit elements held as lane 4 i + j: row i, columns 2 j and 2 j + 1.
+__device__ __forceinline__ uint32_t movmatrix_trans(uint32_t v) {
+  uint32_t r;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
+  return r;
+}
 // (x0, x1) -> bf16 pair (x0 in the low half)
 __device__ __forceinline__ uint32_t pack_bf16x2(float x0, float x1) {
   const __nv_bfloat162 p = __floats2bfloat162_rn(x0, x1);
@@ -101,19 +107,16 @@ __device__ __forceinline__ bool ac_is_pad(const uint32_t* anc, int tok) { return
 // (sequence, head) that it met.  Results of items that lie within one run are final; the others are joined by
 // attn_few_join_kernel, which also turns the scores that this kernel leaves behind (fp32, 4 to 64 bytes per slot beside
 // the 4 HD bytes of its key and value) into the weight of every slot, so that keys are read once.
-// Scores come from mma.sync (a 16-row tile fills its M; a tcgen05 tile has 128 rows).  The weights are split into two bf16
+// Scores come from mma.sync (eight rows fill its N; a tcgen05 tile has 128 rows).  The weights are split into two bf16
 // halves (16 significant bits), which costs nothing where reading bounds the kernel.
 constexpr int AF_WARPS = 8;
 constexpr int AF_THREADS = 32 * AF_WARPS;
 constexpr int AF_STAGES = 3;
 constexpr int AF_ROWS = 16;
 constexpr int AF_SLOTS = 16;   // slots of a unit
-constexpr int AF_MIN_RUN = 4;  // units of a run at least (short lists use fewer warps)
+constexpr int AF_MIN_RUN = 2;  // units of a run at least (short lists use fewer warps)
 enum { AF_WAIT_LOAD = 151 };
 
-struct AfRun {
-  int s, h, u, left;  // first unit (unit u of item (s, h)) and number of units
-};
 struct AfHead {
   int units, runs;  // of the whole list; runs in use
   int per, more;    // units of a run; the first `more` runs have one more
@@ -124,9 +127,10 @@ struct AfArgs {
   int rows_cap;    // rows of a sequence and head at most: max_new * rep
   int score_rows;  // rows_cap rounded up to 4, 8 or 16
   int max_runs;
+  int join_slots;  // slots of a CTA of the join
   float* scores;   // [pages][kv heads][page][score_rows] or nullptr: scores in base-two units, -inf where unseen
   AfHead* head;
-  AfRun* run;      // [max_runs]
+  int* item_at;    // [n_seq * n_kv] place of an item's first unit in the list
 };
 
 // First unit of run r.
@@ -147,13 +151,15 @@ constexpr uint32_t af_smem_bytes() {
   return AF_WARPS * AF_STAGES * 2 * AF_SLOTS * HD * 2 + 1024;
 }
 
-template <int HD>
+// NG: groups of eight rows.
+template <int HD, int NG>
 __global__ void __launch_bounds__(AF_THREADS, 1)
 attn_few_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constant__ CUtensorMap tmap_v, const __grid_constant__ AfArgs f) {
-  constexpr int KS = HD / 16, ND = HD / 8, NH = HD / 64;
+  constexpr int KS = HD / 16, MD = HD / 16, NH = HD / 64;
   constexpr uint32_t HALF = AF_SLOTS * 128, TILE = NH * HALF;  // a 64-dimension block of the keys (or values) of a unit
   extern __shared__ unsigned char af_smem_raw[];
   __shared__ __align__(8) unsigned long long bars[AF_WARPS * AF_STAGES];
+  __shared__ int row_s[AF_WARPS * AF_STAGES];  // pool row of the unit in each place of the rings
   __shared__ int part[AF_WARPS], first_of[AF_THREADS + 1];
   const AcArgs& a = f.a;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3, lm = lane >> 3, lr = lane & 7;
@@ -192,10 +198,7 @@ attn_few_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constan
   // neighbouring runs go to different CTAs, so that a short list spreads over all SMs
   const int r = warp * gridDim.x + blockIdx.x;
   if (blockIdx.x == 0 && threadIdx.x == 0) *f.head = head;
-  if (r >= head.runs) {
-    if (lane == 0) f.run[r].left = 0;
-    return;
-  }
+  if (r >= head.runs) return;
   const int w0 = af_start(head, r);
   int left = af_start(head, r + 1) - w0, s = 0, h = 0, u0 = 0;
   {
@@ -213,23 +216,27 @@ attn_few_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constan
     h = rem / n;
     u0 = rem % n;
   }
-  if (lane == 0) f.run[r] = AfRun{s, h, u0, left};
 
-  // ---- loads, ahead of the arithmetic: a position of their own in the list
+  // ---- loads, ahead of the arithmetic: a position of their own in the list; the page of the next unit is read one unit early
   const uint32_t raw = ptx::smem_u32(af_smem_raw), ring = ((raw + 1023u) & ~1023u) + warp * (AF_STAGES * 2 * TILE);
+  const uint32_t rows_at = ptx::smem_u32(row_s + warp * AF_STAGES);
   const int slot_mask = (1 << a.c.page_shift) - 1;
+  const int none_row = (a.c.n_pages * a.c.n_kv) << a.c.page_shift;  // behind the pool: such a copy fills with zeros
   int ls = s, lh = h, lu = u0, l_left = left;
   KvSeq lq = q;
   int l_units = af_units(a, ls, lq);
+  const int* l_pages = a.c.page_table + static_cast<long long>(ls) * a.c.max_pages;
+  int l_page = l_pages[(lu * AF_SLOTS) >> a.c.page_shift];
   auto load = [&](int stage) {
     if (l_left <= 0) return;
     if (lane == 0) {
-      const int slot0 = lu * AF_SLOTS;
-      const int page = kv_page(a.c, ls, slot0);
-      // a page that the table does not have: a row behind the pool, which fills with zeros
-      const int row = page < 0 ? a.c.n_pages * a.c.n_kv << a.c.page_shift
-                               : static_cast<int>(((page * a.c.n_kv + lh) << a.c.page_shift) + (slot0 & slot_mask));
+      int row = none_row;
+      if (l_page >= 0 && l_page < a.c.n_pages)
+        row = ((l_page * a.c.n_kv + lh) << a.c.page_shift) + ((lu * AF_SLOTS) & slot_mask);
+      else
+        report_status(BITRL_ERR_SHAPE, KV_STAGE_BAD_PAGE);
       const uint32_t dst = ring + stage * 2 * TILE;
+      ptx::sts32(rows_at + 4 * stage, row);
       ptx::mbar_arrive_expect_tx(bar + 8 * stage, 2 * TILE);
 #pragma unroll
       for (int i = 0; i < NH; ++i) {
@@ -237,15 +244,17 @@ attn_few_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constan
         ptx::tma_load_2d(dst + TILE + i * HALF, &tmap_v, 64 * i, row, bar + 8 * stage);
       }
     }
-    --l_left;
-    if (++lu == l_units && l_left > 0) {
+    if (--l_left <= 0) return;
+    if (++lu == l_units) {
       lu = 0;
       if (++lh == a.c.n_kv) {
         lh = 0;
         do l_units = af_units(a, ++ls, lq);
         while (l_units == 0 && ls + 1 < a.c.n_seq);
+        l_pages = a.c.page_table + static_cast<long long>(ls) * a.c.max_pages;
       }
     }
+    l_page = l_pages[(lu * AF_SLOTS) >> a.c.page_shift];
   };
   for (int i = 0; i < AF_STAGES; ++i) load(i);
   uint32_t stage = 0, phase = 0;
@@ -255,28 +264,37 @@ attn_few_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constan
     const int units = af_units(a, s, q);
     const int u1 = min(units, u0 + left), end = q.used + q.m, rows = q.m * a.rep;
     const uint32_t* anc = a.b.parent ? a.anc + static_cast<long long>(q.t0) * AC_TREE_WORDS : nullptr;
-    // queries of rows g and g + 8
-    uint32_t qa[KS][4];
-    int tok[2];
+    if (u0 == 0 && lane == 0) f.item_at[s * a.c.n_kv + h] = af_start(head, r + 1) - left;
+    // Products are transposed, slots (or dimensions) x rows: S^T = K Q^T, O^T = V^T P^T.  Eight rows fill the N of an
+    // instruction, where they would fill half of its M.  This lane: rows 8 n + 2 t and the next; slots g and g + 8.
+    uint32_t qb[NG][KS][2];
+    int tok[NG][2];
 #pragma unroll
-    for (int rr = 0; rr < 2; ++rr) {
-      const int x = g + 8 * rr;
+    for (int n = 0; n < NG; ++n) {
+      const int x = 8 * n + g;  // B operand: the lane's row is g
       const bool live = x < rows;
-      tok[rr] = live ? x / a.rep : 0;
+      const int tk = live ? x / a.rep : 0;
       const unsigned short* row =
-          a.q + (static_cast<long long>(q.t0 + tok[rr]) * a.n_heads + h * a.rep + (live ? x - tok[rr] * a.rep : 0)) * HD + 2 * t;
+          a.q + (static_cast<long long>(q.t0 + tk) * a.n_heads + h * a.rep + (live ? x - tk * a.rep : 0)) * HD + 2 * t;
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks) {
-        qa[ks][rr] = live ? *reinterpret_cast<const uint32_t*>(row + 16 * ks) : 0u;
-        qa[ks][2 + rr] = live ? *reinterpret_cast<const uint32_t*>(row + 16 * ks + 8) : 0u;
+        qb[n][ks][0] = live ? *reinterpret_cast<const uint32_t*>(row + 16 * ks) : 0u;
+        qb[n][ks][1] = live ? *reinterpret_cast<const uint32_t*>(row + 16 * ks + 8) : 0u;
       }
+#pragma unroll
+      for (int e = 0; e < 2; ++e) tok[n][e] = min(8 * n + 2 * t + e, rows - 1) / a.rep;
     }
-    float o[ND][4];
+    float o[NG][MD][4];
+    float m_run[NG][2], l_run[NG][2];
 #pragma unroll
-    for (int nd = 0; nd < ND; ++nd)
+    for (int n = 0; n < NG; ++n) {
 #pragma unroll
-      for (int e = 0; e < 4; ++e) o[nd][e] = 0.0f;
-    float m_run[2] = {-INFINITY, -INFINITY}, l_run[2] = {0.0f, 0.0f};
+      for (int d = 0; d < MD; ++d)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[n][d][e] = 0.0f;
+#pragma unroll
+      for (int e = 0; e < 2; ++e) { m_run[n][e] = -INFINITY; l_run[n][e] = 0.0f; }
+    }
 
     for (int u = u0; u < u1; ++u) {
       const int slot0 = u * AF_SLOTS;
@@ -285,75 +303,74 @@ attn_few_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constan
         break;
       }
       const uint32_t ks_addr = ring + stage * 2 * TILE, vs_addr = ks_addr + TILE;
-      float c[2][4];
+      float c[NG][4], c2[NG][4];  // two chains of products
 #pragma unroll
-      for (int nt = 0; nt < 2; ++nt)
+      for (int n = 0; n < NG; ++n)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) c[nt][e] = 0.0f;
+        for (int e = 0; e < 4; ++e) c[n][e] = c2[n][e] = 0.0f;
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks) {
-        const int key = 8 * (lm >> 1) + lr, ch = 2 * ks + (lm & 1);
-        uint32_t kb[4];
-        ldmatrix_x4(ks_addr + (ch >> 3) * HALF + key * 128 + (((ch ^ key) & 7) << 4), kb);
-        mma_bf16(c[0], qa[ks], kb[0], kb[1]);
-        mma_bf16(c[1], qa[ks], kb[2], kb[3]);
+        const int key = 8 * (lm & 1) + lr, ch = 2 * ks + (lm >> 1);
+        uint32_t ka[4];
+        ldmatrix_x4(ks_addr + (ch >> 3) * HALF + key * 128 + (((ch ^ key) & 7) << 4), ka);
+#pragma unroll
+        for (int n = 0; n < NG; ++n) mma_bf16(ks & 1 ? c2[n] : c[n], ka, qb[n][ks][0], qb[n][ks][1]);
       }
       // ---- scale, mask; slots below used are seen by every row
       const bool masked = slot0 + AF_SLOTS > q.used;
-      float mx[2] = {-INFINITY, -INFINITY};
 #pragma unroll
-      for (int nt = 0; nt < 2; ++nt)
+      for (int n = 0; n < NG; ++n)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          float v = __fmul_rn(c[nt][e], a.scale2);
+          c[n][e] = __fmul_rn(c[n][e] + c2[n][e], a.scale2);
           if (masked) {
-            const int slot = slot0 + 8 * nt + 2 * t + (e & 1);
-            const bool see = slot < end && (slot < q.used || ac_sees_new(anc, tok[e >> 1], slot - q.used));
-            v = see ? v : -INFINITY;
+            const int slot = slot0 + g + 8 * (e >> 1);
+            const bool see = slot < end && (slot < q.used || ac_sees_new(anc, tok[n][e & 1], slot - q.used));
+            c[n][e] = see ? c[n][e] : -INFINITY;
           }
-          c[nt][e] = v;
-          mx[e >> 1] = fmaxf(mx[e >> 1], v);
         }
       if (f.scores) {
-        const int page = kv_page(a.c, s, slot0);
-        if (page >= 0) {
-          float* at = f.scores + ((kv_row(a.c, 0, page, h) + (slot0 & slot_mask)) + 2 * t) * f.score_rows;
+        const int row = static_cast<int>(ptx::lds32(rows_at + 4 * stage));
+        if (row < none_row) {
+          float* to = f.scores + static_cast<long long>(row + g) * f.score_rows + 2 * t;
 #pragma unroll
-          for (int nt = 0; nt < 2; ++nt)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const int x = g + 8 * (e >> 1);
-              if (x < f.score_rows) at[(8 * nt + (e & 1)) * f.score_rows + x] = c[nt][e];
+          for (int n = 0; n < NG; ++n)
+            if (8 * n + 2 * t < f.score_rows) {
+              *reinterpret_cast<float2*>(to + 8 * n) = make_float2(c[n][0], c[n][1]);
+              *reinterpret_cast<float2*>(to + 8 * f.score_rows + 8 * n) = make_float2(c[n][2], c[n][3]);
             }
         }
       }
-      float alpha[2];
+      float alpha[NG][2];
+      bool moved = false;
 #pragma unroll
-      for (int rr = 0; rr < 2; ++rr) {
-        mx[rr] = fmaxf(mx[rr], __shfl_xor_sync(0xffffffffu, mx[rr], 1));
-        mx[rr] = fmaxf(mx[rr], __shfl_xor_sync(0xffffffffu, mx[rr], 2));
-        const float m_new = fmaxf(m_run[rr], mx[rr]);
-        alpha[rr] = m_new == m_run[rr] ? 1.0f : ac_exp2(m_run[rr] - m_new);
-        m_run[rr] = m_new;
-      }
-      float add[2] = {0.0f, 0.0f};
+      for (int n = 0; n < NG; ++n)
 #pragma unroll
-      for (int nt = 0; nt < 2; ++nt)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          c[nt][e] = c[nt][e] == -INFINITY ? 0.0f : ac_exp2(c[nt][e] - m_run[e >> 1]);
-          add[e >> 1] += c[nt][e];
+        for (int e = 0; e < 2; ++e) {
+          float mx = fmaxf(c[n][e], c[n][2 + e]);
+          mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 4));
+          mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 8));
+          mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 16));
+          const float m_new = fmaxf(m_run[n][e], mx);
+          alpha[n][e] = m_new == m_run[n][e] ? 1.0f : ac_exp2(m_run[n][e] - m_new);
+          moved |= alpha[n][e] != 1.0f;
+          m_run[n][e] = m_new;
         }
-      l_run[0] = fmaf(l_run[0], alpha[0], add[0]);
-      l_run[1] = fmaf(l_run[1], alpha[1], add[1]);
-      if (__any_sync(0xffffffffu, alpha[0] != 1.0f || alpha[1] != 1.0f)) {
 #pragma unroll
-        for (int nd = 0; nd < ND; ++nd) {
-          o[nd][0] = __fmul_rn(o[nd][0], alpha[0]);
-          o[nd][1] = __fmul_rn(o[nd][1], alpha[0]);
-          o[nd][2] = __fmul_rn(o[nd][2], alpha[1]);
-          o[nd][3] = __fmul_rn(o[nd][3], alpha[1]);
-        }
+      for (int n = 0; n < NG; ++n)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) c[n][e] = c[n][e] == -INFINITY ? 0.0f : ac_exp2(c[n][e] - m_run[n][e & 1]);
+#pragma unroll
+      for (int n = 0; n < NG; ++n)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) l_run[n][e] = fmaf(l_run[n][e], alpha[n][e], c[n][e] + c[n][2 + e]);
+      if (__any_sync(0xffffffffu, moved)) {
+#pragma unroll
+        for (int n = 0; n < NG; ++n)
+#pragma unroll
+          for (int d = 0; d < MD; ++d)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[n][d][e] = __fmul_rn(o[n][d][e], alpha[n][e & 1]);
       }
       // A value that is not finite in a slot that some row does not see (or behind the last slot) must not reach that row
       // as 0 * inf: such a unit goes through scalar sums over the seen slots.
@@ -369,43 +386,46 @@ attn_few_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constan
         odd = __any_sync(0xffffffffu, odd);
       }
       if (!odd) {
-        uint32_t ph[4], pl[4];
+        uint32_t ph[NG][2], pl[NG][2];  // B operand: row g, slots 2 t and the next (and + 8): blocks of 8 x 8 transposed
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const float p0 = c[i >> 1][2 * (i & 1)], p1 = c[i >> 1][2 * (i & 1) + 1];
-          ph[i] = pack_bf16x2(p0, p1);
-          pl[i] = pack_bf16x2(p0 - __uint_as_float(ph[i] << 16), p1 - __uint_as_float(ph[i] & 0xffff0000u));
-        }
+        for (int n = 0; n < NG; ++n)
 #pragma unroll
-        for (int nd = 0; nd < ND; nd += 2) {
-          const int key = 8 * (lm & 1) + lr, ch = nd + (lm >> 1);
-          uint32_t vb[4];
-          ldmatrix_x4_trans(vs_addr + (ch >> 3) * HALF + key * 128 + (((ch ^ key) & 7) << 4), vb);
-          mma_bf16(o[nd], ph, vb[0], vb[1]);
-          mma_bf16(o[nd + 1], ph, vb[2], vb[3]);
-          mma_bf16(o[nd], pl, vb[0], vb[1]);
-          mma_bf16(o[nd + 1], pl, vb[2], vb[3]);
+          for (int i = 0; i < 2; ++i) {
+            const float p0 = c[n][2 * i], p1 = c[n][2 * i + 1];
+            const uint32_t hi = pack_bf16x2(p0, p1);
+            ph[n][i] = movmatrix_trans(hi);
+            pl[n][i] = movmatrix_trans(pack_bf16x2(p0 - __uint_as_float(hi << 16), p1 - __uint_as_float(hi & 0xffff0000u)));
+          }
+#pragma unroll
+        for (int d = 0; d < MD; ++d) {
+          const int key = 8 * (lm >> 1) + lr, ch = 2 * d + (lm & 1);
+          uint32_t va[4];
+          ldmatrix_x4_trans(vs_addr + (ch >> 3) * HALF + key * 128 + (((ch ^ key) & 7) << 4), va);
+#pragma unroll
+          for (int n = 0; n < NG; ++n) mma_bf16(o[n][d], va, ph[n][0], ph[n][1]);
+#pragma unroll
+          for (int n = 0; n < NG; ++n) mma_bf16(o[n][d], va, pl[n][0], pl[n][1]);
         }
       } else {
         for (int key = 0; key < AF_SLOTS; ++key) {
-          const int from = (lane & ~3) | ((key & 7) >> 1);  // the lane of this row group that holds the key's weight
-          float p[2];
-          bool see[2];
-          const int slot = slot0 + key;
+          const int from = 4 * (key & 7) + t, slot = slot0 + key;  // the lane that holds this slot's weights of the lane's rows
 #pragma unroll
-          for (int rr = 0; rr < 2; ++rr) {
-            const float w00 = __shfl_sync(0xffffffffu, c[0][2 * rr], from), w01 = __shfl_sync(0xffffffffu, c[0][2 * rr + 1], from);
-            const float w10 = __shfl_sync(0xffffffffu, c[1][2 * rr], from), w11 = __shfl_sync(0xffffffffu, c[1][2 * rr + 1], from);
-            p[rr] = key < 8 ? ((key & 1) ? w01 : w00) : ((key & 1) ? w11 : w10);
-            see[rr] = slot < end && (slot < q.used || ac_sees_new(anc, tok[rr], slot - q.used));
-          }
+          for (int n = 0; n < NG; ++n)
 #pragma unroll
-          for (int nd = 0; nd < ND; ++nd) {
-            const uint32_t w = ptx::lds32(vs_addr + (nd >> 3) * HALF + key * 128 + (((nd ^ key) & 7) << 4) + 4 * t);
-            const float v0 = __uint_as_float(w << 16), v1 = __uint_as_float(w & 0xffff0000u);
-            if (see[0]) { o[nd][0] = fmaf(p[0], v0, o[nd][0]); o[nd][1] = fmaf(p[0], v1, o[nd][1]); }
-            if (see[1]) { o[nd][2] = fmaf(p[1], v0, o[nd][2]); o[nd][3] = fmaf(p[1], v1, o[nd][3]); }
-          }
+            for (int e = 0; e < 2; ++e) {
+              const float lo = __shfl_sync(0xffffffffu, c[n][e], from), hi = __shfl_sync(0xffffffffu, c[n][2 + e], from);
+              const float p = key < 8 ? lo : hi;
+              const bool see = slot < end && (slot < q.used || ac_sees_new(anc, tok[n][e], slot - q.used));
+#pragma unroll
+              for (int d = 0; d < MD; ++d)
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                  const int dim = 16 * d + 8 * i + g;
+                  unsigned short v;
+                  asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(vs_addr + (dim >> 6) * HALF + key * 128 + ((((dim >> 3) ^ key) & 7) << 4) + 2 * (dim & 7)));
+                  if (see) o[n][d][2 * i + e] = fmaf(p, bf16_bits_to_float(v), o[n][d][2 * i + e]);
+                }
+            }
         }
       }
       __syncwarp();
@@ -421,27 +441,34 @@ attn_few_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constan
     const bool whole = u0 == 0 && u1 == units;
     const int cut = 2 * r + (u0 == 0 ? 1 : 0);
 #pragma unroll
-    for (int rr = 0; rr < 2; ++rr) {
-      l_run[rr] += __shfl_xor_sync(0xffffffffu, l_run[rr], 1);
-      l_run[rr] += __shfl_xor_sync(0xffffffffu, l_run[rr], 2);
-      const int x = g + 8 * rr;
-      if (x >= rows) continue;
-      if (whole) {
-        const bool none = l_run[rr] == 0.0f || ac_is_pad(anc, tok[rr]);
-        const float inv = none ? 0.0f : __fdiv_rn(1.0f, l_run[rr]);
-        const long long row = static_cast<long long>(q.t0 + tok[rr]) * a.n_heads + h * a.rep + x - tok[rr] * a.rep;
+    for (int n = 0; n < NG; ++n)
 #pragma unroll
-        for (int nd = 0; nd < ND; ++nd)
-          *reinterpret_cast<uint32_t*>(a.att + row * HD + 8 * nd + 2 * t) =
-              none ? 0u : pack_bf16x2(__fmul_rn(o[nd][2 * rr], inv), __fmul_rn(o[nd][2 * rr + 1], inv));
-        if (t == 0) a.lse[row] = none ? INFINITY : m_run[rr] + __log2f(l_run[rr]);
-      } else {
-        float* to = a.part_o + (static_cast<long long>(cut) * f.rows_cap + x) * HD;
+      for (int e = 0; e < 2; ++e) {
+        float l = l_run[n][e];
+        l += __shfl_xor_sync(0xffffffffu, l, 4);
+        l += __shfl_xor_sync(0xffffffffu, l, 8);
+        l += __shfl_xor_sync(0xffffffffu, l, 16);
+        const int x = 8 * n + 2 * t + e;
+        if (x >= rows) continue;
+        if (whole) {
+          const bool none = l == 0.0f || ac_is_pad(anc, tok[n][e]);
+          const float inv = none ? 0.0f : __fdiv_rn(1.0f, l);
+          const long long row = static_cast<long long>(q.t0 + tok[n][e]) * a.n_heads + h * a.rep + x - tok[n][e] * a.rep;
 #pragma unroll
-        for (int nd = 0; nd < ND; ++nd) *reinterpret_cast<float2*>(to + 8 * nd + 2 * t) = make_float2(o[nd][2 * rr], o[nd][2 * rr + 1]);
-        if (t == 0) a.part_ml[static_cast<long long>(cut) * f.rows_cap + x] = make_float2(m_run[rr], l_run[rr]);
+          for (int d = 0; d < MD; ++d)
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+              a.att[row * HD + 16 * d + 8 * i + g] = none ? 0 : float_to_bf16_bits(__fmul_rn(o[n][d][2 * i + e], inv));
+          if (g == 0) a.lse[row] = none ? INFINITY : m_run[n][e] + __log2f(l);
+        } else {
+          float* to = a.part_o + (static_cast<long long>(cut) * f.rows_cap + x) * HD + g;
+#pragma unroll
+          for (int d = 0; d < MD; ++d)
+#pragma unroll
+            for (int i = 0; i < 2; ++i) to[16 * d + 8 * i] = o[n][d][2 * i + e];
+          if (g == 0) a.part_ml[static_cast<long long>(cut) * f.rows_cap + x] = make_float2(m_run[n][e], l);
+        }
       }
-    }
     left -= u1 - u0;
     u0 = 0;
     if (left > 0 && ++h == a.c.n_kv) {
@@ -457,152 +484,126 @@ attn_few_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constan
   }
 }
 
-// The runs again, without the keys: joins the items that were cut (in run order) and adds every slot's weights, p = 2^(score
-// - lse), to mass.  The AJ_SPLIT warps of a run take its slots in turn, and of the results of a cut item each joins its share,
-// 8 dimensions of a row at a time.  Everything here is short chains of loads, so several are kept in flight: four rows of
-// statistics, four parts of a result, four slots per lane.
-constexpr int AJ_SPLIT = 4;
-
-// (maximum, sum) of two disjoint sets of keys.
-__device__ __forceinline__ float2 aj_merge(float2 x, float2 y) {
-  const float m = fmaxf(x.x, y.x);
-  const float lx = x.x == -INFINITY ? 0.0f : __fmul_rn(x.y, ac_exp2(x.x - m)), ly = y.x == -INFINITY ? 0.0f : __fmul_rn(y.y, ac_exp2(y.x - m));
-  return make_float2(m, lx + ly);
-}
-
+// Per item (sequence, kv head): joins the results of the runs that met it, in run order, and adds every slot's weights,
+// p = 2^(score - lse), to mass.  The CTAs of an item share its slots, f.join_slots each, and the results, by threads (few parts)
+// or by pieces of 8 dimensions (many parts: 4 parts side by side in a warp).  Short chains of loads bound it, so each thread
+// keeps four to eight under way.
 template <int HD, int SR>
 __global__ void __launch_bounds__(AF_THREADS) attn_few_join_kernel(const __grid_constant__ AfArgs f) {
   pdl_enter();
   const AcArgs& a = f.a;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, sub = blockIdx.y;
-  __shared__ float lse_s[AF_WARPS][AF_ROWS], max_s[AF_WARPS][AF_ROWS], inv_s[AF_WARPS][AF_ROWS];
-  const int r = warp * gridDim.x + blockIdx.x;
-  const AfRun run = f.run[r];
-  const AfHead head = *f.head;
-  int left = run.left, s = run.s, h = run.h, u0 = run.u;
-  int at = left > 0 ? af_start(head, r) : 0;  // place in the list
-  const int slot_mask = (1 << a.c.page_shift) - 1;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  __shared__ float lse_s[AF_ROWS], max_s[AF_ROWS], inv_s[AF_ROWS];
+  const int h = blockIdx.x % a.c.n_kv, s = blockIdx.x / a.c.n_kv;
   KvSeq q;
-  while (left > 0) {
-    const int units = af_units(a, s, q);
-    const int u1 = min(units, u0 + left), end = q.used + q.m, rows = q.m * a.rep;
-    const bool whole = u0 == 0 && u1 == units;
-    const uint32_t* anc = a.b.parent ? a.anc + static_cast<long long>(q.t0) * AC_TREE_WORDS : nullptr;
-    auto row_at = [&](int x) { return static_cast<long long>(q.t0 + x / a.rep) * a.n_heads + h * a.rep + x % a.rep; };
-    if (whole) {
-      if (lane < AF_ROWS) lse_s[warp][lane] = lane < rows ? a.lse[row_at(lane)] : INFINITY;
-      __syncwarp();
-    } else {
-      const int ra = af_run_of(head, at - u0), rb = af_run_of(head, at - u0 + units - 1), n = rb - ra + 1, me = r - ra;
-      auto part = [&](int k) { return static_cast<long long>(2 * (ra + k) + (k == 0 ? 1 : 0)) * f.rows_cap; };
-      for (int x0 = 0; x0 < AF_ROWS; x0 += 4) {
-        float2 ml[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) ml[i] = make_float2(-INFINITY, 0.0f);
-        if (x0 < rows) {
-          for (int k = lane; k < n; k += 32) {
-            float2 v[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) v[i] = x0 + i < rows ? a.part_ml[part(k) + x0 + i] : make_float2(-INFINITY, 0.0f);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) ml[i] = aj_merge(ml[i], v[i]);
-          }
-#pragma unroll
-          for (int o = 16; o > 0; o >>= 1)
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-              ml[i] = aj_merge(ml[i], make_float2(__shfl_xor_sync(0xffffffffu, ml[i].x, o), __shfl_xor_sync(0xffffffffu, ml[i].y, o)));
+  const int units = af_units(a, s, q), end = q.used + q.m, slot0 = blockIdx.y * f.join_slots;
+  if (units == 0 || slot0 >= end) return;
+  const int at = f.item_at[blockIdx.x], ctas = (end + f.join_slots - 1) / f.join_slots, rows = q.m * a.rep;
+  const AfHead head = *f.head;
+  const uint32_t* anc = a.b.parent ? a.anc + static_cast<long long>(q.t0) * AC_TREE_WORDS : nullptr;
+  auto row_at = [&](int x) { return static_cast<long long>(q.t0 + x / a.rep) * a.n_heads + h * a.rep + x % a.rep; };
+  const int ra = af_run_of(head, at), n = af_run_of(head, at + units - 1) - ra + 1;
+  if (n == 1) {
+    if (threadIdx.x < AF_ROWS) lse_s[threadIdx.x] = threadIdx.x < rows ? a.lse[row_at(threadIdx.x)] : INFINITY;
+    __syncthreads();
+  } else {
+    auto part = [&](int k) { return static_cast<long long>(2 * (ra + k) + (k == 0 ? 1 : 0)) * f.rows_cap; };
+    for (int x = warp; x < AF_ROWS; x += AF_WARPS) {
+      float m = -INFINITY, l = 0.0f;
+      if (x < rows) {
+        for (int k = lane; k < n; k += 32) m = fmaxf(m, a.part_ml[part(k) + x].x);
+        m = warp_max(m);
+        for (int k = lane; k < n; k += 32) {
+          const float2 ml = a.part_ml[part(k) + x];
+          if (ml.x != -INFINITY) l = fmaf(ml.y, ac_exp2(ml.x - m), l);
         }
-        if (lane < 4) {
-          const float2 v = lane == 0 ? ml[0] : lane == 1 ? ml[1] : lane == 2 ? ml[2] : ml[3];
-          const int x = x0 + lane;
-          const bool none = x >= rows || v.y == 0.0f || ac_is_pad(anc, x / a.rep);
-          lse_s[warp][x] = none ? INFINITY : v.x + __log2f(v.y);
-          max_s[warp][x] = v.x;
-          inv_s[warp][x] = none ? 0.0f : __fdiv_rn(1.0f, v.y);
-        }
+        l = warp_sum(l);
       }
-      __syncwarp();
-      // results: pieces of 8 dimensions, dealt to the warps of the item in turn; lanes: 4 parts side by side x 8 dimensions.
-      // Eight loads of a lane are under way together: parts of one piece, or pieces where an item has few parts.
-      const int k0 = lane >> 3, d = lane & 7, pieces = rows * (HD / 8), step = n * AJ_SPLIT;
-      const int kn = n > 4 ? 8 : 1, pn = n > 4 ? 1 : 8;
-      for (int i0 = me * AJ_SPLIT + sub; i0 < pieces; i0 += pn * step) {
-        float acc[8];
-#pragma unroll
-        for (int j = 0; j < 8; ++j) acc[j] = 0.0f;
-        for (int kb = k0; kb < n; kb += 4 * kn) {
-          float v[8], m[8];
+      if (lane == 0) {
+        const bool none = x >= rows || l == 0.0f || ac_is_pad(anc, x / a.rep);
+        lse_s[x] = none ? INFINITY : m + __log2f(l);
+        max_s[x] = m;
+        inv_s[x] = none ? 0.0f : __fdiv_rn(1.0f, l);
+      }
+    }
+    __syncthreads();
+    if (n <= 16) {
+      for (int i = blockIdx.y * AF_THREADS + threadIdx.x; i < rows * (HD / 2); i += ctas * AF_THREADS) {
+        const int x = i / (HD / 2), d = 2 * (i - x * (HD / 2));
+        const float m = max_s[x];
+        float2 acc = make_float2(0.0f, 0.0f);
+#pragma unroll 4
+        for (int k = 0; k < n; ++k) {
+          const float2 v = *reinterpret_cast<const float2*>(a.part_o + (part(k) + x) * HD + d);
+          const float mk = a.part_ml[part(k) + x].x;
+          const float w = mk == -INFINITY ? 0.0f : ac_exp2(mk - m);
+          acc.x = fmaf(mk == -INFINITY ? 0.0f : v.x, w, acc.x);
+          acc.y = fmaf(mk == -INFINITY ? 0.0f : v.y, w, acc.y);
+        }
+        const bool none = lse_s[x] == INFINITY;
+        *reinterpret_cast<uint32_t*>(a.att + row_at(x) * HD + d) =
+            none ? 0u : pack_bf16x2(__fmul_rn(acc.x, inv_s[x]), __fmul_rn(acc.y, inv_s[x]));
+      }
+    } else {
+      const int k0 = lane >> 3, d = lane & 7;
+      for (int i = blockIdx.y * AF_WARPS + warp; i < rows * (HD / 8); i += ctas * AF_WARPS) {
+        const int x = i / (HD / 8), dim = (i - x * (HD / 8)) * 8 + d;
+        const float m = max_s[x];
+        float acc = 0.0f;
+        for (int kb = k0; kb < n; kb += 32) {
+          float v[8], mk[8];
 #pragma unroll
           for (int j = 0; j < 8; ++j) {
-            const int i = kn == 8 ? i0 : i0 + j * step, k = kn == 8 ? kb + 4 * j : kb, x = i / (HD / 8);
-            const bool have = i < pieces && k < n;
-            v[j] = have ? a.part_o[(part(k) + x) * HD + (i - x * (HD / 8)) * 8 + d] : 0.0f;
-            m[j] = have ? a.part_ml[part(k) + x].x - max_s[warp][x] : -INFINITY;
+            const int k = kb + 4 * j;
+            v[j] = k < n ? a.part_o[(part(k) + x) * HD + dim] : 0.0f;
+            mk[j] = k < n ? a.part_ml[part(k) + x].x : -INFINITY;
           }
 #pragma unroll
           for (int j = 0; j < 8; ++j)
-            if (m[j] > -INFINITY || m[j] != m[j]) acc[j] = fmaf(v[j], ac_exp2(m[j]), acc[j]);
+            if (mk[j] != -INFINITY) acc = fmaf(v[j], ac_exp2(mk[j] - m), acc);
         }
-        if (kn == 8) acc[0] = ((acc[0] + acc[1]) + (acc[2] + acc[3])) + ((acc[4] + acc[5]) + (acc[6] + acc[7]));
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          if (j >= pn) break;
-          acc[j] += __shfl_xor_sync(0xffffffffu, acc[j], 8);
-          acc[j] += __shfl_xor_sync(0xffffffffu, acc[j], 16);
-          const int i = i0 + j * step, x = i / (HD / 8);
-          const bool none = i >= pieces || lse_s[warp][x & (AF_ROWS - 1)] == INFINITY;
-          const float v = none ? 0.0f : __fmul_rn(acc[j], inv_s[warp][x]);
-          const float w = __shfl_down_sync(0xffffffffu, v, 1);
-          if (i < pieces && k0 == 0 && (d & 1) == 0)
-            *reinterpret_cast<uint32_t*>(a.att + row_at(x) * HD + (i - x * (HD / 8)) * 8 + d) = pack_bf16x2(v, w);
-        }
+        acc += __shfl_xor_sync(0xffffffffu, acc, 8);
+        acc += __shfl_xor_sync(0xffffffffu, acc, 16);
+        const float v = lse_s[x] == INFINITY ? 0.0f : __fmul_rn(acc, inv_s[x]);
+        const float w = __shfl_down_sync(0xffffffffu, v, 1);
+        if (k0 == 0 && (d & 1) == 0) *reinterpret_cast<uint32_t*>(a.att + row_at(x) * HD + dim) = pack_bf16x2(v, w);
       }
     }
-    if (f.scores) {
-      float lse[SR];
+  }
+  if (!f.scores) return;
+  float lse[SR];
 #pragma unroll
-      for (int x = 0; x < SR; ++x) lse[x] = lse_s[warp][x];
-      const int slot1 = min(end, u1 * AF_SLOTS);
-      const int* pages = a.c.page_table + static_cast<long long>(s) * a.c.max_pages;
-      for (int base = u0 * AF_SLOTS + 128 * sub + lane; base < slot1; base += 128 * AJ_SPLIT) {
-        int page[4];
-        long long row[4];
-        float4 sc[4][SR / 4];
-        float old[4];
+  for (int x = 0; x < SR; ++x) lse[x] = lse_s[x];
+  const int slot1 = min(end, slot0 + f.join_slots), slot_mask = (1 << a.c.page_shift) - 1;
+  const int* pages = a.c.page_table + static_cast<long long>(s) * a.c.max_pages;
+  for (int base = slot0 + threadIdx.x; base < slot1; base += 4 * AF_THREADS) {
+    int page[4];
+    long long row[4];
+    float4 sc[4][SR / 4];
+    float old[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) page[i] = base + 32 * i < slot1 ? pages[(base + 32 * i) >> a.c.page_shift] : -1;
+    for (int i = 0; i < 4; ++i) page[i] = base + AF_THREADS * i < slot1 ? pages[(base + AF_THREADS * i) >> a.c.page_shift] : -1;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          if (page[i] >= a.c.n_pages) page[i] = -1;  // reported by the kernel that read the keys
-          row[i] = page[i] < 0 ? 0 : kv_row(a.c, 0, page[i], h) + ((base + 32 * i) & slot_mask);
-          if (page[i] >= 0) {
-            old[i] = a.c.mass[row[i]];
+    for (int i = 0; i < 4; ++i) {
+      if (page[i] >= a.c.n_pages) page[i] = -1;  // reported by the kernel that read the keys
+      row[i] = page[i] < 0 ? 0 : kv_row(a.c, 0, page[i], h) + ((base + AF_THREADS * i) & slot_mask);
+      if (page[i] >= 0) {
+        old[i] = a.c.mass[row[i]];
 #pragma unroll
-            for (int x = 0; x < SR / 4; ++x) sc[i][x] = reinterpret_cast<const float4*>(f.scores + row[i] * SR)[x];
-          }
-        }
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          if (page[i] < 0) continue;
-          float got = 0.0f;
-#pragma unroll
-          for (int x = 0; x < SR / 4; ++x) {
-            const float v[4] = {sc[i][x].x, sc[i][x].y, sc[i][x].z, sc[i][x].w};
-#pragma unroll
-            for (int e = 0; e < 4; ++e) got += lse[4 * x + e] == INFINITY ? 0.0f : ac_exp2(v[e] - lse[4 * x + e]);
-          }
-          a.c.mass[row[i]] = old[i] + got;
-        }
+        for (int x = 0; x < SR / 4; ++x) sc[i][x] = reinterpret_cast<const float4*>(f.scores + row[i] * SR)[x];
       }
     }
-    __syncwarp();
-    left -= u1 - u0;
-    at += u1 - u0;
-    u0 = 0;
-    if (left > 0 && ++h == a.c.n_kv) {
-      h = 0;
-      while (++s + 1 < a.c.n_seq && af_units(a, s, q) == 0) {}
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if (page[i] < 0) continue;
+      float got = 0.0f;
+#pragma unroll
+      for (int x = 0; x < SR / 4; ++x) {
+        const float v[4] = {sc[i][x].x, sc[i][x].y, sc[i][x].z, sc[i][x].w};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) got += lse[4 * x + e] == INFINITY ? 0.0f : ac_exp2(v[e] - lse[4 * x + e]);
+      }
+      a.c.mass[row[i]] = old[i] + got;
     }
   }
 }

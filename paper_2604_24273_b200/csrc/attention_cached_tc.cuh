@@ -943,7 +943,7 @@ __global__ void __launch_bounds__(AM_KEYS) attn_mass_join_kernel(const __grid_co
 struct AcPlan {
   bool few;                                    // few rows: attn_few_kernel; else tiles
   int rows_cap;                                // rows kept of a cut item
-  int score_rows, runs;                        // few rows
+  int score_rows, runs, join_slots;            // few rows
   int tok_tile, nx, ctas;                      // tiles
   size_t lse_bytes, ml_bytes, o_bytes, cut_bytes, sum_bytes, score_bytes, anc_bytes, ok_bytes, run_bytes;
   size_t bytes() const { return lse_bytes + ml_bytes + o_bytes + cut_bytes + sum_bytes + score_bytes + 2 * anc_bytes + ok_bytes + run_bytes; }
@@ -969,9 +969,13 @@ inline AcPlan ac_plan(const KvView& c, int T, int max_new, int n_heads) {
     p.rows_cap = static_cast<int>(rows);
     p.score_rows = rows <= 4 ? 4 : rows <= 8 ? 8 : 16;
     p.runs = sm_count() * AF_WARPS;
+    // slots of a CTA of the join: long stretches, unless they would leave SMs idle (2000 slots of one sequence: 13.3 us in
+    // stretches of 2048, 6 us in stretches of 512; 128 sequences: no difference)
+    const long long stretches = ((c.max_pages << c.page_shift) + 2047) / 2048;
+    p.join_slots = stretches * c.n_seq * c.n_kv < 4LL * sm_count() ? 512 : 2048;
     p.ml_bytes = ac_up(static_cast<size_t>(2 * p.runs) * p.rows_cap * 8);
     p.o_bytes = ac_up(static_cast<size_t>(2 * p.runs) * p.rows_cap * c.hd * 4);
-    p.run_bytes = 256 + ac_up(static_cast<size_t>(p.runs) * sizeof(AfRun));
+    p.run_bytes = 256 + ac_up(static_cast<size_t>(c.n_seq) * c.n_kv * 4);
     p.score_bytes = c.mass ? ac_up((static_cast<size_t>(c.n_pages) * c.n_kv << c.page_shift) * p.score_rows * 4) : 0;
   } else {
     p.tok_tile = 128 / rep;
@@ -1019,13 +1023,17 @@ bitrl_status launch_attention_cached_hd(const AcArgs& a, const AcPlan& p, bool m
   if ((s = ac_tensor_map(&mk, a.c.k, 2, kv_size, kv_stride, kv_box)) != BITRL_OK) return s;
   if ((s = ac_tensor_map(&mv, a.c.v, 2, kv_size, kv_stride, kv_box)) != BITRL_OK) return s;
   if (p.few) {
-    static bool done[64] = {false};
-    if ((s = ac_smem(attn_few_kernel<HD>, af_smem_bytes<HD>(), done)) != BITRL_OK) return s;
+    static bool done[2][64] = {};
+    const bool one = p.rows_cap <= 8;
+    if ((s = one ? ac_smem(attn_few_kernel<HD, 1>, af_smem_bytes<HD>(), done[0])
+                 : ac_smem(attn_few_kernel<HD, 2>, af_smem_bytes<HD>(), done[1])) != BITRL_OK) return s;
     const dim3 grid(p.runs / AF_WARPS);
-    BITRL_CUDA(launch_pdl(attn_few_kernel<HD>, grid, dim3(AF_THREADS), af_smem_bytes<HD>(), st, mk, mv, f));
-    BITRL_CUDA(p.score_rows == 4   ? launch_pdl(attn_few_join_kernel<HD, 4>, dim3(grid.x, AJ_SPLIT), dim3(AF_THREADS), 0, st, f)
-               : p.score_rows == 8 ? launch_pdl(attn_few_join_kernel<HD, 8>, dim3(grid.x, AJ_SPLIT), dim3(AF_THREADS), 0, st, f)
-                                   : launch_pdl(attn_few_join_kernel<HD, 16>, dim3(grid.x, AJ_SPLIT), dim3(AF_THREADS), 0, st, f));
+    const dim3 join(static_cast<unsigned>(a.c.n_seq) * a.c.n_kv, ((a.c.max_pages << a.c.page_shift) + f.join_slots - 1) / f.join_slots);
+    BITRL_CUDA(one ? launch_pdl(attn_few_kernel<HD, 1>, grid, dim3(AF_THREADS), af_smem_bytes<HD>(), st, mk, mv, f)
+                   : launch_pdl(attn_few_kernel<HD, 2>, grid, dim3(AF_THREADS), af_smem_bytes<HD>(), st, mk, mv, f));
+    BITRL_CUDA(p.score_rows == 4   ? launch_pdl(attn_few_join_kernel<HD, 4>, join, dim3(AF_THREADS), 0, st, f)
+               : p.score_rows == 8 ? launch_pdl(attn_few_join_kernel<HD, 8>, join, dim3(AF_THREADS), 0, st, f)
+                                   : launch_pdl(attn_few_join_kernel<HD, 16>, join, dim3(AF_THREADS), 0, st, f));
     count_launch(2);
   } else {
     CUtensorMap mq;
@@ -1081,8 +1089,8 @@ bitrl_status launch_attention_cached(const KvView& c, const KvBatch& b, const vo
   a.anc = b.parent ? anc : nullptr;
   a.desc = b.parent ? desc : nullptr;
   a.tree_ok = b.parent ? ok : nullptr;
-  const AfArgs f{a, p.rows_cap, p.score_rows, p.runs, mass ? scores : nullptr, reinterpret_cast<AfHead*>(runs),
-                 reinterpret_cast<AfRun*>(runs + 256)};
+  const AfArgs f{a, p.rows_cap, p.score_rows, p.runs, p.join_slots, mass ? scores : nullptr, reinterpret_cast<AfHead*>(runs),
+                 reinterpret_cast<int*>(runs + 256)};
   if (b.parent) {
     BITRL_CUDA(launch_pdl(attn_tree_kernel, dim3(c.n_seq), dim3(BITRL_TREE_MAX_TOKENS), 0, st, c, b, anc, desc, ok));
     count_launch(1);
