@@ -150,7 +150,13 @@ def _ptr(t):
     return None if t is None else _vp(t.data_ptr())
 
 
+# The current stream's handle without the Stream object around it (3 us a call), where torch has it.
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
 def _stream():
+    if _raw_stream is not None:
+        return _raw_stream(torch.cuda.current_device())
     return _vp(torch.cuda.current_stream().cuda_stream)
 
 
@@ -465,12 +471,13 @@ TREE_MAX_TOKENS = 256
 KV_MAX_SLOTS = 1 << 19
 
 
-def _here(t: torch.Tensor, dtype, name: str, device) -> torch.Tensor:
-    """A contiguous CUDA tensor of that dtype on the cache's device, which has to be the current one."""
-    _dev(t, dtype, name)
-    if t.device != device:
-        raise ValueError(f"{name}: on {t.device}, the cache is on {device}")
-    return t
+def _here(t: torch.Tensor, dtype, name: str, index: int) -> int:
+    """Address of a contiguous tensor of that dtype on CUDA device ``index``."""
+    if not (isinstance(t, torch.Tensor) and t.dtype == dtype and t.is_contiguous() and t.is_cuda):
+        raise TypeError(f"{name}: expected a contiguous CUDA tensor of dtype {dtype}")
+    if t.get_device() != index:
+        raise ValueError(f"{name}: on {t.device}, the cache is on cuda:{index}")
+    return t.data_ptr()
 
 
 class KVCache:
@@ -484,14 +491,14 @@ class KVCache:
         _dev(k, torch.bfloat16, "k")
         if k.dim() != 5 or page_table.dim() != 2:
             raise ValueError("k is [layers, pages, kv heads, page tokens, head dim], page_table [sequences, pages]")
-        self.device = k.device
+        self.device, self.index = k.device, k.get_device()
         if pos is None:
             pos = torch.zeros(k.shape[:4], dtype=torch.int32, device=k.device)
         for t, dt, name in ((v, torch.bfloat16, "v"), (page_table, torch.int32, "page_table"), (used, torch.int32, "used"),
                             (seen, torch.int32, "seen"), (pos, torch.int32, "pos")):
-            _here(t, dt, name, self.device)
+            _here(t, dt, name, self.index)
         if mass is not None:
-            _here(mass, torch.float32, "mass", self.device)
+            _here(mass, torch.float32, "mass", self.index)
         n_layers, n_pages, n_kv, page, hd = k.shape
         n_seq, max_pages = page_table.shape
         if v.shape != k.shape or pos.shape != k.shape[:4] or (mass is not None and mass.shape != k.shape[:4]):
@@ -520,43 +527,44 @@ class KVCache:
                    pos=torch.zeros(shape, dtype=torch.int32, device=device))
 
     def _check_current(self):
-        if self.device.index != torch.cuda.current_device():
+        if self.index != torch.cuda.current_device():
             raise ValueError(f"the cache is on {self.device}, the current device is cuda:{torch.cuda.current_device()}")
 
-    def batch(self, states, T: int, parent):
-        """Checks the new tokens of a call: (offsets or None, max_new_len, parent)."""
+    def _batch(self, states, T: int, parent):
+        """Checks the new tokens of a call: (address of the offsets or None, max_new_len, address of parent or None).  The
+        caller keeps the tensors themselves until its kernels are launched."""
         self._check_current()
         if isinstance(states, int):
             if states < 0 or T != states * self.n_seq:
                 raise ValueError("T must be the common number of new tokens times the number of sequences")
             off, max_len = None, states
         else:
-            off, max_len = states
-            _here(off, torch.int32, "state offsets", self.device)
-            if off.numel() != self.n_seq + 1:
+            t, max_len = states
+            off = _here(t, torch.int32, "state offsets", self.index)
+            if t.numel() != self.n_seq + 1:
                 raise ValueError("state offsets: one entry more than sequences")
         if parent is not None:
-            _here(parent, torch.int32, "parent", self.device)
             if parent.numel() != T:
                 raise ValueError("parent: one entry per new token")
-        return off, int(max_len), parent
+            return off, int(max_len), _here(parent, torch.int32, "parent", self.index)
+        return off, int(max_len), None
 
 
 def kv_append(cache: KVCache, layer: int, qkv: torch.Tensor, states, n_heads: int, parent: torch.Tensor | None = None,
               theta: float = ROPE_THETA, q_out: torch.Tensor | None = None) -> torch.Tensor:
     """Rotates q and k of the new tokens qkv bf16 [T, (nh+2nkv)*hd], writes k and v into the cache and returns q [T, nh*hd].
     ``states``: an int (that many new tokens for every sequence) or (offsets int32 [n_seq+1], largest number)."""
-    _here(qkv, torch.bfloat16, "qkv", cache.device)
-    T = qkv.shape[0]
-    if qkv.dim() != 2 or qkv.shape[1] != (n_heads + 2 * cache.n_kv_heads) * cache.head_dim:
+    src, width = _here(qkv, torch.bfloat16, "qkv", cache.index), n_heads * cache.head_dim
+    if qkv.dim() != 2 or qkv.shape[1] != width + 2 * cache.n_kv_heads * cache.head_dim:
         raise ValueError("qkv must be [T, (n_heads + 2 n_kv_heads) * head_dim]")
-    off, max_len, parent = cache.batch(states, T, parent)
+    T = qkv.shape[0]
+    off, max_len, tree = cache._batch(states, T, parent)
     if q_out is None:
-        q_out = torch.zeros((T, n_heads * cache.head_dim), dtype=torch.bfloat16, device=qkv.device)
-    elif _here(q_out, torch.bfloat16, "q_out", cache.device).shape != (T, n_heads * cache.head_dim):
+        q_out = torch.zeros((T, width), dtype=torch.bfloat16, device=qkv.device)
+    dst = _here(q_out, torch.bfloat16, "q_out", cache.index)
+    if q_out.shape != (T, width):
         raise ValueError("q_out must be [T, n_heads * head_dim]")
-    _check(lib().bitrl_kv_append(cache._ref, layer, _ptr(qkv), T, _ptr(off), max_len, _ptr(parent), n_heads, float(theta),
-                                 _ptr(q_out), _stream()), "bitrl_kv_append")
+    _check(lib().bitrl_kv_append(cache._ref, layer, src, T, off, max_len, tree, n_heads, theta, dst, _stream()), "bitrl_kv_append")
     return q_out
 
 
@@ -569,23 +577,22 @@ def attention_cached(cache: KVCache, layer: int, q: torch.Tensor, states, n_head
                      workspace: torch.Tensor | None = None) -> torch.Tensor:
     """Attention of the appended new tokens (q bf16 [T, nh*hd] from ``kv_append``) over the cache and one another; adds the
     weights to ``cache.mass`` unless told not to.  Returns att bf16 [T, nh*hd]."""
-    _here(q, torch.bfloat16, "q", cache.device)
-    T = q.shape[0]
+    src = _here(q, torch.bfloat16, "q", cache.index)
     if q.dim() != 2 or q.shape[1] != n_heads * cache.head_dim:
         raise ValueError("q must be [T, n_heads * head_dim]")
-    off, max_len, parent = cache.batch(states, T, parent)
+    T = q.shape[0]
+    off, max_len, tree = cache._batch(states, T, parent)
     if att is None:
         att = torch.zeros_like(q)
-    elif _here(att, torch.bfloat16, "att", cache.device).shape != q.shape:
+    dst = _here(att, torch.bfloat16, "att", cache.index)
+    if att.shape != q.shape:
         raise ValueError("att must have q's shape")
     if workspace is None:
         workspace = torch.empty((max(attention_cached_workspace_bytes(cache, T, max_len, n_heads), 16),), dtype=torch.uint8,
                                 device=q.device)
-    else:
-        _here(workspace, torch.uint8, "workspace", cache.device)
-    _check(lib().bitrl_attention_cached(cache._ref, layer, _ptr(q), T, _ptr(off), max_len, _ptr(parent), n_heads,
-                                        int(accumulate_mass), _ptr(att), _ptr(workspace), workspace.numel(), _stream()),
-           "bitrl_attention_cached")
+    ws = _here(workspace, torch.uint8, "workspace", cache.index)
+    _check(lib().bitrl_attention_cached(cache._ref, layer, src, T, off, max_len, tree, n_heads, int(accumulate_mass), dst, ws,
+                                        workspace.numel(), _stream()), "bitrl_attention_cached")
     return att
 
 
@@ -600,12 +607,11 @@ def kv_evict_plan(cache: KVCache, budget: int, recent: int, sink: int = 0, moves
         moves = torch.full((*lists, max(1, min(budget, room - budget)), 2), -1, dtype=torch.int32, device=cache.device)
     if count is None:
         count = torch.empty(lists, dtype=torch.int32, device=cache.device)
-    _here(moves, torch.int32, "moves", cache.device)
-    _here(count, torch.int32, "count", cache.device)
-    if moves.shape[:3] != lists or moves.dim() != 5 or moves.shape[4] != 2 or count.shape != lists:
+    mv, n = _here(moves, torch.int32, "moves", cache.index), _here(count, torch.int32, "count", cache.index)
+    shape = moves.shape
+    if len(shape) != 5 or shape[:3] != lists or shape[4] != 2 or count.shape != lists:
         raise ValueError("moves is [layers, sequences, kv heads, max_moves, 2], count [layers, sequences, kv heads]")
-    _check(lib().bitrl_kv_evict_plan(cache._ref, budget, recent, sink, moves.shape[3], _ptr(moves), _ptr(count), _stream()),
-           "bitrl_kv_evict_plan")
+    _check(lib().bitrl_kv_evict_plan(cache._ref, budget, recent, sink, shape[3], mv, n, _stream()), "bitrl_kv_evict_plan")
     return moves, count
 
 
@@ -613,26 +619,26 @@ def kv_move(cache: KVCache, moves: torch.Tensor, count: torch.Tensor) -> None:
     """Moves rows inside the cache: lists per (layer, sequence, kv head) as from ``kv_evict_plan``, or moves [n_seq, max_moves, 2]
     and count [n_seq], the same for every layer and kv head."""
     cache._check_current()
-    _here(moves, torch.int32, "moves", cache.device)
-    _here(count, torch.int32, "count", cache.device)
-    per_head = moves.dim() == 5
+    mv, n = _here(moves, torch.int32, "moves", cache.index), _here(count, torch.int32, "count", cache.index)
+    shape = moves.shape
+    per_head = len(shape) == 5
     lists = (cache.n_layers, cache.n_seq, cache.n_kv_heads) if per_head else (cache.n_seq,)
-    if moves.shape[:-2] != lists or moves.shape[-1] != 2 or count.shape != lists:
+    if shape[:-2] != lists or shape[-1] != 2 or count.shape != lists:
         raise ValueError("moves and count must hold one list per (layer, sequence, kv head) or per sequence")
-    _check(lib().bitrl_kv_move(cache._ref, _ptr(moves), _ptr(count), moves.shape[-2], int(per_head), _stream()), "bitrl_kv_move")
+    _check(lib().bitrl_kv_move(cache._ref, mv, n, shape[-2], int(per_head), _stream()), "bitrl_kv_move")
 
 
 def kv_advance(cache: KVCache, states, n_keep: torch.Tensor | None = None, budget: int = 0) -> None:
     """After all layers of a step: used = min(used + n, budget), seen += n, with n = the new tokens, or ``n_keep`` [n_seq] of them.
     ``states`` 0 applies the budget alone."""
     cache._check_current()
-    if isinstance(states, int):
-        off, max_len = None, states
-    else:
-        off, max_len, _ = cache.batch(states, 0, None)
-    if n_keep is not None and _here(n_keep, torch.int32, "n_keep", cache.device).shape != (cache.n_seq,):
-        raise ValueError("n_keep: one entry per sequence")
-    _check(lib().bitrl_kv_advance(cache._ref, _ptr(off), max_len, _ptr(n_keep), budget, _stream()), "bitrl_kv_advance")
+    off, max_len = (None, states) if isinstance(states, int) else cache._batch(states, 0, None)[:2]
+    keep = None
+    if n_keep is not None:
+        keep = _here(n_keep, torch.int32, "n_keep", cache.index)
+        if n_keep.shape != (cache.n_seq,):
+            raise ValueError("n_keep: one entry per sequence")
+    _check(lib().bitrl_kv_advance(cache._ref, off, max_len, keep, budget, _stream()), "bitrl_kv_advance")
 
 
 def w8_quantize(W: torch.Tensor):
@@ -848,25 +854,29 @@ class Encoder:
                        pooled: torch.Tensor | None = None, want_pooled: bool = False, workspace: torch.Tensor | None = None):
         """The encoder over a cache: the new tokens h_in [T,d] attend to what their sequences have cached and to one another, and
         their keys and values are appended in every layer (``kv_advance`` then counts them).  Returns h_out, or (h_out, pooled)."""
-        _here(h_in, torch.bfloat16, "h_in", cache.device)
-        T = h_in.shape[0]
+        src = _here(h_in, torch.bfloat16, "h_in", cache.index)
         if h_in.dim() != 2 or h_in.shape[1] != self.d:
             raise ValueError("h_in must be [T, d]")
-        off, max_len, parent = cache.batch(states, T, parent)
+        T = h_in.shape[0]
+        off, max_len, tree = cache._batch(states, T, parent)
         if h_out is None:
             h_out = torch.empty_like(h_in)
-        elif _here(h_out, torch.bfloat16, "h_out", cache.device).shape != h_in.shape:
+        dst = _here(h_out, torch.bfloat16, "h_out", cache.index)
+        if h_out.shape != h_in.shape:
             raise ValueError("h_out must have h_in's shape")
         if pooled is None and want_pooled:
             pooled = torch.zeros((cache.n_seq, self.d), dtype=torch.bfloat16, device=h_in.device)
-        elif pooled is not None and _here(pooled, torch.bfloat16, "pooled", cache.device).shape != (cache.n_seq, self.d):
-            raise ValueError("pooled must be [n_seq, d]")
+        pool = None
+        if pooled is not None:
+            pool = _here(pooled, torch.bfloat16, "pooled", cache.index)
+            if pooled.shape != (cache.n_seq, self.d):
+                raise ValueError("pooled must be [n_seq, d]")
         if workspace is None:
             workspace = torch.empty((max(self.cached_workspace_bytes(cache, T, max_len), 16),), dtype=torch.uint8,
                                     device=h_in.device)
-        _check(lib().bitrl_encoder_forward_cached(self.handle, cache._ref, _ptr(h_in), T, _ptr(off), max_len, _ptr(parent),
-                                                  float(theta), int(accumulate_mass), _ptr(h_out), _ptr(pooled),
-                                                  _ptr(workspace), workspace.numel(), _stream()),
+        ws = _here(workspace, torch.uint8, "workspace", cache.index)
+        _check(lib().bitrl_encoder_forward_cached(self.handle, cache._ref, src, T, off, max_len, tree, float(theta),
+                                                  int(accumulate_mass), dst, pool, ws, workspace.numel(), _stream()),
                "bitrl_encoder_forward_cached")
         return (h_out, pooled) if pooled is not None else h_out
 

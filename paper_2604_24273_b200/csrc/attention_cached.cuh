@@ -109,8 +109,10 @@ __device__ __forceinline__ bool ac_is_pad(const uint32_t* anc, int tok) { return
 // the 4 HD bytes of its key and value) into the weight of every slot, so that keys are read once.
 // Scores come from mma.sync (eight rows fill its N; a tcgen05 tile has 128 rows).  The weights are split into two bf16
 // halves (16 significant bits), which costs nothing where reading bounds the kernel.
-constexpr int AF_WARPS = 8;
+constexpr int AF_WARPS = 4;
+constexpr int AF_CTAS = 2;  // per SM
 constexpr int AF_THREADS = 32 * AF_WARPS;
+constexpr int AJ_THREADS = 256, AJ_WARPS = AJ_THREADS / 32;
 constexpr int AF_STAGES = 3;
 constexpr int AF_ROWS = 16;
 constexpr int AF_SLOTS = 16;   // slots of a unit
@@ -153,7 +155,7 @@ constexpr uint32_t af_smem_bytes() {
 
 // NG: groups of eight rows.
 template <int HD, int NG>
-__global__ void __launch_bounds__(AF_THREADS, 1)
+__global__ void __launch_bounds__(AF_THREADS, AF_CTAS)
 attn_few_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constant__ CUtensorMap tmap_v, const __grid_constant__ AfArgs f) {
   constexpr int KS = HD / 16, MD = HD / 16, NH = HD / 64;
   constexpr uint32_t HALF = AF_SLOTS * 128, TILE = NH * HALF;  // a 64-dimension block of the keys (or values) of a unit
@@ -489,7 +491,7 @@ attn_few_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constan
 // or by pieces of 8 dimensions (many parts: 4 parts side by side in a warp).  Short chains of loads bound it, so each thread
 // keeps four to eight under way.
 template <int HD, int SR>
-__global__ void __launch_bounds__(AF_THREADS) attn_few_join_kernel(const __grid_constant__ AfArgs f) {
+__global__ void __launch_bounds__(AJ_THREADS) attn_few_join_kernel(const __grid_constant__ AfArgs f) {
   pdl_enter();
   const AcArgs& a = f.a;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -503,21 +505,53 @@ __global__ void __launch_bounds__(AF_THREADS) attn_few_join_kernel(const __grid_
   const uint32_t* anc = a.b.parent ? a.anc + static_cast<long long>(q.t0) * AC_TREE_WORDS : nullptr;
   auto row_at = [&](int x) { return static_cast<long long>(q.t0 + x / a.rep) * a.n_heads + h * a.rep + x % a.rep; };
   const int ra = af_run_of(head, at), n = af_run_of(head, at + units - 1) - ra + 1;
+  // The first slots' scores are on their way before the statistics are known.
+  const int slot1 = min(end, slot0 + f.join_slots), slot_mask = (1 << a.c.page_shift) - 1;
+  const int* pages = a.c.page_table + static_cast<long long>(s) * a.c.max_pages;
+  long long row[4];  // pool row of each of this thread's slots; -1: none
+  float4 sc[4][SR / 4];
+  float old[4];
+  auto fetch = [&](int base) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int slot = base + AJ_THREADS * i;
+      row[i] = slot < slot1 ? pages[slot >> a.c.page_shift] : -1;
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if (row[i] < 0 || row[i] >= a.c.n_pages) {  // a bad page was reported by the kernel that read the keys
+        row[i] = -1;
+        continue;
+      }
+      row[i] = kv_row(a.c, 0, static_cast<int>(row[i]), h) + ((base + AJ_THREADS * i) & slot_mask);
+      old[i] = a.c.mass[row[i]];
+#pragma unroll
+      for (int x = 0; x < SR / 4; ++x) sc[i][x] = reinterpret_cast<const float4*>(f.scores + row[i] * SR)[x];
+    }
+  };
+  if (f.scores) fetch(slot0 + threadIdx.x);
   if (n == 1) {
     if (threadIdx.x < AF_ROWS) lse_s[threadIdx.x] = threadIdx.x < rows ? a.lse[row_at(threadIdx.x)] : INFINITY;
     __syncthreads();
   } else {
     auto part = [&](int k) { return static_cast<long long>(2 * (ra + k) + (k == 0 ? 1 : 0)) * f.rows_cap; };
-    for (int x = warp; x < AF_ROWS; x += AF_WARPS) {
+    for (int x = warp; x < AF_ROWS; x += AJ_WARPS) {
       float m = -INFINITY, l = 0.0f;
       if (x < rows) {
-        for (int k = lane; k < n; k += 32) m = fmaxf(m, a.part_ml[part(k) + x].x);
-        m = warp_max(m);
-        for (int k = lane; k < n; k += 32) {
-          const float2 ml = a.part_ml[part(k) + x];
-          if (ml.x != -INFINITY) l = fmaf(ml.y, ac_exp2(ml.x - m), l);
+        for (int kb = lane; kb - lane < n; kb += 32 * 8) {
+          float2 ml[8];
+          float top = -INFINITY, sum = 0.0f;
+#pragma unroll
+          for (int j = 0; j < 8; ++j) ml[j] = kb + 32 * j < n ? a.part_ml[part(kb + 32 * j) + x] : make_float2(-INFINITY, 0.0f);
+#pragma unroll
+          for (int j = 0; j < 8; ++j) top = fmaxf(top, ml[j].x);
+          top = fmaxf(warp_max(top), m);
+#pragma unroll
+          for (int j = 0; j < 8; ++j)
+            if (ml[j].x != -INFINITY) sum = fmaf(ml[j].y, ac_exp2(ml[j].x - top), sum);
+          l = fmaf(l, m == -INFINITY ? 0.0f : ac_exp2(m - top), warp_sum(sum));
+          m = top;
         }
-        l = warp_sum(l);
       }
       if (lane == 0) {
         const bool none = x >= rows || l == 0.0f || ac_is_pad(anc, x / a.rep);
@@ -528,7 +562,7 @@ __global__ void __launch_bounds__(AF_THREADS) attn_few_join_kernel(const __grid_
     }
     __syncthreads();
     if (n <= 16) {
-      for (int i = blockIdx.y * AF_THREADS + threadIdx.x; i < rows * (HD / 2); i += ctas * AF_THREADS) {
+      for (int i = blockIdx.y * AJ_THREADS + threadIdx.x; i < rows * (HD / 2); i += ctas * AJ_THREADS) {
         const int x = i / (HD / 2), d = 2 * (i - x * (HD / 2));
         const float m = max_s[x];
         float2 acc = make_float2(0.0f, 0.0f);
@@ -546,7 +580,7 @@ __global__ void __launch_bounds__(AF_THREADS) attn_few_join_kernel(const __grid_
       }
     } else {
       const int k0 = lane >> 3, d = lane & 7;
-      for (int i = blockIdx.y * AF_WARPS + warp; i < rows * (HD / 8); i += ctas * AF_WARPS) {
+      for (int i = blockIdx.y * AJ_WARPS + warp; i < rows * (HD / 8); i += ctas * AJ_WARPS) {
         const int x = i / (HD / 8), dim = (i - x * (HD / 8)) * 8 + d;
         const float m = max_s[x];
         float acc = 0.0f;
@@ -574,28 +608,10 @@ __global__ void __launch_bounds__(AF_THREADS) attn_few_join_kernel(const __grid_
   float lse[SR];
 #pragma unroll
   for (int x = 0; x < SR; ++x) lse[x] = lse_s[x];
-  const int slot1 = min(end, slot0 + f.join_slots), slot_mask = (1 << a.c.page_shift) - 1;
-  const int* pages = a.c.page_table + static_cast<long long>(s) * a.c.max_pages;
-  for (int base = slot0 + threadIdx.x; base < slot1; base += 4 * AF_THREADS) {
-    int page[4];
-    long long row[4];
-    float4 sc[4][SR / 4];
-    float old[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) page[i] = base + AF_THREADS * i < slot1 ? pages[(base + AF_THREADS * i) >> a.c.page_shift] : -1;
+  for (int base = slot0 + threadIdx.x;;) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      if (page[i] >= a.c.n_pages) page[i] = -1;  // reported by the kernel that read the keys
-      row[i] = page[i] < 0 ? 0 : kv_row(a.c, 0, page[i], h) + ((base + AF_THREADS * i) & slot_mask);
-      if (page[i] >= 0) {
-        old[i] = a.c.mass[row[i]];
-#pragma unroll
-        for (int x = 0; x < SR / 4; ++x) sc[i][x] = reinterpret_cast<const float4*>(f.scores + row[i] * SR)[x];
-      }
-    }
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      if (page[i] < 0) continue;
+      if (row[i] < 0) continue;
       float got = 0.0f;
 #pragma unroll
       for (int x = 0; x < SR / 4; ++x) {
@@ -605,6 +621,9 @@ __global__ void __launch_bounds__(AF_THREADS) attn_few_join_kernel(const __grid_
       }
       a.c.mass[row[i]] = old[i] + got;
     }
+    base += 4 * AJ_THREADS;
+    if (base >= slot1) break;
+    fetch(base);
   }
 }
 

@@ -968,7 +968,9 @@ inline AcPlan ac_plan(const KvView& c, int T, int max_new, int n_heads) {
   if (p.few) {
     p.rows_cap = static_cast<int>(rows);
     p.score_rows = rows <= 4 ? 4 : rows <= 8 ? 8 : 16;
-    p.runs = sm_count() * AF_WARPS;
+    // one run per resident warp: with two to four times as many, parts and their joining cost more than the evener end gives
+    // (100k slots of one sequence: 66 us against 82 .. 117; 128 sequences of up to 4096: 133 against 137 .. 139)
+    p.runs = sm_count() * AF_WARPS * AF_CTAS;
     // slots of a CTA of the join: long stretches, unless they would leave SMs idle (2000 slots of one sequence: 13.3 us in
     // stretches of 2048, 6 us in stretches of 512; 128 sequences: no difference)
     const long long stretches = ((c.max_pages << c.page_shift) + 2047) / 2048;
@@ -1031,9 +1033,9 @@ bitrl_status launch_attention_cached_hd(const AcArgs& a, const AcPlan& p, bool m
     const dim3 join(static_cast<unsigned>(a.c.n_seq) * a.c.n_kv, ((a.c.max_pages << a.c.page_shift) + f.join_slots - 1) / f.join_slots);
     BITRL_CUDA(one ? launch_pdl(attn_few_kernel<HD, 1>, grid, dim3(AF_THREADS), af_smem_bytes<HD>(), st, mk, mv, f)
                    : launch_pdl(attn_few_kernel<HD, 2>, grid, dim3(AF_THREADS), af_smem_bytes<HD>(), st, mk, mv, f));
-    BITRL_CUDA(p.score_rows == 4   ? launch_pdl(attn_few_join_kernel<HD, 4>, join, dim3(AF_THREADS), 0, st, f)
-               : p.score_rows == 8 ? launch_pdl(attn_few_join_kernel<HD, 8>, join, dim3(AF_THREADS), 0, st, f)
-                                   : launch_pdl(attn_few_join_kernel<HD, 16>, join, dim3(AF_THREADS), 0, st, f));
+    BITRL_CUDA(p.score_rows == 4   ? launch_pdl(attn_few_join_kernel<HD, 4>, join, dim3(AJ_THREADS), 0, st, f)
+               : p.score_rows == 8 ? launch_pdl(attn_few_join_kernel<HD, 8>, join, dim3(AJ_THREADS), 0, st, f)
+                                   : launch_pdl(attn_few_join_kernel<HD, 16>, join, dim3(AJ_THREADS), 0, st, f));
     count_launch(2);
   } else {
     CUtensorMap mq;

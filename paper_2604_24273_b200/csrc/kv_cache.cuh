@@ -199,7 +199,10 @@ bitrl_status launch_kv_append(const KvView& c, const KvBatch& b, const void* qkv
   a.q_out = static_cast<unsigned short*>(q_out);
   a.n_heads = n_heads;
   a.tiles = (b.max_new + APP_TOKENS - 1) / APP_TOKENS;
-  for (int f = 0; f < 64; ++f) a.turns[f] = f < c.hd / 2 ? pow(theta, -2.0 * f / c.hd) / (2.0 * 3.14159265358979323846) : 0.0;
+  // one power and 80-bit products (each off by 2^-64) in place of 64 powers
+  const long double ratio = powl(static_cast<long double>(theta), -2.0L / c.hd);
+  long double turn = 1.0L / (2.0L * 3.14159265358979323846264338327950288L);
+  for (int f = 0; f < 64; ++f, turn *= ratio) a.turns[f] = f < c.hd / 2 ? static_cast<double>(turn) : 0.0;
   const dim3 grid(static_cast<unsigned>(c.n_seq) * a.tiles);
   BITRL_CUDA(c.hd == 128 ? launch_pdl(kv_append_kernel<128>, grid, dim3(APP_THREADS), 0, st, a)
                          : launch_pdl(kv_append_kernel<64>, grid, dim3(APP_THREADS), 0, st, a));
