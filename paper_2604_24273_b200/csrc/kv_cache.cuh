@@ -213,12 +213,14 @@ bitrl_status launch_kv_append(const KvView& c, const KvBatch& b, const void* qkv
 // ---- eviction plan --------------------------------------------------------------------------------------------------
 // One CTA per (layer, sequence, kv head).  The weight of a slot becomes an unsigned key whose order is the numbers' order
 // (NaN lowest, -0 = +0).  Protected slots come first, so the threshold lies in one group alone: the free slots when the
-// protected ones fit into the budget, else the protected ones.  A radix select (11 + 11 + 10 bits from the top, counts in
-// shared memory) finds the threshold key and how many slots that equal it stay, lowest first; one ordered pass then
-// turns the decision into a bit per slot and the bits into the two ascending lists.  Each slot is read from memory once.
-constexpr int PLAN_THREADS = 512;
-constexpr int PLAN_WARPS = PLAN_THREADS / 32;
+// protected ones fit into the budget, else the protected ones.  Selection: counts over up to 2048 equal steps of the key
+// range that the group really spans (weights fill a few binades, so fixed digits would pile up in a few counters), then
+// over the step that holds the threshold, until few keys are left in it (or one value), whose ranks are counted directly.
+// One ordered pass then makes a bit per slot (ties: lower slots stay), another turns bits into the two ascending lists.
+// Every slot is read from memory once, its key kept in shared memory.  8 bytes per slot would take 17 us for 2400 lists of up
+// to 8192 slots; the passes over shared memory and the meeting points between them bound it.
 constexpr int PLAN_BINS = 2048;
+constexpr int PLAN_FEW = 128;  // keys whose ranks are counted directly
 
 struct PlanArgs {
   KvView c;
@@ -234,11 +236,15 @@ __device__ __forceinline__ uint32_t plan_key(float w) {
   return (u & 0x80000000u) ? ~u : (u | 0x80000000u);  // -inf is 0x007fffff: above NaN
 }
 
-__global__ void __launch_bounds__(PLAN_THREADS) kv_evict_plan_kernel(const PlanArgs a) {
+template <int THREADS>
+__global__ void __launch_bounds__(THREADS) kv_evict_plan_kernel(const PlanArgs a) {
+  constexpr int WARPS = THREADS / 32;
   extern __shared__ __align__(16) unsigned char plan_smem[];
   __shared__ int hist[PLAN_BINS];
-  __shared__ int warp_part[PLAN_WARPS + 1], warp_part2[PLAN_WARPS + 1];
-  __shared__ int sel[4];  // chosen bin, slots still wanted inside it, protected slots, all pages valid
+  __shared__ int part[WARPS], part2[WARPS];
+  __shared__ uint32_t few[PLAN_FEW];
+  __shared__ uint32_t group_lo, group_hi, chosen;
+  __shared__ int n_prot, wanted, n_few, inside;
   pdl_enter();
   const KvView& c = a.c;
   const int list = blockIdx.x;
@@ -255,142 +261,220 @@ __global__ void __launch_bounds__(PLAN_THREADS) kv_evict_plan_kernel(const PlanA
     return;
   }
   const int words = (n + 31) >> 5;
-  uint32_t* key_s = reinterpret_cast<uint32_t*>(plan_smem);                   // [min(n, smem_slots)]
-  uint32_t* prot_s = key_s + a.smem_slots;                                    // [words] bit per slot: protected
   const bool cached = n <= a.smem_slots;
-  uint32_t* keep_s = prot_s + (static_cast<int>(room) + 31) / 32;             // [words] bit per slot: stays
-  const int recent_from = seen > a.recent ? seen - a.recent : 0;
-  auto row_of = [&](int t) -> long long {
-    const int page = c.page_table[static_cast<long long>(s) * c.max_pages + (t >> c.page_shift)];
-    if (page < 0 || page >= c.n_pages) return -1;
-    return kv_row(c, layer, page, head) + (t & ((1 << c.page_shift) - 1));
+  uint32_t* key_s = reinterpret_cast<uint32_t*>(plan_smem);        // [min(n, smem_slots)]
+  uint32_t* prot_s = key_s + a.smem_slots;                         // [words] bit per slot: protected
+  uint32_t* keep_s = prot_s + (static_cast<int>(room) + 31) / 32;  // [words] bit per slot: stays
+  const int recent_from = seen > a.recent ? seen - a.recent : 0, slot_mask = (1 << c.page_shift) - 1;
+  const int* pages = c.page_table + static_cast<long long>(s) * c.max_pages;
+  auto key_at = [&](int t) -> uint32_t {
+    return cached ? key_s[t] : plan_key(c.mass[kv_row(c, layer, pages[t >> c.page_shift], head) + (t & slot_mask)]);
   };
-  auto key_at = [&](int t) -> uint32_t { return cached ? key_s[t] : plan_key(c.mass[row_of(t)]); };
-
-  // ---- read every slot once: key, protected bit
+  if (threadIdx.x == 0) {
+    n_prot = 0;
+    group_lo = 0xffffffffu;
+    group_hi = 0u;
+  }
+  // ---- read every slot once: key, protected bit, range of the keys of either group
   int prot = 0;
+  uint32_t lo[2] = {0xffffffffu, 0xffffffffu}, hi[2] = {0u, 0u};  // free, protected
   bool bad = false;
-  for (int w = warp; w < words; w += PLAN_WARPS) {
-    const int t = 32 * w + lane;
-    bool p = false;
-    if (t < n) {
-      const long long r = row_of(t);
-      if (r < 0) {
+  for (int w = warp; w < words; w += 4 * WARPS) {
+    int page[4], ps[4];
+    float m[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int t = 32 * (w + i * WARPS) + lane;
+      page[i] = t < n ? pages[t >> c.page_shift] : 0;
+      if (page[i] < 0 || page[i] >= c.n_pages) {
         bad = true;
-      } else {
-        const int ps = c.pos[r];
-        p = ps >= recent_from || ps < a.sink;
-        if (cached) key_s[t] = plan_key(c.mass[r]);
+        page[i] = 0;
       }
     }
-    const uint32_t bits = __ballot_sync(0xffffffffu, p);
-    if (lane == 0) prot_s[w] = bits;
-    prot += p;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int t = 32 * (w + i * WARPS) + lane;
+      const long long r = kv_row(c, layer, page[i], head) + (t & slot_mask);
+      ps[i] = t < n ? c.pos[r] : INT_MAX;
+      m[i] = t < n ? c.mass[r] : 0.0f;
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int at = w + i * WARPS, t = 32 * at + lane;
+      if (at >= words) break;
+      const bool p = t < n && (ps[i] >= recent_from || ps[i] < a.sink);
+      const uint32_t bits = __ballot_sync(0xffffffffu, p), key = plan_key(m[i]);
+      if (t < n) {
+        if (cached) key_s[t] = key;
+        lo[0] = p ? lo[0] : min(lo[0], key);
+        hi[0] = p ? hi[0] : max(hi[0], key);
+        lo[1] = p ? min(lo[1], key) : lo[1];
+        hi[1] = p ? max(hi[1], key) : hi[1];
+      }
+      if (lane == 0) prot_s[at] = bits;
+      prot += __popc(bits);
+    }
   }
-  if (threadIdx.x == 0) sel[2] = 0;
   if (__syncthreads_or(bad)) {
     if (threadIdx.x == 0) { report_status(BITRL_ERR_SHAPE, KV_STAGE_BAD_PAGE); a.count[list] = 0; }
     return;
   }
-  prot = warp_sum_i(prot);
-  if (lane == 0) atomicAdd(&sel[2], prot);
+  if (lane == 0 && prot) atomicAdd(&n_prot, prot);
   __syncthreads();
-  const int P = sel[2];
-  const bool among_protected = P >= B;        // which group the threshold lies in
-  int want = among_protected ? B : B - P;     // slots of that group that stay
-  uint32_t prefix = 0;                        // bits of the threshold found so far
-  // ---- radix select, from the top bits down
-  for (int pass = 0; pass < 3; ++pass) {
-    const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, width = pass == 2 ? 10 : 11;
-    for (int i = threadIdx.x; i < PLAN_BINS; i += PLAN_THREADS) hist[i] = 0;
-    __syncthreads();
-    for (int w = warp; w < words; w += PLAN_WARPS) {
-      const int t = 32 * w + lane;
-      if (t < n && (((prot_s[w] >> lane) & 1u) != 0) == among_protected) {
-        const uint32_t key = key_at(t);
-        if (pass == 0 || (key >> (shift + width)) == prefix) atomicAdd(&hist[(key >> shift) & ((1u << width) - 1u)], 1);
-      }
+  const bool among_protected = n_prot >= B;  // which group the threshold lies in
+  int want = among_protected ? B : B - n_prot;  // slots of that group that stay
+  {
+    const uint32_t l = __reduce_min_sync(0xffffffffu, lo[among_protected]), h = __reduce_max_sync(0xffffffffu, hi[among_protected]);
+    if (lane == 0) {
+      atomicMin(&group_lo, l);
+      atomicMax(&group_hi, h);
     }
+  }
+  __syncthreads();
+  uint32_t from = group_lo, to = group_hi;  // the threshold key lies in from .. to; `want` slots of that range stay
+  uint32_t thr = from;
+  int at_thr = 0;  // slots whose key is the threshold
+  // words of this warp, as `in` flags with their keys
+  auto each = [&](auto&& f) {
+    for (int w = warp; w < words; w += WARPS) {
+      const int t = 32 * w + lane;
+      if (t < n && (((prot_s[w] >> lane) & 1u) != 0) == among_protected) f(key_at(t));
+    }
+  };
+  while (true) {
+    const uint32_t span = to - from;
+    const int shift = span < PLAN_BINS ? 0 : 21 - __clz(span);  // span >> shift < PLAN_BINS
+    for (int i = threadIdx.x; i < PLAN_BINS; i += THREADS) hist[i] = 0;
+    if (threadIdx.x == 0) n_few = 0;
     __syncthreads();
-    // bins from the top: thread i owns PLAN_BINS / PLAN_THREADS of them
-    constexpr int PER = PLAN_BINS / PLAN_THREADS;
+    each([&](uint32_t key) {
+      if (key >= from && key <= to) atomicAdd(&hist[(key - from) >> shift], 1);
+    });
+    __syncthreads();
+    // steps from the top: thread i owns PLAN_BINS / THREADS of them
+    constexpr int PER = PLAN_BINS / THREADS;
+    const int top = PLAN_BINS - 1 - PER * static_cast<int>(threadIdx.x);
     int mine = 0;
-    const int hi = PLAN_BINS - 1 - PER * static_cast<int>(threadIdx.x);
 #pragma unroll
-    for (int j = 0; j < PER; ++j) mine += hist[hi - j];
+    for (int j = 0; j < PER; ++j) mine += hist[top - j];
     int incl = mine;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
       const int v = __shfl_up_sync(0xffffffffu, incl, o);
       if (lane >= o) incl += v;
     }
-    if (lane == 31) warp_part[warp] = incl;
+    if (lane == 31) part[warp] = incl;
     __syncthreads();
-    int before = 0;
-    for (int w = 0; w < warp; ++w) before += warp_part[w];
-    int above = before + incl - mine;  // slots in higher bins than this thread's
+    int above = incl - mine;  // slots in higher steps than this thread's
+    for (int w = 0; w < warp; ++w) above += part[w];
     if (above < want && above + mine >= want) {
       int j = 0;
-      while (above + hist[hi - j] < want) above += hist[hi - j++];
-      sel[0] = hi - j;
-      sel[1] = want - above;
+      while (above + hist[top - j] < want) above += hist[top - j++];
+      chosen = static_cast<uint32_t>(top - j);
+      wanted = want - above;
+      inside = hist[top - j];
     }
     __syncthreads();
-    prefix = (prefix << width) | static_cast<uint32_t>(sel[0]);
-    want = sel[1];
-    __syncthreads();
+    want = wanted;
+    const int left = inside;
+    from += chosen << shift;
+    to = min(to, from + ((1u << shift) - 1u));
+    if (shift == 0) {
+      thr = from;
+      at_thr = left;
+      break;
+    }
+    if (left <= PLAN_FEW) {
+      each([&](uint32_t key) {
+        if (key >= from && key <= to) few[atomicAdd(&n_few, 1)] = key;
+      });
+      __syncthreads();
+      if (threadIdx.x < left) {
+        const uint32_t key = few[threadIdx.x];
+        int greater = 0, equal = 0;
+        for (int i = 0; i < left; ++i) {
+          greater += few[i] > key;
+          equal += few[i] == key;
+        }
+        if (greater < want && greater + equal >= want) {  // the same values from every thread that finds them
+          chosen = key;
+          wanted = want - greater;
+          inside = equal;
+        }
+      }
+      __syncthreads();
+      thr = chosen;
+      want = wanted;
+      at_thr = inside;
+      break;
+    }
   }
-  const uint32_t thr = prefix;  // `want` slots that equal it stay, the lowest ones
 
-  // ---- ordered decision: every warp owns a run of words
-  const int per_warp = (words + PLAN_WARPS - 1) / PLAN_WARPS, w0 = warp * per_warp, w1 = min(words, w0 + per_warp);
-  int ties = 0;
-  for (int w = w0; w < w1; ++w) {
-    const int t = 32 * w + lane;
-    const bool in = t < n && (((prot_s[w] >> lane) & 1u) != 0) == among_protected;
-    ties += __popc(__ballot_sync(0xffffffffu, in && key_at(t) == thr));
-  }
-  if (lane == 0) warp_part[warp] = ties;
-  __syncthreads();
+  // ---- ordered decision: every warp owns a run of words.  Of the at_thr slots that equal the threshold the `want` lowest stay.
+  const int per_warp = (words + WARPS - 1) / WARPS, w0 = warp * per_warp, w1 = min(words, w0 + per_warp);
   int tie_rank = 0;
-  for (int w = 0; w < warp; ++w) tie_rank += warp_part[w];
+  if (want < at_thr) {
+    int ties = 0;
+    for (int w = w0; w < w1; ++w) {
+      const int t = 32 * w + lane;
+      const bool in = t < n && (((prot_s[w] >> lane) & 1u) != 0) == among_protected;
+      ties += __popc(__ballot_sync(0xffffffffu, in && key_at(t) == thr));
+    }
+    __syncthreads();
+    if (lane == 0) part[warp] = ties;
+    __syncthreads();
+    for (int w = 0; w < warp; ++w) tie_rank += part[w];
+  }
   int n_src = 0, n_dst = 0;
   for (int w = w0; w < w1; ++w) {
     const int t = 32 * w + lane;
-    const bool p = t < n && ((prot_s[w] >> lane) & 1u) != 0;
-    const bool in = t < n && p == among_protected;
+    const bool p = ((prot_s[w] >> lane) & 1u) != 0, in = t < n && p == among_protected;
     const uint32_t key = in ? key_at(t) : 0u;
-    const uint32_t tie = __ballot_sync(0xffffffffu, in && key == thr);
-    const bool keep = (p && !among_protected) ||
-                      (in && (key > thr || (key == thr && tie_rank + __popc(tie & ((1u << lane) - 1u)) < want)));
-    tie_rank += __popc(tie);
+    bool keep = (p && !among_protected) || (in && key >= thr);
+    if (want < at_thr) {
+      const uint32_t tie = __ballot_sync(0xffffffffu, in && key == thr);
+      if (in && key == thr) keep = tie_rank + __popc(tie & ((1u << lane) - 1u)) < want;
+      tie_rank += __popc(tie);
+    }
     const uint32_t kept = __ballot_sync(0xffffffffu, keep);
     if (lane == 0) keep_s[w] = kept;
-    n_src += __popc(__ballot_sync(0xffffffffu, keep && t >= B));
-    n_dst += __popc(__ballot_sync(0xffffffffu, !keep && t < B));
+    const uint32_t below = 32 * w + 32 <= B ? 0xffffffffu : 32 * w >= B ? 0u : (1u << (B - 32 * w)) - 1u;  // slots < B
+    n_src += __popc(kept & ~below);
+    n_dst += __popc(~kept & below);
   }
   __syncthreads();
-  if (lane == 0) { warp_part[warp] = n_src; warp_part2[warp] = n_dst; }
+  if (lane == 0) { part[warp] = n_src; part2[warp] = n_dst; }
   __syncthreads();
   int at_src = 0, at_dst = 0;
-  for (int w = 0; w < warp; ++w) { at_src += warp_part[w]; at_dst += warp_part2[w]; }
+  for (int w = 0; w < warp; ++w) { at_src += part[w]; at_dst += part2[w]; }
   if (threadIdx.x == 0) {
     int total = 0;
-    for (int w = 0; w < PLAN_WARPS; ++w) total += warp_part[w];
+    for (int w = 0; w < WARPS; ++w) total += part[w];
     a.count[list] = total;
   }
   int* out = a.moves + static_cast<long long>(list) * a.max_moves * 2;
   for (int w = w0; w < w1; ++w) {
-    const int t = 32 * w + lane;
-    const bool keep = (keep_s[w] >> lane) & 1u;
-    const bool src = keep && t >= B, dst = !keep && t < B;
-    const uint32_t bs = __ballot_sync(0xffffffffu, src), bd = __ballot_sync(0xffffffffu, dst);
-    const uint32_t below = (1u << lane) - 1u;
-    if (src) out[2 * (at_src + __popc(bs & below))] = t;
-    if (dst) out[2 * (at_dst + __popc(bd & below)) + 1] = t;
+    const uint32_t kept = keep_s[w], below = 32 * w + 32 <= B ? 0xffffffffu : 32 * w >= B ? 0u : (1u << (B - 32 * w)) - 1u;
+    const uint32_t bs = kept & ~below, bd = ~kept & below, mine = 1u << lane;
+    if (bs & mine) out[2 * (at_src + __popc(bs & (mine - 1u)))] = 32 * w + lane;
+    if (bd & mine) out[2 * (at_dst + __popc(bd & (mine - 1u))) + 1] = 32 * w + lane;
     at_src += __popc(bs);
     at_dst += __popc(bd);
   }
+}
+
+template <int THREADS>
+bitrl_status launch_kv_evict_plan_t(const PlanArgs& a, size_t smem, size_t limit, unsigned lists, cudaStream_t st) {
+  static bool done[64] = {false};
+  int dev = 0;
+  BITRL_CUDA(cudaGetDevice(&dev));
+  if (dev >= 0 && dev < 64 && !done[dev]) {
+    BITRL_CUDA(cudaFuncSetAttribute(kv_evict_plan_kernel<THREADS>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(limit)));
+    done[dev] = true;
+  }
+  BITRL_CUDA(launch_pdl(kv_evict_plan_kernel<THREADS>, dim3(lists), dim3(THREADS), smem, st, a));
+  count_launch(1);
+  return BITRL_OK;
 }
 
 bitrl_status launch_kv_evict_plan(const KvView& c, int budget, int recent, int sink, int max_moves, int* moves, int* count,
@@ -403,27 +487,21 @@ bitrl_status launch_kv_evict_plan(const KvView& c, int budget, int recent, int s
   const size_t left = (LIMIT - bits) / 4;
   a.smem_slots = static_cast<int>(left < static_cast<size_t>(room) ? left : room);
   const size_t smem = static_cast<size_t>(a.smem_slots) * 4 + bits;
-  static size_t attr_set[64] = {0};
-  int dev = 0;
-  BITRL_CUDA(cudaGetDevice(&dev));
-  if (dev >= 0 && dev < 64 && attr_set[dev] < smem) {
-    BITRL_CUDA(cudaFuncSetAttribute(kv_evict_plan_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(LIMIT)));
-    attr_set[dev] = LIMIT;
-  }
-  BITRL_CUDA(launch_pdl(kv_evict_plan_kernel, dim3(static_cast<unsigned>(c.n_layers) * c.n_seq * c.n_kv), dim3(PLAN_THREADS), smem, st, a));
-  count_launch(1);
-  return BITRL_OK;
+  const long long lists = static_cast<long long>(c.n_layers) * c.n_seq * c.n_kv;
+  // few lists: more threads on each
+  return lists <= 2 * sm_count() ? launch_kv_evict_plan_t<512>(a, smem, LIMIT, static_cast<unsigned>(lists), st)
+                                 : launch_kv_evict_plan_t<256>(a, smem, LIMIT, static_cast<unsigned>(lists), st);
 }
 
 // ---- moving rows ------------------------------------------------------------------------------------------------------
-// A pure gather/scatter of head_dim rows (437 MB read and written for 700 moves in 1200 lists), bound by the copy rate.
-// A CTA takes the moves of one list MOVE_CHUNK at a time: it reads all rows of a chunk, meets at a barrier and writes
-// them.  Sources and destinations ascend and no destination is above its source, so the source of a later move lies above every
-// earlier destination: reading chunk by chunk is as good as reading everything first, and the next chunk's reads need
-// not wait for this one's writes.  Where a list's last destination lies below its first source (always so for an
-// eviction) chunks do not touch one another at all and may be spread over several CTAs.
-constexpr int MOVE_THREADS = 256;
-constexpr int MOVE_ROWS = 4;  // rows in flight per lane group
+// A pure gather/scatter of head_dim rows, bound by the copy rate for long lists and by one chain of loads (count, move, page,
+// row) for short ones.  A CTA takes the moves of one list THREADS at a time: a thread looks up the pool rows of one move and
+// carries its mass and pos; then all threads move the rows of k and v, chunk by chunk, the next chunk's reads before this one's
+// writes.  Sources and destinations ascend and no destination is above its source, so the source of a later move lies above
+// every earlier destination: it is enough that a chunk is written after it and everything before it has been read.  Where a list's
+// last destination lies below its first source (always so for an eviction) moves do not touch one another at all: no barrier,
+// and the list may be spread over several CTAs.
+constexpr int MOVE_ROWS = 4;  // rows of a chunk per lane group
 
 struct MoveArgs {
   KvView c;
@@ -432,89 +510,114 @@ struct MoveArgs {
   int max_moves, per_head, splits;
 };
 
-template <int HD>
-__global__ void __launch_bounds__(MOVE_THREADS) kv_move_kernel(const MoveArgs a) {
-  constexpr int LANES = HD / 8;                     // lanes of 16 bytes per row
-  constexpr int GROUPS = MOVE_THREADS / (2 * LANES);  // moves handled side by side: one lane group for k, one for v
+template <int HD, int THREADS>
+__global__ void __launch_bounds__(THREADS) kv_move_kernel(const MoveArgs a) {
+  constexpr int LANES = HD / 8;                // lanes of 16 bytes per row
+  constexpr int GROUPS = THREADS / (2 * LANES);  // moves side by side: one lane group for k, one for v
   constexpr int CHUNK = GROUPS * MOVE_ROWS;
+  __shared__ long long from_s[THREADS], to_s[THREADS];  // pool rows; -1: skip
   pdl_enter();
   const KvView& c = a.c;
   const int list = blockIdx.x / a.splits, split = blockIdx.x - list * a.splits;
   const int head = list % c.n_kv, s = (list / c.n_kv) % c.n_seq, layer = list / (c.n_kv * c.n_seq);
   const int which = a.per_head ? list : s;
   const int n = a.count[which];
+  const int2* mv = reinterpret_cast<const int2*>(a.moves) + static_cast<long long>(which) * a.max_moves;
   if (n < 0 || n > a.max_moves) {
     if (threadIdx.x == 0) report_status(BITRL_ERR_SHAPE, KV_STAGE_BAD_MOVE);
     return;
   }
   if (n == 0) return;
-  const int2* mv = reinterpret_cast<const int2*>(a.moves) + static_cast<long long>(which) * a.max_moves;
-  int step = CHUNK, first = 0;
+  const bool apart = mv[n - 1].y < mv[0].x;
+  int first = 0, step = THREADS;
   if (a.splits > 1) {
-    if (mv[n - 1].y < mv[0].x) {
-      first = split * CHUNK;
-      step = a.splits * CHUNK;
+    if (apart) {
+      first = split * THREADS;
+      step = a.splits * THREADS;
     } else if (split > 0) {
       return;
     }
   }
   const int group = threadIdx.x / (2 * LANES), sub = threadIdx.x % (2 * LANES);
-  const bool is_v = sub >= LANES;
-  const int lane16 = sub % LANES;
-  uint4* pool = reinterpret_cast<uint4*>(is_v ? c.v : c.k);
-  const int room = c.max_pages << c.page_shift;
-  auto row_of = [&](int t) -> long long {
-    if (t < 0 || t >= room) {
-      report_status(BITRL_ERR_SHAPE, KV_STAGE_BAD_MOVE);
-      return -1;
-    }
-    const int page = kv_page(c, s, t);
-    return page < 0 ? -1 : kv_row(c, layer, page, head) + (t & ((1 << c.page_shift) - 1));
-  };
+  uint4* pool = reinterpret_cast<uint4*>(sub >= LANES ? c.v : c.k) + sub % LANES;
+  const int room = c.max_pages << c.page_shift, slot_mask = (1 << c.page_shift) - 1;
+  const int* pages = c.page_table + static_cast<long long>(s) * c.max_pages;
   for (int base = first; base < n; base += step) {
-    uint4 row[MOVE_ROWS];
-    long long to[MOVE_ROWS];
-    float w[MOVE_ROWS];
-    int ps[MOVE_ROWS];
-#pragma unroll
-    for (int u = 0; u < MOVE_ROWS; ++u) {
-      const int i = base + u * GROUPS + group;
-      to[u] = -1;
-      if (i < n) {
-        const int2 m = mv[i];
-        const long long fr = row_of(m.x);
-        to[u] = row_of(m.y);
-        if (fr < 0) to[u] = -1;
-        if (to[u] >= 0) {
-          row[u] = pool[fr * LANES + lane16];
-          if (sub == 0) w[u] = c.mass ? c.mass[fr] : 0.0f;
-          if (sub == LANES) ps[u] = c.pos[fr];
-        }
+    const int here = min(THREADS, n - base);
+    long long fr = -1, to = -1;
+    float w = 0.0f;
+    int ps = 0;
+    if (static_cast<int>(threadIdx.x) < here) {
+      const int2 m = mv[base + threadIdx.x];
+      const bool in = m.x >= 0 && m.x < room && m.y >= 0 && m.y < room;
+      const int pf = in ? pages[m.x >> c.page_shift] : -1, pt = in ? pages[m.y >> c.page_shift] : -1;
+      if (!in) {
+        report_status(BITRL_ERR_SHAPE, KV_STAGE_BAD_MOVE);
+      } else if (pf < 0 || pf >= c.n_pages || pt < 0 || pt >= c.n_pages) {
+        report_status(BITRL_ERR_SHAPE, KV_STAGE_BAD_PAGE);
+      } else {
+        fr = kv_row(c, layer, pf, head) + (m.x & slot_mask);
+        to = kv_row(c, layer, pt, head) + (m.y & slot_mask);
+        if (c.mass) w = c.mass[fr];
+        ps = c.pos[fr];
       }
     }
-    __syncthreads();  // every source of the chunk has been read
+    from_s[threadIdx.x] = fr;
+    to_s[threadIdx.x] = to;
+    __syncthreads();  // the rows are known, and every mass and pos has been read
+    if (to >= 0) {
+      if (c.mass) c.mass[to] = w;
+      c.pos[to] = ps;
+    }
+    uint4 row[2][MOVE_ROWS];
+    auto read = [&](int chunk, uint4 (&r)[MOVE_ROWS]) {
 #pragma unroll
-    for (int u = 0; u < MOVE_ROWS; ++u)
-      if (to[u] >= 0) {
-        pool[to[u] * LANES + lane16] = row[u];
-        if (sub == 0 && c.mass) c.mass[to[u]] = w[u];
-        if (sub == LANES) c.pos[to[u]] = ps[u];
+      for (int u = 0; u < MOVE_ROWS; ++u) {
+        const int i = chunk * CHUNK + u * GROUPS + group;
+        if (i < here && from_s[i] >= 0) r[u] = pool[from_s[i] * LANES];
       }
+    };
+    auto write = [&](int chunk, const uint4 (&r)[MOVE_ROWS]) {
+#pragma unroll
+      for (int u = 0; u < MOVE_ROWS; ++u) {
+        const int i = chunk * CHUNK + u * GROUPS + group;
+        if (i < here && to_s[i] >= 0) pool[to_s[i] * LANES] = r[u];
+      }
+    };
+    const int chunks = (here + CHUNK - 1) / CHUNK;
+    read(0, row[0]);
+    for (int k = 0; k < chunks; k += 2) {
+      if (k + 1 < chunks) read(k + 1, row[1]);
+      if (!apart) __syncthreads();  // everything up to chunk k (and k + 1) has been read
+      write(k, row[0]);
+      if (k + 1 < chunks) {
+        if (k + 2 < chunks) read(k + 2, row[0]);
+        if (!apart) __syncthreads();
+        write(k + 1, row[1]);
+      }
+    }
+    __syncthreads();  // from_s and to_s are free
   }
 }
 
-bitrl_status launch_kv_move(const KvView& c, const int* moves, const int* count, int max_moves, int per_head, cudaStream_t st) {
-  const long long lists = static_cast<long long>(c.n_layers) * c.n_seq * c.n_kv;
-  const int chunk = MOVE_THREADS / (c.hd / 4) * MOVE_ROWS;
+template <int HD>
+bitrl_status launch_kv_move_hd(MoveArgs a, cudaStream_t st) {
+  const long long lists = static_cast<long long>(a.c.n_layers) * a.c.n_seq * a.c.n_kv;
+  const bool small = a.max_moves <= 64;  // short lists: small CTAs, so that all of them are resident together
+  const int threads = small ? 64 : 256;
   long long splits = (4LL * sm_count() + lists - 1) / lists;
-  const long long most = (max_moves + chunk - 1) / chunk;
+  const long long most = (a.max_moves + threads - 1) / threads;
   if (splits > most) splits = most;
-  MoveArgs a{c, moves, count, max_moves, per_head, static_cast<int>(splits)};
+  a.splits = static_cast<int>(splits);
   const dim3 grid(static_cast<unsigned>(lists * splits));
-  BITRL_CUDA(c.hd == 128 ? launch_pdl(kv_move_kernel<128>, grid, dim3(MOVE_THREADS), 0, st, a)
-                         : launch_pdl(kv_move_kernel<64>, grid, dim3(MOVE_THREADS), 0, st, a));
+  BITRL_CUDA(small ? launch_pdl(kv_move_kernel<HD, 64>, grid, dim3(64), 0, st, a) : launch_pdl(kv_move_kernel<HD, 256>, grid, dim3(256), 0, st, a));
   count_launch(1);
   return BITRL_OK;
+}
+
+bitrl_status launch_kv_move(const KvView& c, const int* moves, const int* count, int max_moves, int per_head, cudaStream_t st) {
+  const MoveArgs a{c, moves, count, max_moves, per_head, 1};
+  return c.hd == 128 ? launch_kv_move_hd<128>(a, st) : launch_kv_move_hd<64>(a, st);
 }
 
 // out[s, :] = row of the last new token of sequence s; sequences without new tokens keep theirs.
