@@ -212,13 +212,14 @@ bitrl_status launch_kv_append(const KvView& c, const KvBatch& b, const void* qkv
 
 // ---- eviction plan --------------------------------------------------------------------------------------------------
 // One CTA per (layer, sequence, kv head).  The weight of a slot becomes an unsigned key whose order is the numbers' order
-// (NaN lowest, -0 = +0).  Protected slots come first, so the threshold lies in one group alone: the free slots when the
-// protected ones fit into the budget, else the protected ones.  Selection: counts over up to 2048 equal steps of the key
-// range that the group really spans (weights fill a few binades, so fixed digits would pile up in a few counters), then
-// over the step that holds the threshold, until few keys are left in it (or one value), whose ranks are counted directly.
-// One ordered pass then makes a bit per slot (ties: lower slots stay), another turns bits into the two ascending lists.
-// Every slot is read from memory once, its key kept in shared memory.  8 bytes per slot would take 17 us for 2400 lists of up
-// to 8192 slots; the passes over shared memory and the meeting points between them bound it.
+// (NaN lowest, -0 = +0); 0 and the greatest key stand for slots that go and stay whatever their weight.  Protected slots come
+// first, so the threshold lies in one group alone: as a rule the protected ones fit into the budget, stay, and the free ones
+// compete; else (a second reading) the free ones go and the protected ones compete.  Selection: counts over up to 2048 equal
+// steps of the key range that the group really spans (weights fill a few binades, so fixed digits would pile up in a few
+// counters), then over the step that holds the threshold, until few keys are left in it (or one value), whose ranks are
+// counted directly.  Two ordered passes over the keys count and write the ascending lists (ties: lower slots stay).
+// Every slot is read from memory once, four by a lane, its key kept in shared memory.  Reading 8 bytes per slot would take 17 us
+// for 2400 lists of up to 8192 slots; instructions bound it (one slot per lane, with bits per slot: 107 us).
 constexpr int PLAN_BINS = 2048;
 constexpr int PLAN_FEW = 128;  // keys whose ranks are counted directly
 
@@ -231,7 +232,7 @@ struct PlanArgs {
 };
 
 __device__ __forceinline__ uint32_t plan_key(float w) {
-  if (w != w) return 0u;
+  if (w != w) return 1u;
   const uint32_t u = __float_as_uint(w + 0.0f);
   return (u & 0x80000000u) ? ~u : (u | 0x80000000u);  // -inf is 0x007fffff: above NaN
 }
@@ -260,85 +261,109 @@ __global__ void __launch_bounds__(THREADS) kv_evict_plan_kernel(const PlanArgs a
     if (threadIdx.x == 0) a.count[list] = 0;
     return;
   }
-  const int words = (n + 31) >> 5;
+  const int slot_mask = (1 << c.page_shift) - 1, quads = (n + 3) >> 2;
   const bool cached = n <= a.smem_slots;
-  uint32_t* key_s = reinterpret_cast<uint32_t*>(plan_smem);        // [min(n, smem_slots)]
-  uint32_t* prot_s = key_s + a.smem_slots;                         // [words] bit per slot: protected
-  uint32_t* keep_s = prot_s + (static_cast<int>(room) + 31) / 32;  // [words] bit per slot: stays
-  const int recent_from = seen > a.recent ? seen - a.recent : 0, slot_mask = (1 << c.page_shift) - 1;
+  uint4* key_s = reinterpret_cast<uint4*>(plan_smem);  // [quads]
+  const int recent_from = seen > a.recent ? seen - a.recent : 0;
   const int* pages = c.page_table + static_cast<long long>(s) * c.max_pages;
-  auto key_at = [&](int t) -> uint32_t {
-    return cached ? key_s[t] : plan_key(c.mass[kv_row(c, layer, pages[t >> c.page_shift], head) + (t & slot_mask)]);
+  const long long base = kv_row(c, layer, 0, head);  // pool row of slot 0 of page 0
+  const float* mass = c.mass + base;
+  const int* pos = c.pos + base;
+  const int page_rows = c.n_kv << c.page_shift;
+  // Keys of slots 4 i .. 4 i + 3 when protected slots stay (or, `swap`, compete while the free ones go); lo, hi: range of the
+  // keys that compete; n_p: protected slots.
+  auto keys_of = [&](int i, bool swap, const float4& m, const int4& ps, uint32_t& lo, uint32_t& hi, int& n_p) {
+    const float mv[4] = {m.x, m.y, m.z, m.w};
+    const int pv[4] = {ps.x, ps.y, ps.z, ps.w};
+    uint32_t k[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const bool have = 4 * i + e < n, p = pv[e] >= recent_from || pv[e] < a.sink;
+      k[e] = plan_key(mv[e]);
+      const bool in = have && p == swap;
+      lo = in ? min(lo, k[e]) : lo;
+      hi = in ? max(hi, k[e]) : hi;
+      n_p += have && p;
+      k[e] = in ? k[e] : have && p ? 0xffffffffu : 0u;
+    }
+    return make_uint4(k[0], k[1], k[2], k[3]);
   };
-  if (threadIdx.x == 0) {
-    n_prot = 0;
-    group_lo = 0xffffffffu;
-    group_hi = 0u;
-  }
-  // ---- read every slot once: key, protected bit, range of the keys of either group
-  int prot = 0;
-  uint32_t lo[2] = {0xffffffffu, 0xffffffffu}, hi[2] = {0u, 0u};  // free, protected
-  bool bad = false;
-  for (int w = warp; w < words; w += 4 * WARPS) {
-    int page[4], ps[4];
-    float m[4];
+  auto at_quad = [&](int i, int page) { return static_cast<long long>(page) * page_rows + ((4 * i) & slot_mask); };
+  bool swap = false, bad = false;
+  int P = 0;
+  uint32_t from, to;  // the threshold key lies in from .. to; `want` slots of that range stay
+  while (true) {
+    if (threadIdx.x == 0) {
+      n_prot = 0;
+      group_lo = 0xffffffffu;
+      group_hi = 0u;
+    }
+    __syncthreads();
+    int prot = 0;
+    uint32_t lo = 0xffffffffu, hi = 0u;
+    for (int i0 = threadIdx.x; i0 < quads; i0 += 2 * THREADS) {
+      int page[2];
+      float4 m[2];
+      int4 ps[2];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int t = 32 * (w + i * WARPS) + lane;
-      page[i] = t < n ? pages[t >> c.page_shift] : 0;
-      if (page[i] < 0 || page[i] >= c.n_pages) {
-        bad = true;
-        page[i] = 0;
+      for (int j = 0; j < 2; ++j) {
+        const int i = i0 + j * THREADS;
+        page[j] = i < quads ? pages[(4 * i) >> c.page_shift] : 0;
+        if (page[j] < 0 || page[j] >= c.n_pages) {
+          bad = true;
+          page[j] = 0;
+        }
+      }
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const long long at = at_quad(i0 + j * THREADS, page[j]);
+        m[j] = *reinterpret_cast<const float4*>(mass + at);
+        ps[j] = *reinterpret_cast<const int4*>(pos + at);
+      }
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const int i = i0 + j * THREADS;
+        if (i >= quads) break;
+        const uint4 k = keys_of(i, swap, m[j], ps[j], lo, hi, prot);
+        if (cached) key_s[i] = k;
       }
     }
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int t = 32 * (w + i * WARPS) + lane;
-      const long long r = kv_row(c, layer, page[i], head) + (t & slot_mask);
-      ps[i] = t < n ? c.pos[r] : INT_MAX;
-      m[i] = t < n ? c.mass[r] : 0.0f;
-    }
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int at = w + i * WARPS, t = 32 * at + lane;
-      if (at >= words) break;
-      const bool p = t < n && (ps[i] >= recent_from || ps[i] < a.sink);
-      const uint32_t bits = __ballot_sync(0xffffffffu, p), key = plan_key(m[i]);
-      if (t < n) {
-        if (cached) key_s[t] = key;
-        lo[0] = p ? lo[0] : min(lo[0], key);
-        hi[0] = p ? hi[0] : max(hi[0], key);
-        lo[1] = p ? min(lo[1], key) : lo[1];
-        hi[1] = p ? max(hi[1], key) : hi[1];
-      }
-      if (lane == 0) prot_s[at] = bits;
-      prot += __popc(bits);
-    }
-  }
-  if (__syncthreads_or(bad)) {
-    if (threadIdx.x == 0) { report_status(BITRL_ERR_SHAPE, KV_STAGE_BAD_PAGE); a.count[list] = 0; }
-    return;
-  }
-  if (lane == 0 && prot) atomicAdd(&n_prot, prot);
-  __syncthreads();
-  const bool among_protected = n_prot >= B;  // which group the threshold lies in
-  int want = among_protected ? B : B - n_prot;  // slots of that group that stay
-  {
-    const uint32_t l = __reduce_min_sync(0xffffffffu, lo[among_protected]), h = __reduce_max_sync(0xffffffffu, hi[among_protected]);
+    prot = warp_sum_i(prot);
+    lo = __reduce_min_sync(0xffffffffu, lo);
+    hi = __reduce_max_sync(0xffffffffu, hi);
     if (lane == 0) {
-      atomicMin(&group_lo, l);
-      atomicMax(&group_hi, h);
+      atomicAdd(&n_prot, prot);
+      atomicMin(&group_lo, lo);
+      atomicMax(&group_hi, hi);
     }
+    if (__syncthreads_or(bad)) {
+      if (threadIdx.x == 0) { report_status(BITRL_ERR_SHAPE, KV_STAGE_BAD_PAGE); a.count[list] = 0; }
+      return;
+    }
+    P = n_prot;
+    from = group_lo;
+    to = group_hi;
+    if (swap || P < B) break;
+    swap = true;
+    __syncthreads();
   }
-  __syncthreads();
-  uint32_t from = group_lo, to = group_hi;  // the threshold key lies in from .. to; `want` slots of that range stay
+  int want = swap ? B : B - P;
+  auto keys_at = [&](int i) -> uint4 {  // i < quads
+    if (cached) return key_s[i];
+    const long long at = at_quad(i, pages[(4 * i) >> c.page_shift]);
+    uint32_t lo = 0u, hi = 0u;
+    int n_p = 0;
+    return keys_of(i, swap, *reinterpret_cast<const float4*>(mass + at), *reinterpret_cast<const int4*>(pos + at), lo, hi, n_p);
+  };
   uint32_t thr = from;
   int at_thr = 0;  // slots whose key is the threshold
-  // words of this warp, as `in` flags with their keys
   auto each = [&](auto&& f) {
-    for (int w = warp; w < words; w += WARPS) {
-      const int t = 32 * w + lane;
-      if (t < n && (((prot_s[w] >> lane) & 1u) != 0) == among_protected) f(key_at(t));
+    for (int i = threadIdx.x; i < quads; i += THREADS) {
+      const uint4 k = keys_at(i);
+      f(k.x);
+      f(k.y);
+      f(k.z);
+      f(k.w);
     }
   };
   while (true) {
@@ -348,7 +373,7 @@ __global__ void __launch_bounds__(THREADS) kv_evict_plan_kernel(const PlanArgs a
     if (threadIdx.x == 0) n_few = 0;
     __syncthreads();
     each([&](uint32_t key) {
-      if (key >= from && key <= to) atomicAdd(&hist[(key - from) >> shift], 1);
+      if (key - from <= span && key - 1u < 0xfffffffeu) atomicAdd(&hist[(key - from) >> shift], 1);
     });
     __syncthreads();
     // steps from the top: thread i owns PLAN_BINS / THREADS of them
@@ -385,11 +410,15 @@ __global__ void __launch_bounds__(THREADS) kv_evict_plan_kernel(const PlanArgs a
       break;
     }
     if (left <= PLAN_FEW) {
+      const uint32_t width = to - from;
       each([&](uint32_t key) {
-        if (key >= from && key <= to) few[atomicAdd(&n_few, 1)] = key;
+        if (key - from <= width && key - 1u < 0xfffffffeu) {
+          const int at = atomicAdd(&n_few, 1);
+          if (at < PLAN_FEW) few[at] = key;  // more only if another stream changes the weights meanwhile
+        }
       });
       __syncthreads();
-      if (threadIdx.x < left) {
+      if (static_cast<int>(threadIdx.x) < left) {
         const uint32_t key = few[threadIdx.x];
         int greater = 0, equal = 0;
         for (int i = 0; i < left; ++i) {
@@ -410,38 +439,56 @@ __global__ void __launch_bounds__(THREADS) kv_evict_plan_kernel(const PlanArgs a
     }
   }
 
-  // ---- ordered decision: every warp owns a run of words.  Of the at_thr slots that equal the threshold the `want` lowest stay.
-  const int per_warp = (words + WARPS - 1) / WARPS, w0 = warp * per_warp, w1 = min(words, w0 + per_warp);
-  int tie_rank = 0;
-  if (want < at_thr) {
-    int ties = 0;
-    for (int w = w0; w < w1; ++w) {
-      const int t = 32 * w + lane;
-      const bool in = t < n && (((prot_s[w] >> lane) & 1u) != 0) == among_protected;
-      ties += __popc(__ballot_sync(0xffffffffu, in && key_at(t) == thr));
+  // ---- ordered passes: every warp owns a run of 128-slot blocks.  Of the at_thr slots that equal the threshold the `want`
+  // lowest stay; as a rule that is all of them and no ranks are needed.
+  const int blocks = (n + 127) >> 7, per_warp = (blocks + WARPS - 1) / WARPS, b0 = warp * per_warp, b1 = min(blocks, b0 + per_warp);
+  const bool ranked = want < at_thr;
+  auto equal_bits = [&](const uint4& k) {
+    return (k.x == thr ? 1u : 0u) | (k.y == thr ? 2u : 0u) | (k.z == thr ? 4u : 0u) | (k.w == thr ? 8u : 0u);
+  };
+  auto inclusive = [&](int v) {
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int u = __shfl_up_sync(0xffffffffu, v, o);
+      if (lane >= o) v += u;
     }
-    __syncthreads();
-    if (lane == 0) part[warp] = ties;
-    __syncthreads();
-    for (int w = 0; w < warp; ++w) tie_rank += part[w];
-  }
-  int n_src = 0, n_dst = 0;
-  for (int w = w0; w < w1; ++w) {
-    const int t = 32 * w + lane;
-    const bool p = ((prot_s[w] >> lane) & 1u) != 0, in = t < n && p == among_protected;
-    const uint32_t key = in ? key_at(t) : 0u;
-    bool keep = (p && !among_protected) || (in && key >= thr);
-    if (want < at_thr) {
-      const uint32_t tie = __ballot_sync(0xffffffffu, in && key == thr);
-      if (in && key == thr) keep = tie_rank + __popc(tie & ((1u << lane) - 1u)) < want;
-      tie_rank += __popc(tie);
+    return v;
+  };
+  // Bits of this lane's four slots that stay; advances `ties`, the slots equal to the threshold so far.
+  auto keep_bits = [&](int i, int& ties) -> uint32_t {
+    const uint4 k = i < quads ? keys_at(i) : make_uint4(0u, 0u, 0u, 0u);
+    uint32_t keep = (k.x >= thr ? 1u : 0u) | (k.y >= thr ? 2u : 0u) | (k.z >= thr ? 4u : 0u) | (k.w >= thr ? 8u : 0u);
+    if (thr == 0u) keep &= (k.x ? 1u : 0u) | (k.y ? 2u : 0u) | (k.z ? 4u : 0u) | (k.w ? 8u : 0u);
+    if (ranked) {
+      const uint32_t eq = equal_bits(k);
+      const int incl = inclusive(__popc(eq)), room_left = want - ties - (incl - __popc(eq));  // of this lane's ties so many stay
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (((eq >> e) & 1u) && __popc(eq & ((1u << e) - 1u)) >= room_left) keep &= ~(1u << e);
+      ties += __shfl_sync(0xffffffffu, incl, 31);
     }
-    const uint32_t kept = __ballot_sync(0xffffffffu, keep);
-    if (lane == 0) keep_s[w] = kept;
-    const uint32_t below = 32 * w + 32 <= B ? 0xffffffffu : 32 * w >= B ? 0u : (1u << (B - 32 * w)) - 1u;  // slots < B
-    n_src += __popc(kept & ~below);
-    n_dst += __popc(~kept & below);
+    return keep;
+  };
+  auto low_bits = [&](int i) { return 4 * i + 4 <= B ? 15u : 4 * i >= B ? 0u : (1u << (B - 4 * i)) - 1u; };  // slots < B
+  int ties0 = 0;
+  if (ranked) {
+    int mine = 0;
+    for (int b = b0; b < b1; ++b)
+      if (32 * b + lane < quads) mine += __popc(equal_bits(keys_at(32 * b + lane)));
+    mine = warp_sum_i(mine);
+    __syncthreads();
+    if (lane == 0) part[warp] = mine;
+    __syncthreads();
+    for (int w = 0; w < warp; ++w) ties0 += part[w];
   }
+  int n_src = 0, n_dst = 0, ties = ties0;
+  for (int b = b0; b < b1; ++b) {
+    const uint32_t keep = keep_bits(32 * b + lane, ties), low = low_bits(32 * b + lane);
+    n_src += __popc(keep & ~low);
+    n_dst += __popc(~keep & low);
+  }
+  n_src = warp_sum_i(n_src);
+  n_dst = warp_sum_i(n_dst);
   __syncthreads();
   if (lane == 0) { part[warp] = n_src; part2[warp] = n_dst; }
   __syncthreads();
@@ -453,23 +500,28 @@ __global__ void __launch_bounds__(THREADS) kv_evict_plan_kernel(const PlanArgs a
     a.count[list] = total;
   }
   int* out = a.moves + static_cast<long long>(list) * a.max_moves * 2;
-  for (int w = w0; w < w1; ++w) {
-    const uint32_t kept = keep_s[w], below = 32 * w + 32 <= B ? 0xffffffffu : 32 * w >= B ? 0u : (1u << (B - 32 * w)) - 1u;
-    const uint32_t bs = kept & ~below, bd = ~kept & below, mine = 1u << lane;
-    if (bs & mine) out[2 * (at_src + __popc(bs & (mine - 1u)))] = 32 * w + lane;
-    if (bd & mine) out[2 * (at_dst + __popc(bd & (mine - 1u))) + 1] = 32 * w + lane;
-    at_src += __popc(bs);
-    at_dst += __popc(bd);
+  ties = ties0;
+  for (int b = b0; b < b1; ++b) {
+    const int i = 32 * b + lane;
+    const uint32_t keep = keep_bits(i, ties), low = low_bits(i);
+    uint32_t src = keep & ~low, dst = ~keep & low;
+    const int mine = __popc(src) | (__popc(dst) << 16);
+    const int incl = inclusive(mine), before = incl - mine, all = __shfl_sync(0xffffffffu, incl, 31);
+    int js = at_src + (before & 0xffff), jd = at_dst + (before >> 16);
+    for (; src; src &= src - 1u) out[2 * js++] = 4 * i + __ffs(src) - 1;
+    for (; dst; dst &= dst - 1u) out[2 * jd++ + 1] = 4 * i + __ffs(dst) - 1;
+    at_src += all & 0xffff;
+    at_dst += all >> 16;
   }
 }
 
 template <int THREADS>
-bitrl_status launch_kv_evict_plan_t(const PlanArgs& a, size_t smem, size_t limit, unsigned lists, cudaStream_t st) {
+bitrl_status launch_kv_evict_plan_t(const PlanArgs& a, size_t smem, int limit, unsigned lists, cudaStream_t st) {
   static bool done[64] = {false};
   int dev = 0;
   BITRL_CUDA(cudaGetDevice(&dev));
   if (dev >= 0 && dev < 64 && !done[dev]) {
-    BITRL_CUDA(cudaFuncSetAttribute(kv_evict_plan_kernel<THREADS>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(limit)));
+    BITRL_CUDA(cudaFuncSetAttribute(kv_evict_plan_kernel<THREADS>, cudaFuncAttributeMaxDynamicSharedMemorySize, limit));
     done[dev] = true;
   }
   BITRL_CUDA(launch_pdl(kv_evict_plan_kernel<THREADS>, dim3(lists), dim3(THREADS), smem, st, a));
@@ -481,12 +533,9 @@ bitrl_status launch_kv_evict_plan(const KvView& c, int budget, int recent, int s
                                   cudaStream_t st) {
   PlanArgs a{c, budget, recent, sink, max_moves, moves, count, 0};
   const int room = c.max_pages << c.page_shift;
-  const size_t bits = static_cast<size_t>((room + 31) / 32) * 8;  // two bit arrays
-  constexpr size_t LIMIT = 200 * 1024;
-  if (bits > LIMIT) return BITRL_ERR_LIMIT;
-  const size_t left = (LIMIT - bits) / 4;
-  a.smem_slots = static_cast<int>(left < static_cast<size_t>(room) ? left : room);
-  const size_t smem = static_cast<size_t>(a.smem_slots) * 4 + bits;
+  constexpr int LIMIT = 200 * 1024;
+  a.smem_slots = room < LIMIT / 4 ? room : LIMIT / 4;
+  const size_t smem = static_cast<size_t>(a.smem_slots) * 4;
   const long long lists = static_cast<long long>(c.n_layers) * c.n_seq * c.n_kv;
   // few lists: more threads on each
   return lists <= 2 * sm_count() ? launch_kv_evict_plan_t<512>(a, smem, LIMIT, static_cast<unsigned>(lists), st)
