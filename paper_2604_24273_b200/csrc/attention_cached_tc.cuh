@@ -605,9 +605,9 @@ __global__ void __launch_bounds__(256) attn_tiles_join_kernel(const __grid_const
 // fixed order and without a word to other threads.  An item is 256 slots (two tiles) of one kv head, a unit is one row tile;
 // an item that is cut between CTAs leaves partial sums that attn_mass_join_kernel adds in order.
 //   warp 0 producer (keys of an item, double-buffered; queries through a ring of two), warp 1 MMA (two accumulators per key
-//   tile), warp 2 row statistics, warps 4-7 and 8-11 the sums of key tile 0 and 1.
+//   tile), warp 2 row statistics, warps 4-11 and 12-19 the sums of key tile 0 and 1, four warps for every other unit.
 // Bound: 1024 cycles of exponentials per 128 x 128 tile (the products take 512) for long chunks; reading for short ones.
-constexpr int AM_THREADS = 384;
+constexpr int AM_THREADS = 640;
 constexpr int AM_KEYS = 256;
 enum { AM_WAIT_LOAD = 141, AM_WAIT_MMA = 142, AM_WAIT_LSE = 143, AM_WAIT_SUM = 144 };
 
@@ -615,9 +615,10 @@ template <int HD>
 struct AmSmem {
   static constexpr uint32_t TILE = 128 * HD * 2, HALF = 128 * 128;
   static constexpr uint32_t K = 0, Q = 4 * TILE, LSE = Q + 2 * TILE;  // K [2][2 tiles], Q [2], LSE [4][128]
-  static constexpr uint32_t LIVE = LSE + 4 * 512, BAR = LIVE + 64;    // LIVE [4][4] bits: columns that hold a row
+  static constexpr uint32_t LIVE = LSE + 4 * 512, SUM = LIVE + 64, BAR = SUM + 1024;  // LIVE [4][4] bits: columns that hold a row; SUM [2][128]
   static constexpr uint32_t K_FULL = BAR, K_EMPTY = K_FULL + 16, Q_FULL = K_EMPTY + 16, Q_EMPTY = Q_FULL + 16, S_FULL = Q_EMPTY + 16,
-                            S_EMPTY = S_FULL + 32, L_FULL = S_EMPTY + 32, L_EMPTY = L_FULL + 32, DRAIN = L_EMPTY + 32;
+                            S_EMPTY = S_FULL + 32, L_FULL = S_EMPTY + 32, L_EMPTY = L_FULL + 32, SUM_FULL = L_EMPTY + 32, SUM_EMPTY = SUM_FULL + 16,
+                            DRAIN = SUM_EMPTY + 16;
   static constexpr uint32_t MISC = DRAIN + 8, RUN = MISC + 8, PART = RUN + 32;
   static constexpr uint32_t BYTES = PART + 8 * (AM_THREADS / 32 + 1) + 1024;
   static constexpr uint32_t LAUNCH = BYTES > 120 * 1024 ? BYTES : 120 * 1024;  // one CTA per SM: it takes all of tensor memory
@@ -666,12 +667,14 @@ attn_mass_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_consta
       ptx::mbar_init(base + M::K_EMPTY + 8 * i, 1);
       ptx::mbar_init(base + M::Q_FULL + 8 * i, 1);
       ptx::mbar_init(base + M::Q_EMPTY + 8 * i, 1);
+      ptx::mbar_init(base + M::SUM_FULL + 8 * i, 4);
+      ptx::mbar_init(base + M::SUM_EMPTY + 8 * i, 4);
     }
     for (int i = 0; i < 4; ++i) {
       ptx::mbar_init(base + M::S_FULL + 8 * i, 1);
       ptx::mbar_init(base + M::S_EMPTY + 8 * i, 4);
       ptx::mbar_init(base + M::L_FULL + 8 * i, 1);
-      ptx::mbar_init(base + M::L_EMPTY + 8 * i, 8);
+      ptx::mbar_init(base + M::L_EMPTY + 8 * i, 16);
     }
     ptx::mbar_init(base + M::DRAIN, 1);
     ptx::mbar_init_fence();
@@ -802,37 +805,51 @@ attn_mass_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_consta
     if (!ok && lane == 0) give_up(AM_WAIT_LSE);
   } else if (warp >= 4) {
     // ------------------------------------------------------------------ sums, one slot per thread
-    const int x = (warp - 4) >> 2;
+    const int x = (warp - 4) >> 3, turn = ((warp - 4) >> 2) & 1;  // key tile; every other unit (its accumulator is `turn`)
     const uint32_t lane_base = static_cast<uint32_t>((warp & 3) * 32) << 16;
     const int r = (warp & 3) * 32 + lane;
     const uint64_t scale_x2 = ptx::pack_f32x2(__float_as_uint(a.scale2), __float_as_uint(a.scale2));
-    uint32_t un = 0, n = 0;
+    const uint32_t s_addr = tmem + 256 * x + 128 * turn + lane_base, s_bar = 8 * (2 * x + turn);
+    float* other = reinterpret_cast<float*>(sm + M::SUM) + 128 * x + r;
+    uint32_t un = 0, n = 0, mine = 0, items = 0;  // units of this key tile, of all items, of this warp's turn; items of this key tile
     while (ok && more) {
       const bool active = x < key_tiles();
-      const int slot = w.x * AM_KEYS + 128 * x + r, j = slot - q.used;
+      const int slot = w.x * AM_KEYS + 128 * x + r, j = slot - q.used, end = q.used + q.m;
+      const bool whole = w.u0 == 0 && w.u1 == w.units;
+      // where the sum goes, and what is there: read ahead of the sums
+      long long row = -1;
+      float before = 0.0f;
+      if (active && turn == 0 && slot < end && whole) {
+        const int page = kv_page(a.c, w.s, slot);
+        if (page >= 0) {
+          row = kv_row(a.c, 0, page, w.h) + (slot & ((1 << a.c.page_shift) - 1));
+          before = a.c.mass[row];
+        }
+      }
       float got[4] = {0.0f, 0.0f, 0.0f, 0.0f};
       for (int u = w.u0; u < w.u1; ++u, ++n) {
         const uint32_t b = n & 3;
         if (!(ok = wait(M::L_FULL + 8 * b, (n >> 2) & 1))) break;
-        if (active) {
-          const uint32_t sb = un & 1;
-          if (!(ok = wait(M::S_FULL + 8 * (2 * x + sb), (un >> 1) & 1))) break;
-          ++un;
+        if (active && (un++ & 1) == static_cast<uint32_t>(turn)) {
+          if (!(ok = wait(M::S_FULL + s_bar, mine & 1))) break;
+          ++mine;
           ptx::tc_fence_after_sync();
-          uint32_t s[4][32];
           const int rows = rows_of(u);
-#pragma unroll
-          for (int c = 0; c < 4; ++c)
-            if (32 * c < rows) ptx::tmem_ld_32x32b_x32(tmem + 256 * x + 128 * sb + 32 * c + lane_base, s[c]);
-          ptx::tmem_ld_wait();
-          ptx::tc_fence_before_sync();
-          __syncwarp();
-          if (lane == 0) ptx::mbar_arrive(base + M::S_EMPTY + 8 * (2 * x + sb));
           const int tok0 = (first + u) * tok_tile, last_slot = w.x * AM_KEYS + 128 * x + 127;
           const bool masked = last_slot >= q.used + (a.b.parent ? 0 : tok0 + 1);
+          uint32_t s[2][32];
+          ptx::tmem_ld_32x32b_x32(s_addr, s[0]);
 #pragma unroll
           for (int c = 0; c < 4; ++c) {
             if (32 * c >= rows) break;
+            ptx::tmem_ld_wait();
+            if (32 * c + 32 < rows) {
+              ptx::tmem_ld_32x32b_x32(s_addr + 32 * (c + 1), s[(c + 1) & 1]);
+            } else {
+              ptx::tc_fence_before_sync();
+              __syncwarp();
+              if (lane == 0) ptx::mbar_arrive(base + M::S_EMPTY + s_bar);
+            }
             uint32_t see = ptx::lds32(base + M::LIVE + 16 * b + 4 * c);
             const uint32_t lse = base + M::LSE + 512 * b + 128 * c;
             if (masked && j >= 0) {
@@ -842,14 +859,16 @@ attn_mass_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_consta
                 const int from = (j - tok0) * a.rep - 32 * c;  // rows from token j on
                 can = from >= 32 ? 0u : from <= 0 ? 0xffffffffu : 0xffffffffu << from;
               } else if (j < q.m) {
+                // the (at most 32) tokens of the chunk as bits, then each bit on the columns of its token
                 const uint32_t* who = a.desc + static_cast<long long>(q.t0 + j) * AC_TREE_WORDS;
-                for (int tk = 32 * c / a.rep; tk * a.rep < 32 * c + 32; ++tk) {
-                  const int tok = tok0 + tk, lo = tk * a.rep - 32 * c;
-                  if (tk >= tok_tile || tok >= q.m) break;
-                  if (((who[tok >> 5] >> (tok & 31)) & 1u) == 0) continue;
-                  const int from = max(lo, 0), n = min(lo + a.rep, 32) - from;
-                  can |= (n >= 32 ? 0xffffffffu : (1u << n) - 1u) << from;
-                }
+                const int t0 = tok0 + 32 * c / a.rep, at = t0 >> 5;
+                const uint32_t bits = __funnelshift_r(who[at], at + 1 < AC_TREE_WORDS ? who[at + 1] : 0u, t0 & 31);
+                int lo = (t0 - tok0) * a.rep - 32 * c;  // first column of token t0: at or before the chunk's first
+                for (uint32_t left = bits; lo < 32; lo += a.rep, left >>= 1)
+                  if (left & 1u) {
+                    const int from = max(lo, 0), cnt = min(lo + a.rep, 32) - from;
+                    can |= (cnt >= 32 ? 0xffffffffu : (1u << cnt) - 1u) << from;
+                  }
               }
               see &= can;
             }
@@ -858,19 +877,19 @@ attn_mass_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_consta
               for (int i = 0; i < 32; i += 4) {
                 const uint4 e = ptx::lds128(lse + 4 * i);
                 float p[4];
-                ptx::unpack_f32x2(ptx::fma_f32x2(ptx::pack_f32x2(s[c][i], s[c][i + 1]), scale_x2, ptx::pack_f32x2(e.x, e.y)), p[0], p[1]);
-                ptx::unpack_f32x2(ptx::fma_f32x2(ptx::pack_f32x2(s[c][i + 2], s[c][i + 3]), scale_x2, ptx::pack_f32x2(e.z, e.w)), p[2], p[3]);
+                ptx::unpack_f32x2(ptx::fma_f32x2(ptx::pack_f32x2(s[c & 1][i], s[c & 1][i + 1]), scale_x2, ptx::pack_f32x2(e.x, e.y)), p[0], p[1]);
+                ptx::unpack_f32x2(ptx::fma_f32x2(ptx::pack_f32x2(s[c & 1][i + 2], s[c & 1][i + 3]), scale_x2, ptx::pack_f32x2(e.z, e.w)), p[2], p[3]);
 #pragma unroll
                 for (int k = 0; k < 4; ++k) got[k] += ac_exp2(p[k]);
               }
-            } else {
+            } else if (__any_sync(0xffffffffu, see != 0u)) {
 #pragma unroll
               for (int i = 0; i < 32; i += 4) {
                 const uint4 e = ptx::lds128(lse + 4 * i);
                 const uint32_t ev[4] = {e.x, e.y, e.z, e.w};
 #pragma unroll
                 for (int k = 0; k < 4; ++k)
-                  if ((see >> (i + k)) & 1u) got[k] += ac_exp2(fmaf(__uint_as_float(s[c][i + k]), a.scale2, __uint_as_float(ev[k])));
+                  if ((see >> (i + k)) & 1u) got[k] += ac_exp2(fmaf(__uint_as_float(s[c & 1][i + k]), a.scale2, __uint_as_float(ev[k])));
               }
             }
           }
@@ -879,16 +898,28 @@ attn_mass_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_consta
         if (lane == 0) ptx::mbar_arrive(base + M::L_EMPTY + 8 * b);
       }
       if (!ok) break;
-      const float sum = (got[0] + got[1]) + (got[2] + got[3]);
-      if (w.u0 == 0 && w.u1 == w.units) {
-        if (slot < q.used + q.m) {
-          const int page = kv_page(a.c, w.s, slot);
-          if (page >= 0) a.c.mass[kv_row(a.c, 0, page, w.h) + (slot & ((1 << a.c.page_shift) - 1))] += sum;
+      float sum = (got[0] + got[1]) + (got[2] + got[3]);
+      if (active) {
+        // turn 1 hands its sum to turn 0
+        if (turn == 1) {
+          if (!(ok = wait(M::SUM_EMPTY + 8 * x, (items & 1) ^ 1))) break;
+          *other = sum;
+          __syncwarp();
+          if (lane == 0) ptx::mbar_arrive(base + M::SUM_FULL + 8 * x);
+        } else {
+          if (!(ok = wait(M::SUM_FULL + 8 * x, items & 1))) break;
+          sum += *other;
+          __syncwarp();
+          if (lane == 0) ptx::mbar_arrive(base + M::SUM_EMPTY + 8 * x);
+          if (whole) {
+            if (row >= 0) a.c.mass[row] = before + sum;
+          } else {
+            const int cut = w.u0 == 0 ? 1 : 0;
+            t.part[(2 * static_cast<long long>(blockIdx.x) + cut) * AM_KEYS + 128 * x + r] = sum;
+            if (threadIdx.x == 128) cuts[cut] = AtCut{w.s, w.x, w.h, w.u1 == w.units};
+          }
         }
-      } else {
-        const int cut = w.u0 == 0 ? 1 : 0;
-        t.part[(2 * static_cast<long long>(blockIdx.x) + cut) * AM_KEYS + 128 * x + r] = sum;
-        if (threadIdx.x == 128) cuts[cut] = AtCut{w.s, w.x, w.h, w.u1 == w.units};
+        ++items;
       }
       more = w.next(cost);
       __syncwarp();

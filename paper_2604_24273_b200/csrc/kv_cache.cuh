@@ -291,7 +291,7 @@ __global__ void __launch_bounds__(THREADS) kv_evict_plan_kernel(const PlanArgs a
   auto at_quad = [&](int i, int page) { return static_cast<long long>(page) * page_rows + ((4 * i) & slot_mask); };
   bool swap = false, bad = false;
   int P = 0;
-  uint32_t from, to;  // the threshold key lies in from .. to; `want` slots of that range stay
+  uint32_t from, to;  // the threshold key lies in from .. to, which neither 0 nor the greatest key does; `want` slots of that range stay
   while (true) {
     if (threadIdx.x == 0) {
       n_prot = 0;
@@ -373,7 +373,7 @@ __global__ void __launch_bounds__(THREADS) kv_evict_plan_kernel(const PlanArgs a
     if (threadIdx.x == 0) n_few = 0;
     __syncthreads();
     each([&](uint32_t key) {
-      if (key - from <= span && key - 1u < 0xfffffffeu) atomicAdd(&hist[(key - from) >> shift], 1);
+      if (key - from <= span) atomicAdd(&hist[(key - from) >> shift], 1);
     });
     __syncthreads();
     // steps from the top: thread i owns PLAN_BINS / THREADS of them
@@ -412,7 +412,7 @@ __global__ void __launch_bounds__(THREADS) kv_evict_plan_kernel(const PlanArgs a
     if (left <= PLAN_FEW) {
       const uint32_t width = to - from;
       each([&](uint32_t key) {
-        if (key - from <= width && key - 1u < 0xfffffffeu) {
+        if (key - from <= width) {
           const int at = atomicAdd(&n_few, 1);
           if (at < PLAN_FEW) few[at] = key;  // more only if another stream changes the weights meanwhile
         }
@@ -458,7 +458,6 @@ __global__ void __launch_bounds__(THREADS) kv_evict_plan_kernel(const PlanArgs a
   auto keep_bits = [&](int i, int& ties) -> uint32_t {
     const uint4 k = i < quads ? keys_at(i) : make_uint4(0u, 0u, 0u, 0u);
     uint32_t keep = (k.x >= thr ? 1u : 0u) | (k.y >= thr ? 2u : 0u) | (k.z >= thr ? 4u : 0u) | (k.w >= thr ? 8u : 0u);
-    if (thr == 0u) keep &= (k.x ? 1u : 0u) | (k.y ? 2u : 0u) | (k.z ? 4u : 0u) | (k.w ? 8u : 0u);
     if (ranked) {
       const uint32_t eq = equal_bits(k);
       const int incl = inclusive(__popc(eq)), room_left = want - ties - (incl - __popc(eq));  // of this lane's ties so many stay
