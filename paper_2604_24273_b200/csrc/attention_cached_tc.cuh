@@ -11,11 +11,14 @@ namespace bitrl {
 
 // ---- work lists ------------------------------------------------------------------------------------------------------
 // Lengths are known on the device alone, so the kernels cut their work there: pairs (sequence s, index x < nx), each
-// holding n_kv items (kv heads) of cost(s, x) units, form one list, and CTA c of G takes its units [N c / G, N (c+1) / G).
-// Every CTA then has the same share whatever the lengths are; an item may be cut between neighbours.
+// holding n_kv items (kv heads) of cost(s, x) units, form one list, and CTA c of G takes its share [N c / G, N (c+1) / G) of it.
+// Every CTA then has the same share whatever the lengths are; an item may be cut between neighbours.  What an item costs
+// beside its units (loading queries, writing results) counts as AC_LEAD units in front of them: without, CTAs with many
+// short items ended up to twice as late as the others.
+constexpr int AC_LEAD = 1;
 struct AcRun {
-  int s, x, h, u;   // first unit: item (s, x, h), unit u of it
-  long long left;   // units of this CTA
+  int s, x, h, u;   // first place: item (s, x, h), place u of it (AC_LEAD places, then its units)
+  long long left;   // places of this CTA
 };
 
 // All `n_threads` threads call it; `part` holds n_threads / 32 + 1 numbers of shared memory.  cost(s, x) >= 0.
@@ -26,7 +29,11 @@ __device__ __forceinline__ void ac_run_start(Cost cost, int n_seq, int nx, int n
   const long long per = (pairs + n_threads - 1) / n_threads;
   const long long p0 = min(pairs, per * threadIdx.x), p1 = min(pairs, p0 + per);
   long long sum = 0;
-  for (long long p = p0; p < p1; ++p) sum += cost(static_cast<int>(p / nx), static_cast<int>(p % nx));
+  auto places = [&](long long p) {
+    const int n = cost(static_cast<int>(p / nx), static_cast<int>(p % nx));
+    return n > 0 ? n + AC_LEAD : 0;
+  };
+  for (long long p = p0; p < p1; ++p) sum += places(p);
   long long incl = sum;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
@@ -46,7 +53,7 @@ __device__ __forceinline__ void ac_run_start(Cost cost, int n_seq, int nx, int n
   if (w0 < w1 && w0 >= excl && w0 < excl + sum * n_kv) {
     long long rem = w0 - excl;
     for (long long p = p0; p < p1; ++p) {
-      const int c = cost(static_cast<int>(p / nx), static_cast<int>(p % nx));
+      const int c = places(p);
       if (rem < static_cast<long long>(c) * n_kv) {
         *out = AcRun{static_cast<int>(p / nx), static_cast<int>(p % nx), static_cast<int>(rem / c), static_cast<int>(rem % c), w1 - w0};
         break;
@@ -57,57 +64,66 @@ __device__ __forceinline__ void ac_run_start(Cost cost, int n_seq, int nx, int n
   __syncthreads();
 }
 
-// Walks a run item by item: u0 .. u1 are the units of item (s, x, h) that belong to the run.
+// Walks a run item by item: u0 .. u1 (not empty) are the units of item (s, x, h) that belong to the run, of `units` in all.
 struct AcWalk {
   int s, x, h, u0, u1, units;
+  int place;
   long long left;
   int nx, n_kv, n_seq;
   __device__ __forceinline__ AcWalk(const AcRun& r, int nx_, int n_kv_, int n_seq_)
-      : s(r.s), x(r.x), h(r.h), u0(r.u), u1(0), units(0), left(r.left), nx(nx_), n_kv(n_kv_), n_seq(n_seq_) {}
+      : s(r.s), x(r.x), h(r.h), u0(0), u1(0), units(0), place(r.u), left(r.left), nx(nx_), n_kv(n_kv_), n_seq(n_seq_) {}
+  __device__ __forceinline__ bool take() {  // the part of the current item that lies in the run; false: it has no unit there
+    const int end = static_cast<int>(min(static_cast<long long>(units + AC_LEAD), place + left));
+    left -= end - place;
+    u0 = max(0, place - AC_LEAD);
+    u1 = max(0, end - AC_LEAD);
+    return u1 > u0;
+  }
   template <class Cost>
   __device__ __forceinline__ bool start(Cost cost) {
     if (left <= 0) return false;
     units = cost(s, x);
-    u1 = static_cast<int>(min(static_cast<long long>(units), u0 + left));
-    return true;
+    return take() || next(cost);
   }
   template <class Cost>
   __device__ __forceinline__ bool next(Cost cost) {
-    left -= u1 - u0;
-    if (left <= 0) return false;
-    u0 = 0;
-    if (++h == n_kv) {
-      h = 0;
-      do {
-        if (++x == nx) {
-          x = 0;
-          if (++s >= n_seq) return false;
-        }
-        units = cost(s, x);
-      } while (units == 0);
+    while (left > 0) {
+      place = 0;
+      if (++h == n_kv) {
+        h = 0;
+        do {
+          if (++x == nx) {
+            x = 0;
+            if (++s >= n_seq) return false;
+          }
+          units = cost(s, x);
+        } while (units == 0);
+      }
+      if (take()) return true;
     }
-    u1 = static_cast<int>(min(static_cast<long long>(units), left));
-    return true;
+    return false;
   }
 };
 
 // ---- forward -----------------------------------------------------------------------------------------------------------
 // An item is 256 rows (two tiles of 128, whole tokens each) of one kv head; a unit is 128 slots of its keys.  One CTA per SM:
 //   warp 0      producer: queries of an item (3-D TMA: dims x heads of the group x tokens), then per unit the keys and the
-//               values, page by page, 128-byte swizzled, through a ring of four tiles
-//   warp 1      MMA: S_a = Q_a K^T (128 x 128) and O_a += P_a V for the two row tiles a in turn; the softmax of one tile runs
-//               beside the products of the other.  P replaces S in tensor memory (A operand); V is the MN-major B operand.
-//   warps 2,3   make a unit's values harmless where some row must not see them: rows behind the last slot and of padding
+//               values, page by page, 128-byte swizzled, through a ring of five tiles
+//   warps 1, 2  MMA: S_a = Q_a K^T and O_a += P_a V for row tile a, 64 slots at a time (one issuer for both was what the
+//               kernel waited for: 2400 cycles a step, of which 1360 issuing and 1000 in waits); each row tile has two score
+//               buffers, so the scores of the next 64 slots are there when the softmax of the last 64 ends.  P replaces S in
+//               tensor memory (A operand); V is the MN-major B operand.  512 columns: 2 x (2 x 64 of S, 128 of O).
+//   warp 3      makes a unit's values harmless where some row must not see them: rows behind the last slot and of padding
 //               become zero, and so do values that are not finite (rows that do see them get them back at the end)
 //   warps 4-7, 8-11   softmax of row tile 0 / 1, one row per thread: no exchange between threads.  The running maximum is
 //               followed only when it has grown by more than 2^8 (weights stay below 2^8, statistics and sums are fp32), so
 //               the result is rescaled rarely.  Weights are rounded to bf16 for the product (2^-9 relative each, of random
 //               sign over the keys: below the rounding of the result itself); their sum is taken before the rounding.
-// Bound: 2 * 512 tensor cycles and 1024 cycles of exponentials per 128 x 128 tile for long chunks; the reading of keys and
-// values for up to ~100 rows.  Every wait is bounded; on expiry the CTA records a status word and leaves normally.
+// Bound: 1024 cycles of exponentials and as many of products per 128 x 128 tile for long chunks (scores take 3/4 of the rate
+// with 64 columns, as both operands come from shared memory); the reading of keys and values for few rows.  Every wait is bounded; on expiry the CTA records a status word and leaves normally.
 constexpr int AT_THREADS = 384;
 constexpr int AT_KEYS = 128;
-constexpr int AT_RING = 4;
+constexpr int AT_RING = 5;  // odd: a place holds keys and values in turn, so its V_READY barrier turns every second round
 constexpr float AT_GROWTH = 8.0f;
 enum { AT_WAIT_LOAD = 131, AT_WAIT_MMA = 132, AT_WAIT_SOFTMAX = 133, AT_WAIT_FIX = 134 };
 
@@ -116,10 +132,11 @@ struct AtSmem {
   static constexpr uint32_t TILE = 128 * HD * 2, HALF = 128 * 128;  // HALF: one 64-dimension block of a tile
   static constexpr uint32_t Q = 0, RING = 2 * TILE, BAR = RING + AT_RING * TILE;
   static constexpr uint32_t KV_FULL = BAR, KV_EMPTY = KV_FULL + 8 * AT_RING, Q_FULL = KV_EMPTY + 8 * AT_RING, Q_EMPTY = Q_FULL + 8,
-                            S_FULL = Q_EMPTY + 8, P_FULL = S_FULL + 16, O_FULL = P_FULL + 16, V_READY = O_FULL + 16, DRAIN = V_READY + 16;
+                            S_FULL = Q_EMPTY + 8, P_FULL = S_FULL + 32, O_DONE = P_FULL + 32, V_READY = O_DONE + 32, DRAIN = V_READY + 8 * AT_RING;
   static constexpr uint32_t MISC = DRAIN + 8;  // tensor-memory base, failed, odd[4]
   static constexpr uint32_t RUN = MISC + 32, PART = RUN + 32;
   static constexpr uint32_t BYTES = PART + 8 * (AT_THREADS / 32 + 1) + 1024;  // + slack to align the base
+  static_assert(AT_RING % 2 == 1 && BYTES <= 232448, "ring");
   // one CTA per SM: it takes all of tensor memory
   static constexpr uint32_t LAUNCH = BYTES > 120 * 1024 ? BYTES : 120 * 1024;
 };
@@ -178,16 +195,19 @@ attn_tiles_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
   if (threadIdx.x == 0) {
     *failed = 0u;
     for (int i = 0; i < 4; ++i) odd[i] = 0u;
-    for (int i = 0; i < AT_RING; ++i) { ptx::mbar_init(base + M::KV_FULL + 8 * i, 1); ptx::mbar_init(base + M::KV_EMPTY + 8 * i, 1); }
+    for (int i = 0; i < AT_RING; ++i) {
+      ptx::mbar_init(base + M::KV_FULL + 8 * i, 1);
+      ptx::mbar_init(base + M::KV_EMPTY + 8 * i, 2);
+      ptx::mbar_init(base + M::V_READY + 8 * i, 1);
+    }
     ptx::mbar_init(base + M::Q_FULL, 1);
-    ptx::mbar_init(base + M::Q_EMPTY, 1);
-    for (int i = 0; i < 2; ++i) {
+    ptx::mbar_init(base + M::Q_EMPTY, 2);
+    for (int i = 0; i < 4; ++i) {
       ptx::mbar_init(base + M::S_FULL + 8 * i, 1);
       ptx::mbar_init(base + M::P_FULL + 8 * i, 4);
-      ptx::mbar_init(base + M::O_FULL + 8 * i, 1);
-      ptx::mbar_init(base + M::V_READY + 8 * i, 2);
+      ptx::mbar_init(base + M::O_DONE + 8 * i, 1);
     }
-    ptx::mbar_init(base + M::DRAIN, 1);
+    ptx::mbar_init(base + M::DRAIN, 2);
     ptx::mbar_init_fence();
     ptx::tma_prefetch_desc(&tmap_q);
     ptx::tma_prefetch_desc(&tmap_k);
@@ -215,10 +235,13 @@ attn_tiles_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
   auto masked = [&](int u) {
     return (u + 1) * AT_KEYS > q.used + (a.b.parent ? 0 : w.x * 2 * tok_tile + 1);
   };
+  // 64-slot steps of the run's part of the item; the last unit may have one
+  auto steps_of = [&]() {
+    const int end = q.used + (a.b.parent ? q.m : min(q.m, (w.x + 1) * 2 * tok_tile));
+    return min(2 * (w.u1 - w.u0), (end - w.u0 * AT_KEYS + 63) / 64);
+  };
   bool more = w.start(cost);
   if (warp < 4) {
-  // 128 threads at 88 registers and 256 at 208: the launch's 384 at 168
-  ptx::regs_dec<88>();
   if (warp == 0) {
     // ------------------------------------------------------------------ producer
     uint32_t e = 0, qn = 0;  // tiles put into the ring; items
@@ -229,13 +252,6 @@ attn_tiles_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
     while (ok && more) {
       const int end = q.used + (a.b.parent ? q.m : min(q.m, (w.x + 1) * 2 * tok_tile));
       const int na = w.x * 2 * tok_tile + tok_tile < q.m ? 2 : 1;
-      if (!__any_sync(0xffffffffu, wait(M::Q_EMPTY, (qn & 1) ^ 1))) { ok = false; break; }
-      if (lane == 0) ptx::mbar_arrive_expect_tx(base + M::Q_FULL, na * NH * 128 * a.rep * tok_tile);
-      __syncwarp();
-      if (lane < na * NH)
-        ptx::tma_load_3d(base + M::Q + (lane / NH) * M::TILE + (lane % NH) * M::HALF, &tmap_q, 64 * (lane % NH), w.h * a.rep,
-                         q.t0 + (w.x * 2 + lane / NH) * tok_tile, base + M::Q_FULL);
-      ++qn;
       auto row_of = [&](int u) {  // first row of this lane's page of unit u
         const int slot = u * AT_KEYS + piece * page;
         if (piece >= pieces || slot >= end) return none;
@@ -254,6 +270,15 @@ attn_tiles_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
           if (piece < pieces)
             ptx::tma_load_2d(base + M::RING + slot * M::TILE + half * M::HALF + piece * page * 128, kv ? &tmap_v : &tmap_k, 64 * half,
                              row, base + M::KV_FULL + 8 * slot);
+          if (u == w.u0 && kv == 0) {  // the queries: the first keys need not wait for the place that the last item's leave
+            if (!__any_sync(0xffffffffu, wait(M::Q_EMPTY, (qn & 1) ^ 1))) { ok = false; break; }
+            if (lane == 0) ptx::mbar_arrive_expect_tx(base + M::Q_FULL, na * NH * 128 * a.rep * tok_tile);
+            __syncwarp();
+            if (lane < na * NH)
+              ptx::tma_load_3d(base + M::Q + (lane / NH) * M::TILE + (lane % NH) * M::HALF, &tmap_q, 64 * (lane % NH), w.h * a.rep,
+                               q.t0 + (w.x * 2 + lane / NH) * tok_tile, base + M::Q_FULL);
+            ++qn;
+          }
         }
         if (!ok) break;
         row = row_next;
@@ -262,71 +287,76 @@ attn_tiles_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
       __syncwarp();
     }
     if (!ok && lane == 0) give_up(AT_WAIT_LOAD);
-  } else if (warp == 1) {
-    // ------------------------------------------------------------------ MMA issuer
-    constexpr uint32_t id_s = ptx::idesc_bf16(128, AT_KEYS, false), id_o = ptx::idesc_bf16(128, HD, true);
-    uint32_t e = 0, qn = 0, pn[2] = {0, 0};
+  } else if (warp <= 2) {
+    // ------------------------------------------------------------------ MMA issuers: row tile x
+    constexpr uint32_t id_s = ptx::idesc_bf16(128, 64, false), id_o = ptx::idesc_bf16(128, HD, true);
+    const int x = warp - 1;
+    uint32_t e = 0, qn = 0, p_par = 0;  // p_par: phase of either P_FULL barrier, as bits
     bool ok = true;
     auto all_wait = [&](uint32_t bar, uint32_t parity) { return __any_sync(0xffffffffu, wait(bar, parity)); };
-    auto scores = [&](int x, uint32_t slot) {
-      if (ptx::elect_one()) {
-        const uint64_t qd = ptx::smem_desc_sw128(base + M::Q + x * M::TILE), kd = ptx::smem_desc_sw128(base + M::RING + slot * M::TILE);
-#pragma unroll
-        for (int k = 0; k < HD / 16; ++k) {
-          const uint32_t off = ((k / 4) * M::HALF + (k % 4) * 32) >> 4;
-          ptx::mma_bf16_ss(tmem + 128 * x, qd + off, kd + off, id_s, k != 0);
-        }
-        ptx::mma_commit(base + M::S_FULL + 8 * x);
-      }
-      __syncwarp();
-    };
+    auto full_wait = [&](uint32_t at) { return all_wait(M::KV_FULL + 8 * (at % AT_RING), (at / AT_RING) & 1); };
     auto commit = [&](uint32_t bar) {
       if (ptx::elect_one()) ptx::mma_commit(base + bar);
       __syncwarp();
     };
-    while (ok && more) {
-      const int na = w.x * 2 * tok_tile + tok_tile < q.m ? 2 : 1;
-      ok = all_wait(M::Q_FULL, qn & 1) && all_wait(M::KV_FULL + 8 * (e % AT_RING), (e / AT_RING) & 1);
-      if (!ok) break;
-      ++qn;
-      ptx::tc_fence_after_sync();
-      for (int x = 0; x < na; ++x) scores(x, e % AT_RING);
-      commit(M::KV_EMPTY + 8 * (e % AT_RING));
-      if (w.u1 - w.u0 == 1) commit(M::Q_EMPTY);
-      ++e;
-      for (int u = w.u0; ok && u < w.u1; ++u) {
-        const uint32_t v_slot = e % AT_RING, v_par = (e / AT_RING) & 1, k_slot = (e + 1) % AT_RING;
-        const bool last = u + 1 == w.u1;
-        ok = all_wait(M::V_READY + 8 * (v_slot >> 1), v_par);
-        for (int x = 0; ok && x < na; ++x) {
-          ok = all_wait(M::P_FULL + 8 * x, pn[x] & 1);
-          if (!ok) break;
-          ++pn[x];
-          ptx::tc_fence_after_sync();
-          if (ptx::elect_one()) {
-            const uint64_t vd = ptx::smem_desc_mn_sw128(base + M::RING + v_slot * M::TILE, M::HALF);
+    auto scores = [&](uint32_t slot, int b) {  // half b of the keys in `slot`
+      if (ptx::elect_one()) {
+        const uint64_t qd = ptx::smem_desc_sw128(base + M::Q + x * M::TILE), kd = ptx::smem_desc_sw128(base + M::RING + slot * M::TILE + b * 8192);
 #pragma unroll
-            for (int k = 0; k < AT_KEYS / 16; ++k)
-              ptx::mma_bf16_ts(tmem + 256 + 128 * x, tmem + 128 * x + 8 * k, vd + k * (2048 >> 4), id_o, u != w.u0 || k != 0);
-            if (last) ptx::mma_commit(base + M::O_FULL + 8 * x);
-          }
-          __syncwarp();
-          if (!last) {
-            if (x == 0) ok = all_wait(M::KV_FULL + 8 * k_slot, ((e + 1) / AT_RING) & 1);
-            if (!ok) break;
-            scores(x, k_slot);
-          }
+        for (int k = 0; k < HD / 16; ++k) {
+          const uint32_t off = ((k / 4) * M::HALF + (k % 4) * 32) >> 4;
+          ptx::mma_bf16_ss(tmem + 128 * x + 64 * b, qd + off, kd + off, id_s, k != 0);
         }
-        if (!ok) break;
-        commit(M::KV_EMPTY + 8 * v_slot);
-        ++e;
-        if (!last) {
-          commit(M::KV_EMPTY + 8 * k_slot);
-          ++e;
-          if (u + 2 == w.u1) commit(M::Q_EMPTY);
-        }
+        ptx::mma_commit(base + M::S_FULL + 8 * (2 * x + b));
       }
-      more = w.next(cost);
+      __syncwarp();
+    };
+    while (ok && more) {
+      const int steps = steps_of();
+      if (!(ok = all_wait(M::Q_FULL, qn & 1))) break;
+      ++qn;
+      if (x == 1 && w.x * 2 * tok_tile + tok_tile >= q.m) {
+        // no second row tile: this issuer only gives its leave for what it does not use
+        if (lane == 0) ptx::mbar_arrive(base + M::Q_EMPTY);
+        for (uint32_t i = 0; ok && i < 2u * (w.u1 - w.u0); ++i, ++e) {
+          ok = full_wait(e);
+          if (ok && lane == 0) ptx::mbar_arrive(base + M::KV_EMPTY + 8 * (e % AT_RING));
+        }
+        if (ok) more = w.next(cost);
+        __syncwarp();
+        continue;
+      }
+      if (!(ok = full_wait(e))) break;
+      ptx::tc_fence_after_sync();
+      for (int b = 0; b < min(steps, 2); ++b) scores(e % AT_RING, b);
+      commit(M::KV_EMPTY + 8 * (e % AT_RING));
+      if (steps <= 2) commit(M::Q_EMPTY);
+      for (int i = 0; i < steps; ++i) {
+        const int b = i & 1;
+        const uint32_t ve = e + 2 * (i >> 1) + 1, ke = ve + 1;  // ring places of this unit's values and the next one's keys
+        const bool next = i + 2 < steps;
+        if (b == 0 && !(ok = all_wait(M::V_READY + 8 * (ve % AT_RING), (ve / (2 * AT_RING)) & 1))) break;
+        if (!(ok = all_wait(M::P_FULL + 8 * (2 * x + b), (p_par >> b) & 1))) break;
+        p_par ^= 1u << b;
+        ptx::tc_fence_after_sync();
+        if (ptx::elect_one()) {
+          const uint64_t vd = ptx::smem_desc_mn_sw128(base + M::RING + (ve % AT_RING) * M::TILE + b * 8192, M::HALF);
+#pragma unroll
+          for (int k = 0; k < 4; ++k)
+            ptx::mma_bf16_ts(tmem + 256 + 128 * x, tmem + 128 * x + 64 * b + 8 * k, vd + k * (2048 >> 4), id_o, i != 0 || k != 0);
+          ptx::mma_commit(base + M::O_DONE + 8 * (2 * x + b));
+        }
+        __syncwarp();
+        if (b == 1 || i + 1 == steps) commit(M::KV_EMPTY + 8 * (ve % AT_RING));
+        if (next) {
+          if (b == 0 && !(ok = full_wait(ke))) break;
+          scores(ke % AT_RING, b);
+          if (b == 1 || i + 3 == steps) commit(M::KV_EMPTY + 8 * (ke % AT_RING));
+        }
+        if (i + 3 == steps) commit(M::Q_EMPTY);
+      }
+      e += 2 * (w.u1 - w.u0);
+      if (ok) more = w.next(cost);
       __syncwarp();
     }
     if (!ok && lane == 0) give_up(AT_WAIT_MMA);
@@ -338,34 +368,42 @@ attn_tiles_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
       const int end = q.used + q.m;
       for (int u = w.u0; u < w.u1; ++u, e += 2) {
         const uint32_t slot = e % AT_RING;
-        if (!__any_sync(0xffffffffu, wait(M::KV_FULL + 8 * slot, (e / AT_RING) & 1))) { ok = false; break; }
+        // the keys' tile too: a place's barrier must be followed through every round, or a later one looks like this one
+        if (!__any_sync(0xffffffffu, wait(M::KV_FULL + 8 * ((e - 1) % AT_RING), ((e - 1) / AT_RING) & 1)) ||
+            !__any_sync(0xffffffffu, wait(M::KV_FULL + 8 * slot, (e / AT_RING) & 1))) {
+          ok = false;
+          break;
+        }
         if (masked(u)) {
+          // from the first slot that some row does not see; a lane takes 16 bytes of a row, four rows side by side (the swizzle
+          // moves pieces inside a row, which does not matter here)
           const uint32_t tile = base + M::RING + slot * M::TILE;
+          const int r0 = max(0, q.used + (a.b.parent ? 0 : w.x * 2 * tok_tile + 1) - u * AT_KEYS);
           bool found = false;
-          for (int i = (warp - 2) * 32 + lane; i < AT_KEYS * HD / 8; i += 64) {
-            const int r = i & 127, c16 = i >> 7;  // key, 16-byte piece of its row
-            const int at = u * AT_KEYS + r;
-            if (at < q.used) continue;
-            const uint32_t addr = tile + (c16 >> 3) * M::HALF + r * 128 + (c16 & 7) * 16;
-            bool drop = at >= end;
-            if (!drop && a.b.parent) drop = a.b.parent[q.t0 + at - q.used] == BITRL_PARENT_PAD;
-            uint4 v = ptx::lds128(addr);
-            uint32_t x[4] = {v.x, v.y, v.z, v.w};
-            bool touch = drop;
+          for (int half = 0; half < NH; ++half)
+#pragma unroll 4
+            for (int r = (r0 & ~3) + (lane >> 3); r < AT_KEYS; r += 4) {
+              const int at = u * AT_KEYS + r;
+              const uint32_t addr = tile + half * M::HALF + r * 128 + (lane & 7) * 16;
+              bool drop = at >= end;
+              if (!drop && a.b.parent && at >= q.used) drop = a.b.parent[q.t0 + at - q.used] == BITRL_PARENT_PAD;
+              const uint4 v = ptx::lds128(addr);
+              uint32_t x[4] = {v.x, v.y, v.z, v.w};
+              bool touch = drop;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-              const bool lo = (x[j] & 0x7f80u) == 0x7f80u, hi = (x[j] & 0x7f800000u) == 0x7f800000u;
-              if (!drop && (lo || hi)) { found = true; touch = true; }
-              if (drop || lo) x[j] &= 0xffff0000u;
-              if (drop || hi) x[j] &= 0x0000ffffu;
+              for (int j = 0; j < 4; ++j) {
+                const bool lo = (x[j] & 0x7f80u) == 0x7f80u, hi = (x[j] & 0x7f800000u) == 0x7f800000u;
+                if (!drop && r >= r0 && (lo || hi)) found = touch = true;
+                if (drop || lo) x[j] &= 0xffff0000u;
+                if (drop || hi) x[j] &= 0x0000ffffu;
+              }
+              if (touch && r >= r0) ptx::sts128(addr, make_uint4(x[0], x[1], x[2], x[3]));
             }
-            if (touch) ptx::sts128(addr, make_uint4(x[0], x[1], x[2], x[3]));
-          }
           if (__any_sync(0xffffffffu, found) && lane == 0) odd[item & 3] = item + 1;
           ptx::fence_proxy_async_smem();
         }
         __syncwarp();
-        if (lane == 0) ptx::mbar_arrive(base + M::V_READY + 8 * (slot >> 1));
+        if (lane == 0) ptx::mbar_arrive(base + M::V_READY + 8 * slot);
       }
       ++item;
       if (ok) more = w.next(cost);
@@ -375,90 +413,91 @@ attn_tiles_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
   }
   } else {
     // ------------------------------------------------------------------ softmax, one row per thread
-    ptx::regs_inc<208>();
     const int x = (warp - 4) >> 2;  // row tile
     const uint32_t lane_base = static_cast<uint32_t>((warp & 3) * 32) << 16;
     const int r = (warp & 3) * 32 + lane, r_tok = r / a.rep, r_head = r - r_tok * a.rep;
     const uint32_t s_addr = tmem + 128 * x + lane_base, o_addr = tmem + 256 + 128 * x + lane_base;
-    uint32_t sn = 0, on = 0, item = 0;
+    const bool wide = (reinterpret_cast<uintptr_t>(a.att) & 31u) == 0;  // att is 16-byte aligned at least
+    uint32_t s_par = 0, o_par = 0, item = 0;  // phases, as bits: of either score buffer, of the products from either buffer
+    const uint64_t scale_x2 = ptx::pack_f32x2(__float_as_uint(a.scale2), __float_as_uint(a.scale2));
     bool ok = true;
     while (ok && more) {
       const int tok_first = (w.x * 2 + x) * tok_tile, tok = tok_first + r_tok;
       if (tok_first < q.m) {
         const bool exists = r_tok < tok_tile && tok < q.m;
-        const int tk = min(tok, q.m - 1);
+        const int tk = min(tok, q.m - 1), steps = steps_of();
         float m_ref = -INFINITY, l = 0.0f;
-        for (int u = w.u0; u < w.u1; ++u, ++sn) {
-          if (!__any_sync(0xffffffffu, wait(M::S_FULL + 8 * x, sn & 1))) { ok = false; break; }
+        for (int i = 0; i < steps; ++i) {
+          const int b = i & 1;
+          if (!__any_sync(0xffffffffu, wait(M::S_FULL + 8 * (2 * x + b), (s_par >> b) & 1))) { ok = false; break; }
+          s_par ^= 1u << b;
           ptx::tc_fence_after_sync();
-          uint32_t s[4][32];
-#pragma unroll
-          for (int c = 0; c < 4; ++c) ptx::tmem_ld_32x32b_x32(s_addr + 32 * c, s[c]);
+          uint32_t s[2][32];
+          ptx::tmem_ld_32x32b_x32(s_addr + 64 * b, s[0]);
+          ptx::tmem_ld_32x32b_x32(s_addr + 64 * b + 32, s[1]);
           ptx::tmem_ld_wait();
-          if (masked(u)) {
+          if (masked(w.u0 + (i >> 1))) {
 #pragma unroll
-            for (int c = 0; c < 4; ++c) {
-              const uint32_t seen = at_seen(a, q, tk, u * AT_KEYS + 32 * c);
+            for (int c = 0; c < 2; ++c) {
+              const uint32_t seen = at_seen(a, q, tk, w.u0 * AT_KEYS + 64 * i + 32 * c);
 #pragma unroll
-              for (int i = 0; i < 32; ++i) s[c][i] = (seen >> i) & 1u ? s[c][i] : 0xff800000u;
+              for (int j = 0; j < 32; ++j) s[c][j] = (seen >> j) & 1u ? s[c][j] : 0xff800000u;
             }
           }
           float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-          for (int c = 0; c < 4; ++c)
+          for (int c = 0; c < 2; ++c)
 #pragma unroll
-            for (int i = 0; i < 32; i += 2)
-              mx[(i >> 1) & 3] = fmaxf(mx[(i >> 1) & 3], fmaxf(__uint_as_float(s[c][i]), __uint_as_float(s[c][i + 1])));
+            for (int j = 0; j < 32; j += 2)
+              mx[(j >> 1) & 3] = fmaxf(mx[(j >> 1) & 3], fmaxf(__uint_as_float(s[c][j]), __uint_as_float(s[c][j + 1])));
           const float m2 = __fmul_rn(fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])), a.scale2);
-          if (u == w.u0) {
+          if (i == 0) {
             m_ref = m2;
-          } else if (__any_sync(0xffffffffu, m2 > m_ref + AT_GROWTH || (m_ref == -INFINITY && m2 > m_ref))) {
+          } else if (__any_sync(0xffffffffu, m2 > m_ref + AT_GROWTH)) {
+            // the product of the step before (the one before that is done: this step's scores came after it)
+            if (!__any_sync(0xffffffffu, wait(M::O_DONE + 8 * (2 * x + (b ^ 1)), ((o_par >> (b ^ 1)) & 1) ^ 1))) { ok = false; break; }
+            ptx::tc_fence_after_sync();
             const float m_new = fmaxf(m_ref, m2);
             const float f = m_new == m_ref ? 1.0f : ac_exp2(m_ref - m_new);
             m_ref = m_new;
             l = __fmul_rn(l, f);
-#pragma unroll
+#pragma unroll 1
             for (int c = 0; c < HD / 32; ++c) {
               uint32_t o[32];
               ptx::tmem_ld_32x32b_x32(o_addr + 32 * c, o);
               ptx::tmem_ld_wait();
 #pragma unroll
-              for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__fmul_rn(__uint_as_float(o[i]), f));
+              for (int j = 0; j < 32; ++j) o[j] = __float_as_uint(__fmul_rn(__uint_as_float(o[j]), f));
               ptx::tmem_st_32x32b_x32(o_addr + 32 * c, o);
             }
           }
           const float sub = m_ref == -INFINITY ? 0.0f : -m_ref;
-          const uint64_t scale_x2 = ptx::pack_f32x2(__float_as_uint(a.scale2), __float_as_uint(a.scale2));
           const uint64_t sub_x2 = ptx::pack_f32x2(__float_as_uint(sub), __float_as_uint(sub));
           uint64_t sum[2] = {0ull, 0ull};
+          uint32_t p[32];
 #pragma unroll
-          for (int c = 0; c < 4; c += 2) {
-            uint32_t p[32];
-#pragma unroll
-            for (int i = 0; i < 32; ++i) {
-              const int cc = c + (i >> 4), j = 2 * (i & 15);
-              float p0, p1;
-              ptx::unpack_f32x2(ptx::fma_f32x2(ptx::pack_f32x2(s[cc][j], s[cc][j + 1]), scale_x2, sub_x2), p0, p1);
-              p0 = ac_exp2(p0);
-              p1 = ac_exp2(p1);
-              sum[i & 1] = ptx::add_f32x2(sum[i & 1], ptx::pack_f32x2(__float_as_uint(p0), __float_as_uint(p1)));
-              p[i] = pack_bf16x2(p0, p1);
-            }
-            ptx::tmem_st_32x32b_x32(s_addr + 16 * c, p);
+          for (int j = 0; j < 32; ++j) {
+            const int c = j >> 4, k = 2 * (j & 15);
+            float p0, p1;
+            ptx::unpack_f32x2(ptx::fma_f32x2(ptx::pack_f32x2(s[c][k], s[c][k + 1]), scale_x2, sub_x2), p0, p1);
+            p0 = ac_exp2(p0);
+            p1 = ac_exp2(p1);
+            sum[j & 1] = ptx::add_f32x2(sum[j & 1], ptx::pack_f32x2(__float_as_uint(p0), __float_as_uint(p1)));
+            p[j] = pack_bf16x2(p0, p1);
           }
-          {
-            float l0, l1;
-            ptx::unpack_f32x2(ptx::add_f32x2(sum[0], sum[1]), l0, l1);
-            l += l0 + l1;
-          }
+          ptx::tmem_st_32x32b_x32(s_addr + 64 * b, p);
+          float l0, l1;
+          ptx::unpack_f32x2(ptx::add_f32x2(sum[0], sum[1]), l0, l1);
+          l += l0 + l1;
           ptx::tmem_st_wait();
           ptx::tc_fence_before_sync();
           __syncwarp();
-          if (lane == 0) ptx::mbar_arrive(base + M::P_FULL + 8 * x);
+          if (lane == 0) ptx::mbar_arrive(base + M::P_FULL + 8 * (2 * x + b));
+          o_par ^= 1u << b;
         }
         if (!ok) break;
-        if (!__any_sync(0xffffffffu, wait(M::O_FULL + 8 * x, on & 1))) { ok = false; break; }
-        ++on;
+        const int lb = (steps - 1) & 1;
+        if (!__any_sync(0xffffffffu, wait(M::O_DONE + 8 * (2 * x + lb), ((o_par >> lb) & 1) ^ 1))) { ok = false; break; }
         ptx::tc_fence_after_sync();
         const bool whole = w.u0 == 0 && w.u1 == w.units;
         const bool fix = odd[item & 3] == item + 1;
@@ -468,15 +507,17 @@ attn_tiles_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
         const long long row = static_cast<long long>(q.t0 + tok) * a.n_heads + w.h * a.rep + r_head;
         const int cut = 2 * blockIdx.x + (w.u0 == 0 ? 1 : 0);
         const int cut_row = x * tok_tile * a.rep + r;
-        float* part = a.part_o + (static_cast<long long>(cut) * t.rows_cap + cut_row) * HD;
+        // parts lie dimension by dimension, so that the lanes' rows are neighbours (row by row, every store touched 32 lines
+        // and writing a part took 20000 cycles)
+        float* part = a.part_o + static_cast<long long>(cut) * HD * t.rows_cap + cut_row;
 #pragma unroll 1
         for (int c = 0; c < HD / 32; ++c) {
           uint32_t o[32];
           ptx::tmem_ld_32x32b_x32(o_addr + 32 * c, o);
           ptx::tmem_ld_wait();
           if (fix && exists && !pad) {  // rare: values that are not finite, of masked units, for the rows that see them
-            for (int at = max(q.used, w.u0 * AT_KEYS); at < min(q.used + q.m, w.u1 * AT_KEYS); ++at) {
-              if (!masked(at / AT_KEYS) || !(at_seen(a, q, tok, at) & 1u)) continue;
+            for (int at = max(q.used + (a.b.parent ? 0 : w.x * 2 * tok_tile + 1), w.u0 * AT_KEYS); at < min(q.used + q.m, w.u1 * AT_KEYS); ++at) {
+              if (!(at_seen(a, q, tok, at) & 1u)) continue;
               const int pg = kv_page(a.c, w.s, at);
               if (pg < 0) continue;
               const unsigned short* v = a.c.v + (kv_row(a.c, 0, pg, w.h) + (at & slots_mask)) * HD + 32 * c;
@@ -489,19 +530,23 @@ attn_tiles_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
           }
           if (!exists) continue;
           if (whole) {
-            uint4* dst = reinterpret_cast<uint4*>(a.att + row * HD + 32 * c);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              uint32_t b[4];
+            for (int i = 0; i < 2; ++i) {
+              uint32_t v[8];
 #pragma unroll
-              for (int j = 0; j < 4; ++j)
-                b[j] = none ? 0u : pack_bf16x2(__fmul_rn(__uint_as_float(o[8 * i + 2 * j]), inv), __fmul_rn(__uint_as_float(o[8 * i + 2 * j + 1]), inv));
-              dst[i] = make_uint4(b[0], b[1], b[2], b[3]);
+              for (int j = 0; j < 8; ++j)
+                v[j] = none ? 0u : pack_bf16x2(__fmul_rn(__uint_as_float(o[16 * i + 2 * j]), inv), __fmul_rn(__uint_as_float(o[16 * i + 2 * j + 1]), inv));
+              if (wide) {
+                ptx::stg256(a.att + row * HD + 32 * c + 16 * i, v);
+              } else {
+                uint4* dst = reinterpret_cast<uint4*>(a.att + row * HD + 32 * c + 16 * i);
+                dst[0] = make_uint4(v[0], v[1], v[2], v[3]);
+                dst[1] = make_uint4(v[4], v[5], v[6], v[7]);
+              }
             }
           } else {
-            uint4* dst = reinterpret_cast<uint4*>(part + 32 * c);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) dst[i] = make_uint4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
+            for (int i = 0; i < 32; ++i) part[static_cast<long long>(32 * c + i) * t.rows_cap] = __uint_as_float(o[i]);
           }
         }
         if (exists) {
@@ -524,7 +569,7 @@ attn_tiles_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
   __syncthreads();
   if (*failed) {
     // Failure path only: copies and MMAs that nobody waited for may still be in flight.
-    if (warp == 1) {
+    if (warp == 1 || warp == 2) {
       if (ptx::elect_one()) ptx::mma_commit(base + M::DRAIN);
       __syncwarp();
       ptx::mbar_wait(base + M::DRAIN, 0, 2000000LL);
@@ -551,7 +596,7 @@ __global__ void __launch_bounds__(256) attn_tiles_join_kernel(const __grid_const
   KvSeq q;
   if (!kv_seq(a.c, a.b, head.s, q)) return;
   constexpr int PER = HD / 8;  // dimensions of a thread
-  const int cut_row = blockIdx.y * 32 + threadIdx.x / 8, d0 = (threadIdx.x % 8) * PER;
+  const int cut_row = blockIdx.y * 32 + (threadIdx.x & 31), d0 = (threadIdx.x >> 5) * PER;
   const int tile_rows = t.tok_tile * a.rep;
   const int x = cut_row / tile_rows, r = cut_row - x * tile_rows;
   const int tok = (head.x * 2 + x) * t.tok_tile + r / a.rep;
@@ -576,15 +621,9 @@ __global__ void __launch_bounds__(256) attn_tiles_join_kernel(const __grid_const
     if (ml.x == -INFINITY) continue;
     const float f = ac_exp2(ml.x - m_all);
     l = fmaf(ml.y, f, l);
-    const float4* p = reinterpret_cast<const float4*>(a.part_o + part_at(c) * HD + d0);
+    const float* p = a.part_o + (part_at(c) - cut_row) * HD + static_cast<long long>(d0) * t.rows_cap + cut_row;
 #pragma unroll
-    for (int i = 0; i < PER / 4; ++i) {
-      const float4 v = p[i];
-      acc[4 * i] = fmaf(v.x, f, acc[4 * i]);
-      acc[4 * i + 1] = fmaf(v.y, f, acc[4 * i + 1]);
-      acc[4 * i + 2] = fmaf(v.z, f, acc[4 * i + 2]);
-      acc[4 * i + 3] = fmaf(v.w, f, acc[4 * i + 3]);
-    }
+    for (int i = 0; i < PER; ++i) acc[i] = fmaf(p[static_cast<long long>(i) * t.rows_cap], f, acc[i]);
   }
   const bool none = l == 0.0f || (a.b.parent && a.b.parent[q.t0 + tok] == BITRL_PARENT_PAD);
   const float inv = none ? 0.0f : __fdiv_rn(1.0f, l);
