@@ -377,28 +377,50 @@ attn_tiles_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
         if (masked(u)) {
           // from the first slot that some row does not see; a lane takes 16 bytes of a row, four rows side by side (the swizzle
           // moves pieces inside a row, which does not matter here)
-          const uint32_t tile = base + M::RING + slot * M::TILE;
-          const int r0 = max(0, q.used + (a.b.parent ? 0 : w.x * 2 * tok_tile + 1) - u * AT_KEYS);
-          bool found = false;
-          for (int half = 0; half < NH; ++half)
-#pragma unroll 4
-            for (int r = (r0 & ~3) + (lane >> 3); r < AT_KEYS; r += 4) {
-              const int at = u * AT_KEYS + r;
-              const uint32_t addr = tile + half * M::HALF + r * 128 + (lane & 7) * 16;
-              bool drop = at >= end;
-              if (!drop && a.b.parent && at >= q.used) drop = a.b.parent[q.t0 + at - q.used] == BITRL_PARENT_PAD;
-              const uint4 v = ptx::lds128(addr);
-              uint32_t x[4] = {v.x, v.y, v.z, v.w};
-              bool touch = drop;
+          const uint32_t tile = base + M::RING + slot * M::TILE + (lane & 7) * 16;
+          const int r0 = max(0, q.used + (a.b.parent ? 0 : w.x * 2 * tok_tile + 1) - u * AT_KEYS), rl = min(AT_KEYS, end - u * AT_KEYS);
+          const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
+          for (int r = (rl & ~3) + (lane >> 3); r < AT_KEYS; r += 4)
+            if (r >= rl) {
 #pragma unroll
-              for (int j = 0; j < 4; ++j) {
-                const bool lo = (x[j] & 0x7f80u) == 0x7f80u, hi = (x[j] & 0x7f800000u) == 0x7f800000u;
-                if (!drop && r >= r0 && (lo || hi)) found = touch = true;
-                if (drop || lo) x[j] &= 0xffff0000u;
-                if (drop || hi) x[j] &= 0x0000ffffu;
-              }
-              if (touch && r >= r0) ptx::sts128(addr, make_uint4(x[0], x[1], x[2], x[3]));
+              for (int half = 0; half < NH; ++half) ptx::sts128(tile + half * M::HALF + r * 128, zero);
             }
+          if (a.b.parent)
+            for (int r = (r0 & ~3) + (lane >> 3); r < rl; r += 4)
+              if (u * AT_KEYS + r >= q.used && a.b.parent[q.t0 + u * AT_KEYS + r - q.used] == BITRL_PARENT_PAD) {
+#pragma unroll
+                for (int half = 0; half < NH; ++half) ptx::sts128(tile + half * M::HALF + r * 128, zero);
+              }
+          __syncwarp();
+          // is there an exponent of ones?  (two per word: a half of x that is zero)
+          uint32_t hit = 0u;
+#pragma unroll
+          for (int half = 0; half < NH; ++half)
+#pragma unroll 8
+            for (int r = (r0 & ~3) + (lane >> 3); r < rl; r += 4) {
+              const uint4 v = ptx::lds128(tile + half * M::HALF + r * 128);
+              const uint32_t x0 = ~v.x & 0x7f807f80u, x1 = ~v.y & 0x7f807f80u, x2 = ~v.z & 0x7f807f80u, x3 = ~v.w & 0x7f807f80u;
+              hit |= ((x0 - 0x00010001u) & ~x0) | ((x1 - 0x00010001u) & ~x1) | ((x2 - 0x00010001u) & ~x2) | ((x3 - 0x00010001u) & ~x3);
+            }
+          bool found = false;
+          if (__any_sync(0xffffffffu, (hit & 0x80008000u) != 0u))
+            for (int half = 0; half < NH; ++half)
+              for (int r = (r0 & ~3) + (lane >> 3); r < rl; r += 4) {
+                if (r < r0) continue;
+                const uint32_t addr = tile + half * M::HALF + r * 128;
+                const uint4 v = ptx::lds128(addr);
+                uint32_t x[4] = {v.x, v.y, v.z, v.w};
+                bool touch = false;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                  const bool lo = (x[j] & 0x7f80u) == 0x7f80u, hi = (x[j] & 0x7f800000u) == 0x7f800000u;
+                  touch |= lo || hi;
+                  if (lo) x[j] &= 0xffff0000u;
+                  if (hi) x[j] &= 0x0000ffffu;
+                }
+                if (touch) ptx::sts128(addr, make_uint4(x[0], x[1], x[2], x[3]));
+                found |= touch;
+              }
           if (__any_sync(0xffffffffu, found) && lane == 0) odd[item & 3] = item + 1;
           ptx::fence_proxy_async_smem();
         }
@@ -612,18 +634,23 @@ __global__ void __launch_bounds__(256) attn_tiles_join_kernel(const __grid_const
     m_all = fmaxf(m_all, a.part_ml[part_at(last)].x);
     if (cut.ends) break;
   }
-  float l = 0.0f, acc[PER];
+  float l = 0.0f, acc[PER], v[PER];
+  auto fetch = [&](int c) {
+    const float* p = a.part_o + (part_at(c) - cut_row) * HD + static_cast<long long>(d0) * t.rows_cap + cut_row;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) v[i] = p[static_cast<long long>(i) * t.rows_cap];
+  };
 #pragma unroll
   for (int i = 0; i < PER; ++i) acc[i] = 0.0f;
   for (int c = c0; c <= last; ++c) {
     if (c != c0 && a.cuts[2 * c].s < 0) continue;
+    fetch(c);
     const float2 ml = a.part_ml[part_at(c)];
     if (ml.x == -INFINITY) continue;
     const float f = ac_exp2(ml.x - m_all);
     l = fmaf(ml.y, f, l);
-    const float* p = a.part_o + (part_at(c) - cut_row) * HD + static_cast<long long>(d0) * t.rows_cap + cut_row;
 #pragma unroll
-    for (int i = 0; i < PER; ++i) acc[i] = fmaf(p[static_cast<long long>(i) * t.rows_cap], f, acc[i]);
+    for (int i = 0; i < PER; ++i) acc[i] = fmaf(v[i], f, acc[i]);
   }
   const bool none = l == 0.0f || (a.b.parent && a.b.parent[q.t0 + tok] == BITRL_PARENT_PAD);
   const float inv = none ? 0.0f : __fdiv_rn(1.0f, l);
