@@ -706,6 +706,50 @@ __device__ __forceinline__ int am_units(const AmArgs& t, int s, int x, KvSeq& q,
   return (q.m + t.tok_tile - 1) / t.tok_tile - first;
 }
 
+// Columns c .. c + 31 of a row tile whose token sees the slot of new token j (j >= 0), as bits.
+__device__ __forceinline__ uint32_t am_columns(const AcArgs& a, const KvSeq& q, int j, int tok0, int c) {
+  if (!a.b.parent) {
+    const int from = (j - tok0) * a.rep - c;  // rows from token j on
+    return from >= 32 ? 0u : from <= 0 ? 0xffffffffu : 0xffffffffu << from;
+  }
+  if (j >= q.m) return 0u;
+  // the (at most 32) tokens of the columns as bits, then each bit on the columns of its token
+  const uint32_t* who = a.desc + static_cast<long long>(q.t0 + j) * AC_TREE_WORDS;
+  const int t0 = tok0 + c / a.rep, at = t0 >> 5;
+  if (at >= AC_TREE_WORDS) return 0u;
+  uint32_t can = 0u, left = __funnelshift_r(who[at], at + 1 < AC_TREE_WORDS ? who[at + 1] : 0u, t0 & 31);
+  for (int lo = (t0 - tok0) * a.rep - c; lo < 32; lo += a.rep, left >>= 1)  // lo: first column of the token
+    if (left & 1u) {
+      const int from = max(lo, 0), n = min(lo + a.rep, 32) - from;
+      can |= (n >= 32 ? 0xffffffffu : (1u << n) - 1u) << from;
+    }
+  return can;
+}
+
+// Adds 2^(score + lse) over the 32 columns whose bit in `see` is set; lse: shared-memory address of -(maximum + log2 sum).
+__device__ __forceinline__ void am_add(const uint32_t (&s)[32], uint32_t see, uint32_t lse, uint64_t scale_x2, float scale, float (&got)[4]) {
+  if (__all_sync(0xffffffffu, see == 0xffffffffu)) {
+#pragma unroll
+    for (int i = 0; i < 32; i += 4) {
+      const uint4 e = ptx::lds128(lse + 4 * i);
+      float p[4];
+      ptx::unpack_f32x2(ptx::fma_f32x2(ptx::pack_f32x2(s[i], s[i + 1]), scale_x2, ptx::pack_f32x2(e.x, e.y)), p[0], p[1]);
+      ptx::unpack_f32x2(ptx::fma_f32x2(ptx::pack_f32x2(s[i + 2], s[i + 3]), scale_x2, ptx::pack_f32x2(e.z, e.w)), p[2], p[3]);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) got[k] += ac_exp2(p[k]);
+    }
+  } else if (__any_sync(0xffffffffu, see != 0u)) {
+#pragma unroll
+    for (int i = 0; i < 32; i += 4) {
+      const uint4 e = ptx::lds128(lse + 4 * i);
+      const uint32_t ev[4] = {e.x, e.y, e.z, e.w};
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        if ((see >> (i + k)) & 1u) got[k] += ac_exp2(fmaf(__uint_as_float(s[i + k]), scale, __uint_as_float(ev[k])));
+    }
+  }
+}
+
 template <int HD>
 __global__ void __launch_bounds__(AM_THREADS, 1)
 attn_mass_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_constant__ CUtensorMap tmap_k, const __grid_constant__ AmArgs t) {
@@ -917,47 +961,8 @@ attn_mass_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_consta
               if (lane == 0) ptx::mbar_arrive(base + M::S_EMPTY + s_bar);
             }
             uint32_t see = ptx::lds32(base + M::LIVE + 16 * b + 4 * c);
-            const uint32_t lse = base + M::LSE + 512 * b + 128 * c;
-            if (masked && j >= 0) {
-              // columns of this chunk whose token sees the slot of new token j
-              uint32_t can = 0u;
-              if (!a.b.parent) {
-                const int from = (j - tok0) * a.rep - 32 * c;  // rows from token j on
-                can = from >= 32 ? 0u : from <= 0 ? 0xffffffffu : 0xffffffffu << from;
-              } else if (j < q.m) {
-                // the (at most 32) tokens of the chunk as bits, then each bit on the columns of its token
-                const uint32_t* who = a.desc + static_cast<long long>(q.t0 + j) * AC_TREE_WORDS;
-                const int t0 = tok0 + 32 * c / a.rep, at = t0 >> 5;
-                const uint32_t bits = __funnelshift_r(who[at], at + 1 < AC_TREE_WORDS ? who[at + 1] : 0u, t0 & 31);
-                int lo = (t0 - tok0) * a.rep - 32 * c;  // first column of token t0: at or before the chunk's first
-                for (uint32_t left = bits; lo < 32; lo += a.rep, left >>= 1)
-                  if (left & 1u) {
-                    const int from = max(lo, 0), cnt = min(lo + a.rep, 32) - from;
-                    can |= (cnt >= 32 ? 0xffffffffu : (1u << cnt) - 1u) << from;
-                  }
-              }
-              see &= can;
-            }
-            if (__all_sync(0xffffffffu, see == 0xffffffffu)) {
-#pragma unroll
-              for (int i = 0; i < 32; i += 4) {
-                const uint4 e = ptx::lds128(lse + 4 * i);
-                float p[4];
-                ptx::unpack_f32x2(ptx::fma_f32x2(ptx::pack_f32x2(s[c & 1][i], s[c & 1][i + 1]), scale_x2, ptx::pack_f32x2(e.x, e.y)), p[0], p[1]);
-                ptx::unpack_f32x2(ptx::fma_f32x2(ptx::pack_f32x2(s[c & 1][i + 2], s[c & 1][i + 3]), scale_x2, ptx::pack_f32x2(e.z, e.w)), p[2], p[3]);
-#pragma unroll
-                for (int k = 0; k < 4; ++k) got[k] += ac_exp2(p[k]);
-              }
-            } else if (__any_sync(0xffffffffu, see != 0u)) {
-#pragma unroll
-              for (int i = 0; i < 32; i += 4) {
-                const uint4 e = ptx::lds128(lse + 4 * i);
-                const uint32_t ev[4] = {e.x, e.y, e.z, e.w};
-#pragma unroll
-                for (int k = 0; k < 4; ++k)
-                  if ((see >> (i + k)) & 1u) got[k] += ac_exp2(fmaf(__uint_as_float(s[c & 1][i + k]), a.scale2, __uint_as_float(ev[k])));
-              }
-            }
+            if (masked && j >= 0) see &= am_columns(a, q, j, tok0, 32 * c);
+            am_add(s[c & 1], see, base + M::LSE + 512 * b + 128 * c, scale_x2, a.scale2, got);
           }
         }
         __syncwarp();
@@ -1034,6 +1039,294 @@ __global__ void __launch_bounds__(AM_KEYS) attn_mass_join_kernel(const __grid_co
   }
   const int page = kv_page(a.c, head.s, slot);
   if (page >= 0) a.c.mass[kv_row(a.c, 0, page, head.h) + (slot & ((1 << a.c.page_shift) - 1))] += sum;
+}
+
+// The same for at most two row tiles a sequence (trees, states), where reading the keys is what counts: the queries of a
+// (sequence, kv head) stay in shared memory while its keys stream by.  An item is a (sequence, kv head), a unit 256 slots; a unit
+// belongs to one CTA, so nothing is left to join.  Warps as above; with two row tiles four warps take each accumulator of a
+// unit, with one they take every other unit of their key tile.  (In the form above, whose items reload their queries, trees
+// of 48 tokens over 8000 slots took 84 us instead of 40, bound by the wait for the queries of every 256 slots.)
+template <int HD>
+struct AnSmem {
+  static constexpr uint32_t TILE = 128 * HD * 2, HALF = 128 * 128;
+  static constexpr uint32_t K = 0, Q = 4 * TILE, LSE = Q + 2 * TILE;               // K [2][2 tiles], Q [2], LSE [2][128]
+  static constexpr uint32_t LIVE = LSE + 1024, SUM = LIVE + 32, BAR = SUM + 1024;  // LIVE [2][4] bits, SUM [2][128]
+  static constexpr uint32_t K_FULL = BAR, K_EMPTY = K_FULL + 16, Q_FULL = K_EMPTY + 16, Q_EMPTY = Q_FULL + 8, S_FULL = Q_EMPTY + 8,
+                            S_EMPTY = S_FULL + 32, L_FULL = S_EMPTY + 32, L_EMPTY = L_FULL + 8, SUM_FULL = L_EMPTY + 8, SUM_EMPTY = SUM_FULL + 16,
+                            DRAIN = SUM_EMPTY + 16;
+  static constexpr uint32_t MISC = DRAIN + 8, RUN = MISC + 8, PART = RUN + 32;
+  static constexpr uint32_t BYTES = PART + 8 * (AM_THREADS / 32 + 1) + 1024;
+  static constexpr uint32_t LAUNCH = BYTES > 120 * 1024 ? BYTES : 120 * 1024;  // one CTA per SM: it takes all of tensor memory
+};
+
+template <int HD>
+__global__ void __launch_bounds__(AM_THREADS, 1)
+attn_mass_near_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_constant__ CUtensorMap tmap_k, const __grid_constant__ AmArgs t) {
+  using M = AnSmem<HD>;
+  constexpr int NH = HD / 64;
+  extern __shared__ unsigned char at_smem_raw[];
+  const uint32_t raw = ptx::smem_u32(at_smem_raw), base = (raw + 1023u) & ~1023u;
+  unsigned char* sm = at_smem_raw + (base - raw);
+  volatile uint32_t* misc = reinterpret_cast<volatile uint32_t*>(sm + M::MISC);
+  volatile uint32_t* failed = misc + 1;
+  const uint32_t failed_addr = base + M::MISC + 4;
+  const AcArgs& a = t.a;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  auto wait = [&](uint32_t bar, uint32_t parity) {
+    return __any_sync(0xffffffffu, ptx::mbar_wait_abortable(base + bar, parity, failed_addr));
+  };
+  auto give_up = [&](int stage) {
+    report_timeout(stage);
+    *failed = 1u;
+  };
+  if (threadIdx.x == 0) {
+    *failed = 0u;
+    for (int i = 0; i < 2; ++i) {
+      ptx::mbar_init(base + M::K_FULL + 8 * i, 1);
+      ptx::mbar_init(base + M::K_EMPTY + 8 * i, 1);
+      ptx::mbar_init(base + M::SUM_FULL + 8 * i, 4);
+      ptx::mbar_init(base + M::SUM_EMPTY + 8 * i, 4);
+    }
+    ptx::mbar_init(base + M::Q_FULL, 1);
+    ptx::mbar_init(base + M::Q_EMPTY, 1);
+    ptx::mbar_init(base + M::L_FULL, 1);
+    ptx::mbar_init(base + M::L_EMPTY, 16);
+    for (int i = 0; i < 4; ++i) {
+      ptx::mbar_init(base + M::S_FULL + 8 * i, 1);
+      ptx::mbar_init(base + M::S_EMPTY + 8 * i, 4);
+    }
+    ptx::mbar_init(base + M::DRAIN, 1);
+    ptx::mbar_init_fence();
+    ptx::tma_prefetch_desc(&tmap_q);
+    ptx::tma_prefetch_desc(&tmap_k);
+  }
+  if (warp == 1) {
+    ptx::tmem_alloc(base + M::MISC, 512);
+    ptx::tmem_relinquish();
+  }
+  ptx::tc_fence_before_sync();
+  __syncthreads();
+  ptx::tc_fence_after_sync();
+  const uint32_t tmem = misc[0];
+  pdl_enter();
+  KvSeq q;
+  auto cost = [&](int s, int) {  // units of (sequence, head)
+    if (!kv_seq(a.c, a.b, s, q) || q.m == 0 || (a.tree_ok && !a.tree_ok[s])) return 0;
+    return (q.used + q.m + AM_KEYS - 1) / AM_KEYS;
+  };
+  AcRun* run = reinterpret_cast<AcRun*>(sm + M::RUN);
+  ac_run_start(cost, a.c.n_seq, a.c.n_kv, 1, AM_THREADS, reinterpret_cast<long long*>(sm + M::PART), run);
+  AcWalk w(*run, a.c.n_kv, 1, a.c.n_seq);  // w.x: the kv head
+  const int tok_tile = t.tok_tile;
+  auto key_tiles = [&](int u) { return u * AM_KEYS + 128 < q.used + q.m ? 2 : 1; };
+  auto row_tiles = [&]() { return q.m > tok_tile ? 2 : 1; };
+  auto rows_of = [&](int rt) { return min(tok_tile, q.m - rt * tok_tile) * a.rep; };
+  bool more = w.start(cost), ok = true;
+  if (warp == 0) {
+    // ------------------------------------------------------------------ producer
+    uint32_t kn = 0, qn = 0;
+    const int page = 1 << a.c.page_shift, pieces = 128 >> a.c.page_shift;
+    const int tile = lane / (pieces * NH), piece = lane % (pieces * NH) / NH, half = lane % NH;
+    const int none = a.c.n_pages * a.c.n_kv * page;  // a row behind the pool: such a copy fills with zeros
+    while (ok && more) {
+      const int rts = row_tiles(), end = q.used + q.m;
+      auto row_of = [&](int u) {
+        const int slot = u * AM_KEYS + tile * 128 + piece * page;
+        const int p = tile < 2 && slot < end ? kv_page(a.c, w.s, slot) : -1;
+        return p < 0 ? none : (p * a.c.n_kv + w.x) * page;
+      };
+      int row = row_of(w.u0);
+      for (int u = w.u0; u < w.u1; ++u, ++kn) {
+        const int na = key_tiles(u), row_next = u + 1 < w.u1 ? row_of(u + 1) : none;
+        const uint32_t kb = kn & 1;
+        if (!(ok = wait(M::K_EMPTY + 8 * kb, ((kn >> 1) & 1) ^ 1))) break;
+        if (lane == 0) ptx::mbar_arrive_expect_tx(base + M::K_FULL + 8 * kb, na * M::TILE);
+        __syncwarp();
+        if (tile < na)
+          ptx::tma_load_2d(base + M::K + (2 * kb + tile) * M::TILE + half * M::HALF + piece * page * 128, &tmap_k, 64 * half, row,
+                           base + M::K_FULL + 8 * kb);
+        if (u == w.u0) {
+          if (!(ok = wait(M::Q_EMPTY, (qn & 1) ^ 1))) break;
+          ++qn;
+          if (lane == 0) ptx::mbar_arrive_expect_tx(base + M::Q_FULL, rts * NH * 128 * a.rep * tok_tile);
+          __syncwarp();
+          if (lane < rts * NH)
+            ptx::tma_load_3d(base + M::Q + (lane / NH) * M::TILE + (lane % NH) * M::HALF, &tmap_q, 64 * (lane % NH), w.x * a.rep,
+                             q.t0 + (lane / NH) * tok_tile, base + M::Q_FULL);
+        }
+        row = row_next;
+      }
+      if (ok) more = w.next(cost);
+      __syncwarp();
+    }
+    if (!ok && lane == 0) give_up(AM_WAIT_LOAD);
+  } else if (warp == 1) {
+    // ------------------------------------------------------------------ MMA issuer
+    uint32_t kn = 0, qn = 0, un[2] = {0, 0}, e_par = 0xf;  // products per key tile; phases of S_EMPTY, as bits
+    while (ok && more) {
+      const int rts = row_tiles();
+      if (!(ok = wait(M::Q_FULL, qn & 1))) break;
+      ++qn;
+      for (int u = w.u0; ok && u < w.u1; ++u, ++kn) {
+        const uint32_t kb = kn & 1;
+        const int na = key_tiles(u);
+        if (!(ok = wait(M::K_FULL + 8 * kb, (kn >> 1) & 1))) break;
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+          if (x >= na || !ok) continue;
+          for (int rt = 0; rt < rts; ++rt) {
+            const uint32_t b = un[x]++ & 1, i = 2 * x + b;
+            if (!(ok = wait(M::S_EMPTY + 8 * i, (e_par >> i) & 1))) break;
+            e_par ^= 1u << i;
+            ptx::tc_fence_after_sync();
+            if (ptx::elect_one()) {
+              const uint32_t idesc = ptx::idesc_bf16(128, (rows_of(rt) + 15) & ~15, false);
+              const uint64_t kd = ptx::smem_desc_sw128(base + M::K + (2 * kb + x) * M::TILE), qd = ptx::smem_desc_sw128(base + M::Q + rt * M::TILE);
+#pragma unroll
+              for (int k = 0; k < HD / 16; ++k) {
+                const uint32_t off = ((k / 4) * M::HALF + (k % 4) * 32) >> 4;
+                ptx::mma_bf16_ss(tmem + 128 * i, kd + off, qd + off, idesc, k != 0);
+              }
+              ptx::mma_commit(base + M::S_FULL + 8 * i);
+            }
+            __syncwarp();
+          }
+        }
+        if (!ok) break;
+        if (ptx::elect_one()) {
+          ptx::mma_commit(base + M::K_EMPTY + 8 * kb);
+          if (u + 1 == w.u1) ptx::mma_commit(base + M::Q_EMPTY);
+        }
+        __syncwarp();
+      }
+      if (ok) more = w.next(cost);
+      __syncwarp();
+    }
+    if (!ok && lane == 0) give_up(AM_WAIT_MMA);
+  } else if (warp == 2) {
+    // ------------------------------------------------------------------ row statistics
+    uint32_t n = 0;
+    while (ok && more) {
+      const int rts = row_tiles();
+      float v[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const int c = lane + 32 * (i & 3), tk = c / a.rep, rt = i >> 2;
+        v[i] = rt < rts && c < rows_of(rt)
+                   ? a.lse[static_cast<long long>(q.t0 + rt * tok_tile + tk) * a.n_heads + w.x * a.rep + c - tk * a.rep]
+                   : INFINITY;
+      }
+      if (!(ok = wait(M::L_EMPTY, (n & 1) ^ 1))) break;
+      ++n;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        reinterpret_cast<float*>(sm + M::LSE)[lane + 32 * i] = -v[i];  // what the sums add
+        const uint32_t live = __ballot_sync(0xffffffffu, v[i] != INFINITY);
+        if (lane == 0) reinterpret_cast<uint32_t*>(sm + M::LIVE)[i] = live;
+      }
+      __syncwarp();
+      if (lane == 0) ptx::mbar_arrive(base + M::L_FULL);
+      more = w.next(cost);
+      __syncwarp();
+    }
+    if (!ok && lane == 0) give_up(AM_WAIT_LSE);
+  } else if (warp >= 4) {
+    // ------------------------------------------------------------------ sums, one slot per thread
+    const int x = (warp - 4) >> 3, turn = ((warp - 4) >> 2) & 1;  // key tile; its accumulator
+    const uint32_t lane_base = static_cast<uint32_t>((warp & 3) * 32) << 16;
+    const int r = (warp & 3) * 32 + lane;
+    const uint64_t scale_x2 = ptx::pack_f32x2(__float_as_uint(a.scale2), __float_as_uint(a.scale2));
+    const uint32_t s_addr = tmem + 256 * x + 128 * turn + lane_base, s_bar = 8 * (2 * x + turn);
+    float* other = reinterpret_cast<float*>(sm + M::SUM) + 128 * x + r;
+    uint32_t un = 0, n = 0, mine = 0, met = 0;  // products of this key tile, items, products of this turn, sums handed over
+    while (ok && more) {
+      const int rts = row_tiles(), end = q.used + q.m;
+      if (!(ok = wait(M::L_FULL, n & 1))) break;
+      ++n;
+      for (int u = w.u0; u < w.u1; ++u) {
+        if (x >= key_tiles(u)) continue;
+        const int slot = u * AM_KEYS + 128 * x + r, j = slot - q.used;
+        const int rt = rts == 2 ? ((un & 1) == static_cast<uint32_t>(turn) ? 0 : 1) : 0;  // the row tile in this turn's accumulator
+        const bool take = rts == 2 || (un & 1) == static_cast<uint32_t>(turn), writes = rts == 2 ? turn == 0 : take;
+        un += rts;
+        if (!take) continue;
+        long long row = -1;
+        float before = 0.0f;
+        if (writes && slot < end) {  // where the sum goes, and what is there: read ahead of the sum
+          const int page = kv_page(a.c, w.s, slot);
+          if (page >= 0) {
+            row = kv_row(a.c, 0, page, w.x) + (slot & ((1 << a.c.page_shift) - 1));
+            before = a.c.mass[row];
+          }
+        }
+        if (!(ok = wait(M::S_FULL + s_bar, mine & 1))) break;
+        ++mine;
+        ptx::tc_fence_after_sync();
+        const int rows = rows_of(rt), tok0 = rt * tok_tile;
+        const bool masked = u * AM_KEYS + 128 * x + 127 >= q.used + (a.b.parent ? 0 : tok0 + 1);
+        float got[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+        uint32_t s[2][32];
+        ptx::tmem_ld_32x32b_x32(s_addr, s[0]);
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          if (32 * c >= rows) break;
+          ptx::tmem_ld_wait();
+          if (32 * c + 32 < rows) {
+            ptx::tmem_ld_32x32b_x32(s_addr + 32 * (c + 1), s[(c + 1) & 1]);
+          } else {
+            ptx::tc_fence_before_sync();
+            __syncwarp();
+            if (lane == 0) ptx::mbar_arrive(base + M::S_EMPTY + s_bar);
+          }
+          uint32_t see = ptx::lds32(base + M::LIVE + 16 * rt + 4 * c);
+          if (masked && j >= 0) see &= am_columns(a, q, j, tok0, 32 * c);
+          am_add(s[c & 1], see, base + M::LSE + 512 * rt + 128 * c, scale_x2, a.scale2, got);
+        }
+        float sum = (got[0] + got[1]) + (got[2] + got[3]);
+        if (rts == 2) {  // turn 1 hands its sum to turn 0
+          if (turn == 1) {
+            if (!(ok = wait(M::SUM_EMPTY + 8 * x, (met & 1) ^ 1))) break;
+            *other = sum;
+            __syncwarp();
+            if (lane == 0) ptx::mbar_arrive(base + M::SUM_FULL + 8 * x);
+          } else {
+            if (!(ok = wait(M::SUM_FULL + 8 * x, met & 1))) break;
+            sum += *other;
+            __syncwarp();
+            if (lane == 0) ptx::mbar_arrive(base + M::SUM_EMPTY + 8 * x);
+          }
+          ++met;
+        }
+        if (row >= 0) a.c.mass[row] = before + sum;
+      }
+      if (!ok) break;
+      __syncwarp();
+      if (lane == 0) ptx::mbar_arrive(base + M::L_EMPTY);
+      more = w.next(cost);
+      __syncwarp();
+    }
+    if (!ok && lane == 0) give_up(AM_WAIT_SUM);
+  }
+
+  // ---- teardown: every role leaves through here, also after a timeout ----
+  __syncwarp();
+  ptx::tc_fence_before_sync();
+  __syncthreads();
+  if (*failed) {
+    // Failure path only: copies and MMAs that nobody waited for may still be in flight.
+    if (warp == 1) {
+      if (ptx::elect_one()) ptx::mma_commit(base + M::DRAIN);
+      __syncwarp();
+      ptx::mbar_wait(base + M::DRAIN, 0, 2000000LL);
+    }
+    const long long t0 = clock64();
+    while (clock64() - t0 < 2000000LL) {}
+    __syncthreads();
+  }
+  if (warp == 1) {
+    ptx::tc_fence_after_sync();
+    ptx::tmem_dealloc(tmem, 512);
+  }
 }
 
 // ---- host --------------------------------------------------------------------------------------------------------------
@@ -1147,9 +1440,16 @@ bitrl_status launch_attention_cached_hd(const AcArgs& a, const AcPlan& p, bool m
     BITRL_CUDA(launch_pdl(attn_tiles_join_kernel<HD>, dim3(p.ctas, (p.rows_cap + 31) / 32), dim3(256), 0, st, t, p.ctas));
     count_launch(2);
     if (mass) {
+      const AmArgs m{a, p.tok_tile, ((a.c.max_pages << a.c.page_shift) + AM_KEYS - 1) / AM_KEYS, sums};
+      if (p.nx == 1) {  // at most two row tiles a sequence
+        static bool near_done[64] = {false};
+        if ((s = ac_smem(attn_mass_near_kernel<HD>, AnSmem<HD>::LAUNCH, near_done)) != BITRL_OK) return s;
+        BITRL_CUDA(launch_pdl(attn_mass_near_kernel<HD>, dim3(p.ctas), dim3(AM_THREADS), AnSmem<HD>::LAUNCH, st, mq, mk, m));
+        count_launch(1);
+        return BITRL_OK;
+      }
       static bool mass_done[64] = {false};
       if ((s = ac_smem(attn_mass_kernel<HD>, AmSmem<HD>::LAUNCH, mass_done)) != BITRL_OK) return s;
-      const AmArgs m{a, p.tok_tile, ((a.c.max_pages << a.c.page_shift) + AM_KEYS - 1) / AM_KEYS, sums};
       BITRL_CUDA(launch_pdl(attn_mass_kernel<HD>, dim3(p.ctas), dim3(AM_THREADS), AmSmem<HD>::LAUNCH, st, mq, mk, m));
       BITRL_CUDA(launch_pdl(attn_mass_join_kernel, dim3(p.ctas), dim3(AM_KEYS), 0, st, m, p.ctas));
       count_launch(2);
