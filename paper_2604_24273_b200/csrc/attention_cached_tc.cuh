@@ -1044,13 +1044,14 @@ __global__ void __launch_bounds__(AM_KEYS) attn_mass_join_kernel(const __grid_co
 // The same for at most two row tiles a sequence (trees, states), where reading the keys is what counts: the queries of a
 // (sequence, kv head) stay in shared memory while its keys stream by.  An item is a (sequence, kv head), a unit 256 slots; a unit
 // belongs to one CTA, so nothing is left to join.  Warps as above; with two row tiles four warps take each accumulator of a
-// unit, with one they take every other unit of their key tile.  (In the form above, whose items reload their queries, trees
-// of 48 tokens over 8000 slots took 84 us instead of 40, bound by the wait for the queries of every 256 slots.)
+// unit, with one they take every other unit of their key tile.  The sums go through shared memory to warp 3, which fetched
+// the places that they are added to one unit earlier: page, weight and sum one after the other in the summing warps cost
+// them 2 us a unit.  (In the form above, whose items reload their queries, trees of 48 tokens over 8000 slots took 84 us.)
 template <int HD>
 struct AnSmem {
   static constexpr uint32_t TILE = 128 * HD * 2, HALF = 128 * 128;
   static constexpr uint32_t K = 0, Q = 4 * TILE, LSE = Q + 2 * TILE;               // K [2][2 tiles], Q [2], LSE [2][128]
-  static constexpr uint32_t LIVE = LSE + 1024, SUM = LIVE + 32, BAR = SUM + 1024;  // LIVE [2][4] bits, SUM [2][128]
+  static constexpr uint32_t LIVE = LSE + 1024, SUM = LIVE + 32, BAR = SUM + 4096;  // LIVE [2][4] bits, SUM [2][2 turns][256]
   static constexpr uint32_t K_FULL = BAR, K_EMPTY = K_FULL + 16, Q_FULL = K_EMPTY + 16, Q_EMPTY = Q_FULL + 8, S_FULL = Q_EMPTY + 8,
                             S_EMPTY = S_FULL + 32, L_FULL = S_EMPTY + 32, L_EMPTY = L_FULL + 8, SUM_FULL = L_EMPTY + 8, SUM_EMPTY = SUM_FULL + 16,
                             DRAIN = SUM_EMPTY + 16;
@@ -1084,8 +1085,8 @@ attn_mass_near_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_c
     for (int i = 0; i < 2; ++i) {
       ptx::mbar_init(base + M::K_FULL + 8 * i, 1);
       ptx::mbar_init(base + M::K_EMPTY + 8 * i, 1);
-      ptx::mbar_init(base + M::SUM_FULL + 8 * i, 4);
-      ptx::mbar_init(base + M::SUM_EMPTY + 8 * i, 4);
+      ptx::mbar_init(base + M::SUM_FULL + 8 * i, 16);
+      ptx::mbar_init(base + M::SUM_EMPTY + 8 * i, 1);
     }
     ptx::mbar_init(base + M::Q_FULL, 1);
     ptx::mbar_init(base + M::Q_EMPTY, 1);
@@ -1230,77 +1231,109 @@ attn_mass_near_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_c
       __syncwarp();
     }
     if (!ok && lane == 0) give_up(AM_WAIT_LSE);
-  } else if (warp >= 4) {
+  } else if (warp == 3) {
+    // ------------------------------------------------------------------ sums into the cache, eight slots per lane
+    uint32_t n = 0, un[2] = {0, 0};  // units; products of either key tile
+    const int x = lane >> 4;         // key tile of this lane's slots
+    const int slot_mask = (1 << a.c.page_shift) - 1;
+    while (ok && more) {
+      const int rts = row_tiles(), end = q.used + q.m;
+      float* next_at = nullptr;
+      float4 next[2];
+      auto fetch = [&](int u) {
+        const int slot = u * AM_KEYS + 8 * lane;
+        next_at = nullptr;
+        if (slot >= end) return;
+        const int page = kv_page(a.c, w.s, slot);
+        if (page < 0) return;
+        next_at = a.c.mass + kv_row(a.c, 0, page, w.x) + (slot & slot_mask);
+        next[0] = *reinterpret_cast<const float4*>(next_at);
+        next[1] = *reinterpret_cast<const float4*>(next_at + 4);
+      };
+      fetch(w.u0);
+      for (int u = w.u0; u < w.u1; ++u, ++n) {
+        float* at = next_at;
+        float m[8] = {next[0].x, next[0].y, next[0].z, next[0].w, next[1].x, next[1].y, next[1].z, next[1].w};
+        if (u + 1 < w.u1) fetch(u + 1);
+        const uint32_t buf = n & 1;
+        if (!(ok = wait(M::SUM_FULL + 8 * buf, (n >> 1) & 1))) break;
+        if (at) {
+          const uint32_t first = rts == 2 ? 0 : (x ? un[1] : un[0]) & 1;
+          const float* sums = reinterpret_cast<const float*>(sm + M::SUM) + (2 * buf + first) * AM_KEYS + 8 * lane;
+#pragma unroll
+          for (int i = 0; i < 8; ++i) m[i] += rts == 2 ? sums[i] + sums[AM_KEYS + i] : sums[i];
+          const int slot = u * AM_KEYS + 8 * lane;
+          if (slot + 8 <= end) {
+            *reinterpret_cast<float4*>(at) = make_float4(m[0], m[1], m[2], m[3]);
+            *reinterpret_cast<float4*>(at + 4) = make_float4(m[4], m[5], m[6], m[7]);
+          } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+              if (slot + i < end) at[i] = m[i];
+          }
+        }
+        un[0] += rts;
+        if (key_tiles(u) == 2) un[1] += rts;
+        __syncwarp();
+        if (lane == 0) ptx::mbar_arrive(base + M::SUM_EMPTY + 8 * buf);
+      }
+      if (ok) more = w.next(cost);
+      __syncwarp();
+    }
+    if (!ok && lane == 0) give_up(AM_WAIT_SUM);
+  } else {
     // ------------------------------------------------------------------ sums, one slot per thread
     const int x = (warp - 4) >> 3, turn = ((warp - 4) >> 2) & 1;  // key tile; its accumulator
     const uint32_t lane_base = static_cast<uint32_t>((warp & 3) * 32) << 16;
     const int r = (warp & 3) * 32 + lane;
     const uint64_t scale_x2 = ptx::pack_f32x2(__float_as_uint(a.scale2), __float_as_uint(a.scale2));
     const uint32_t s_addr = tmem + 256 * x + 128 * turn + lane_base, s_bar = 8 * (2 * x + turn);
-    float* other = reinterpret_cast<float*>(sm + M::SUM) + 128 * x + r;
-    uint32_t un = 0, n = 0, mine = 0, met = 0;  // products of this key tile, items, products of this turn, sums handed over
+    uint32_t un = 0, n = 0, units = 0, mine = 0;  // products of this key tile, items, units, products of this turn
     while (ok && more) {
-      const int rts = row_tiles(), end = q.used + q.m;
+      const int rts = row_tiles();
       if (!(ok = wait(M::L_FULL, n & 1))) break;
       ++n;
-      for (int u = w.u0; u < w.u1; ++u) {
-        if (x >= key_tiles(u)) continue;
-        const int slot = u * AM_KEYS + 128 * x + r, j = slot - q.used;
-        const int rt = rts == 2 ? ((un & 1) == static_cast<uint32_t>(turn) ? 0 : 1) : 0;  // the row tile in this turn's accumulator
-        const bool take = rts == 2 || (un & 1) == static_cast<uint32_t>(turn), writes = rts == 2 ? turn == 0 : take;
-        un += rts;
-        if (!take) continue;
-        long long row = -1;
-        float before = 0.0f;
-        if (writes && slot < end) {  // where the sum goes, and what is there: read ahead of the sum
-          const int page = kv_page(a.c, w.s, slot);
-          if (page >= 0) {
-            row = kv_row(a.c, 0, page, w.x) + (slot & ((1 << a.c.page_shift) - 1));
-            before = a.c.mass[row];
-          }
-        }
-        if (!(ok = wait(M::S_FULL + s_bar, mine & 1))) break;
-        ++mine;
-        ptx::tc_fence_after_sync();
-        const int rows = rows_of(rt), tok0 = rt * tok_tile;
-        const bool masked = u * AM_KEYS + 128 * x + 127 >= q.used + (a.b.parent ? 0 : tok0 + 1);
-        float got[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-        uint32_t s[2][32];
-        ptx::tmem_ld_32x32b_x32(s_addr, s[0]);
+      for (int u = w.u0; u < w.u1; ++u, ++units) {
+        const bool active = x < key_tiles(u);
+        // the row tile in this turn's accumulator, if there is one
+        const bool first = (un & 1) == static_cast<uint32_t>(turn);
+        const bool take = active && (rts == 2 || first);
+        const int rt = rts == 2 && !first ? 1 : 0;
+        if (active) un += rts;
+        float sum = 0.0f;
+        if (take) {
+          if (!(ok = wait(M::S_FULL + s_bar, mine & 1))) break;
+          ++mine;
+          ptx::tc_fence_after_sync();
+          const int rows = rows_of(rt), tok0 = rt * tok_tile, j = u * AM_KEYS + 128 * x + r - q.used;
+          const bool masked = u * AM_KEYS + 128 * x + 127 >= q.used + (a.b.parent ? 0 : tok0 + 1);
+          float got[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+          uint32_t s[2][32];
+          ptx::tmem_ld_32x32b_x32(s_addr, s[0]);
 #pragma unroll
-        for (int c = 0; c < 4; ++c) {
-          if (32 * c >= rows) break;
-          ptx::tmem_ld_wait();
-          if (32 * c + 32 < rows) {
-            ptx::tmem_ld_32x32b_x32(s_addr + 32 * (c + 1), s[(c + 1) & 1]);
-          } else {
-            ptx::tc_fence_before_sync();
-            __syncwarp();
-            if (lane == 0) ptx::mbar_arrive(base + M::S_EMPTY + s_bar);
+          for (int c = 0; c < 4; ++c) {
+            if (32 * c >= rows) break;
+            ptx::tmem_ld_wait();
+            if (32 * c + 32 < rows) {
+              ptx::tmem_ld_32x32b_x32(s_addr + 32 * (c + 1), s[(c + 1) & 1]);
+            } else {
+              ptx::tc_fence_before_sync();
+              __syncwarp();
+              if (lane == 0) ptx::mbar_arrive(base + M::S_EMPTY + s_bar);
+            }
+            uint32_t see = ptx::lds32(base + M::LIVE + 16 * rt + 4 * c);
+            if (masked && j >= 0) see &= am_columns(a, q, j, tok0, 32 * c);
+            am_add(s[c & 1], see, base + M::LSE + 512 * rt + 128 * c, scale_x2, a.scale2, got);
           }
-          uint32_t see = ptx::lds32(base + M::LIVE + 16 * rt + 4 * c);
-          if (masked && j >= 0) see &= am_columns(a, q, j, tok0, 32 * c);
-          am_add(s[c & 1], see, base + M::LSE + 512 * rt + 128 * c, scale_x2, a.scale2, got);
+          sum = (got[0] + got[1]) + (got[2] + got[3]);
         }
-        float sum = (got[0] + got[1]) + (got[2] + got[3]);
-        if (rts == 2) {  // turn 1 hands its sum to turn 0
-          if (turn == 1) {
-            if (!(ok = wait(M::SUM_EMPTY + 8 * x, (met & 1) ^ 1))) break;
-            *other = sum;
-            __syncwarp();
-            if (lane == 0) ptx::mbar_arrive(base + M::SUM_FULL + 8 * x);
-          } else {
-            if (!(ok = wait(M::SUM_FULL + 8 * x, met & 1))) break;
-            sum += *other;
-            __syncwarp();
-            if (lane == 0) ptx::mbar_arrive(base + M::SUM_EMPTY + 8 * x);
-          }
-          ++met;
-        }
-        if (row >= 0) a.c.mass[row] = before + sum;
+        const uint32_t buf = units & 1;
+        if (!(ok = wait(M::SUM_EMPTY + 8 * buf, ((units >> 1) & 1) ^ 1))) break;
+        if (take) reinterpret_cast<float*>(sm + M::SUM)[(2 * buf + turn) * AM_KEYS + 128 * x + r] = sum;
+        __syncwarp();
+        if (lane == 0) ptx::mbar_arrive(base + M::SUM_FULL + 8 * buf);
       }
       if (!ok) break;
-      __syncwarp();
       if (lane == 0) ptx::mbar_arrive(base + M::L_EMPTY);
       more = w.next(cost);
       __syncwarp();
