@@ -473,11 +473,13 @@ KV_MAX_SLOTS = 1 << 19
 
 def _here(t: torch.Tensor, dtype, name: str, index: int) -> int:
     """Address of a contiguous tensor of that dtype on CUDA device ``index``."""
+    if type(t) is torch.Tensor and t.dtype is dtype and t.get_device() == index and t.is_contiguous():
+        return t.data_ptr()
     if not (isinstance(t, torch.Tensor) and t.dtype == dtype and t.is_contiguous() and t.is_cuda):
         raise TypeError(f"{name}: expected a contiguous CUDA tensor of dtype {dtype}")
     if t.get_device() != index:
         raise ValueError(f"{name}: on {t.device}, the cache is on cuda:{index}")
-    return t.data_ptr()
+    return t.data_ptr()  # a subclass, such as a parameter
 
 
 class KVCache:

@@ -6,6 +6,8 @@
 #include <climits>
 #include <math.h>
 
+#include <type_traits>
+
 #include "attention.cuh"
 #include "common.cuh"
 
@@ -91,8 +93,8 @@ __device__ __forceinline__ bool kv_load_tree(const KvBatch& b, const KvSeq& q, i
 // ---- append -------------------------------------------------------------------------------------------------------
 // One pass over qkv: every element is read and written once (109 MB for 256 states of the 20/5-head backbone), so the
 // copy rate bounds it; single tokens are bound by the launch and one chain of dependent loads.  A CTA takes up to
-// APP_TOKENS consecutive tokens of one sequence: first its threads compute the (cos, sin) pairs, one each, then every
-// thread rotates 8 dimensions and their 8 partners per step with 16-byte loads and stores.
+// APP_TOKENS consecutive tokens of one sequence: its threads compute the (cos, sin) pairs, one each, then every thread
+// rotates 8 dimensions and their 8 partners of each token with 16-byte loads and stores.
 // Angles: position * theta^(-2f/hd) / (2 pi) in fp64 (turns), reduced to half a turn there, so that far positions lose
 // nothing; the cosine and sine of the remainder are fp32.
 constexpr int APP_THREADS = 256;
@@ -110,10 +112,10 @@ struct AppArgs {
 
 template <int HD>
 __global__ void __launch_bounds__(APP_THREADS) kv_append_kernel(const __grid_constant__ AppArgs a) {
-  constexpr int HALF = HD / 2;
+  constexpr int HALF = HD / 2, CP = HD / 16;  // CP: pairs of 8-dimension chunks per head row
   __shared__ int par[BITRL_TREE_MAX_TOKENS];
-  __shared__ float2 cs[APP_TOKENS][HALF];
-  __shared__ int depth_of[APP_TOKENS];  // -1: padding
+  __shared__ __align__(16) float4 cs[APP_TOKENS][4][CP];  // (cos, sin) of dimensions 8 c + 2 w and the next
+  __shared__ int depth_of[APP_TOKENS];                    // -1: padding
   pdl_enter();
   const KvView& c = a.c;
   const int s = blockIdx.x / a.tiles, first = (blockIdx.x - s * a.tiles) * APP_TOKENS;
@@ -126,9 +128,27 @@ __global__ void __launch_bounds__(APP_THREADS) kv_append_kernel(const __grid_con
     if (threadIdx.x == 0) report_status(BITRL_ERR_SHAPE, KV_STAGE_BAD_SEQ);
     return;
   }
+  const int heads = a.n_heads + 2 * c.n_kv, per_token = heads * CP;
+  const long long width = static_cast<long long>(heads) * HD;
+  // A thread keeps its place in the row (head, 8 dimensions and their partners) and takes the tokens of the tile together;
+  // the first ones' loads are on their way while the angles are computed.
+  uint4 x1[APP_TOKENS], x2[APP_TOKENS];
+  auto load = [&](int r) {
+    const unsigned short* src = a.qkv + (q.t0 + first) * width + (r / CP) * HD + 8 * (r % CP);
+#pragma unroll
+    for (int t = 0; t < APP_TOKENS; ++t)
+      if (t < n) {
+        x1[t] = *reinterpret_cast<const uint4*>(src + t * width);
+        x2[t] = *reinterpret_cast<const uint4*>(src + t * width + HALF);
+      }
+  };
+  if (static_cast<int>(threadIdx.x) < per_token) load(threadIdx.x);
+  int page[APP_TOKENS];
+#pragma unroll
+  for (int t = 0; t < APP_TOKENS; ++t) page[t] = t < n ? kv_page(c, s, q.used + first + t) : -1;
   if (a.b.parent) {
     if (!kv_load_tree(a.b, q, par, APP_THREADS)) return;
-    if (threadIdx.x < n) {
+    if (static_cast<int>(threadIdx.x) < n) {
       int d = -1;
       for (int i = par[first + threadIdx.x] == BITRL_PARENT_PAD ? -1 : static_cast<int>(first + threadIdx.x); i >= 0; i = par[i]) ++d;
       depth_of[threadIdx.x] = d;
@@ -141,52 +161,47 @@ __global__ void __launch_bounds__(APP_THREADS) kv_append_kernel(const __grid_con
     const double turn = static_cast<double>(seen + d) * a.turns[f];
     float sn, cn;
     sincospif(2.0f * static_cast<float>(turn - rint(turn)), &sn, &cn);
-    cs[t][f] = make_float2(cn, sn);
+    reinterpret_cast<float2*>(&cs[t][(f & 7) >> 1][f >> 3])[f & 1] = make_float2(cn, sn);
   }
   __syncthreads();
-  constexpr int CP = HD / 16;  // pairs of 8-dimension chunks per head row
-  const int heads = a.n_heads + 2 * c.n_kv;
-  const long long width = static_cast<long long>(heads) * HD;
-  const int per_token = heads * CP;
-  for (int i = threadIdx.x; i < n * per_token; i += APP_THREADS) {
-    const int t = i / per_token, r = i - t * per_token;
-    const int head = r / CP, d0 = 8 * (r - head * CP);
-    if (a.b.parent && depth_of[t] < 0) continue;
-    const int tok = first + t;
-    const unsigned short* src = a.qkv + (q.t0 + tok) * width + head * HD + d0;
-    uint4 x1 = *reinterpret_cast<const uint4*>(src), x2 = *reinterpret_cast<const uint4*>(src + HALF);
-    if (head < a.n_heads + c.n_kv) {
-      uint32_t w1[4] = {x1.x, x1.y, x1.z, x1.w}, w2[4] = {x2.x, x2.y, x2.z, x2.w};
+  for (int r = threadIdx.x; r < per_token; r += APP_THREADS) {
+    if (r >= APP_THREADS) load(r);
+    const int head = r / CP, ch = r % CP, d0 = 8 * ch;
+    const bool is_q = head < a.n_heads, is_k = !is_q && head < a.n_heads + c.n_kv;
+    const int kvh = is_q ? 0 : head - a.n_heads - (is_k ? 0 : c.n_kv);
 #pragma unroll
-      for (int w = 0; w < 4; ++w) {
-        const float2 e0 = cs[t][d0 + 2 * w], e1 = cs[t][d0 + 2 * w + 1];
-        const float x1a = __uint_as_float(w1[w] << 16), x1b = __uint_as_float(w1[w] & 0xffff0000u);
-        const float x2a = __uint_as_float(w2[w] << 16), x2b = __uint_as_float(w2[w] & 0xffff0000u);
-        const __nv_bfloat162 o1 = __floats2bfloat162_rn(fmaf(-x2a, e0.y, __fmul_rn(x1a, e0.x)), fmaf(-x2b, e1.y, __fmul_rn(x1b, e1.x)));
-        const __nv_bfloat162 o2 = __floats2bfloat162_rn(fmaf(x1a, e0.y, __fmul_rn(x2a, e0.x)), fmaf(x1b, e1.y, __fmul_rn(x2b, e1.x)));
-        w1[w] = *reinterpret_cast<const uint32_t*>(&o1);
-        w2[w] = *reinterpret_cast<const uint32_t*>(&o2);
+    for (int t = 0; t < APP_TOKENS; ++t) {
+      if (t >= n || (a.b.parent && depth_of[t] < 0) || (!is_q && page[t] < 0)) continue;
+      if (is_q || is_k) {
+        uint32_t w1[4] = {x1[t].x, x1[t].y, x1[t].z, x1[t].w}, w2[4] = {x2[t].x, x2[t].y, x2[t].z, x2[t].w};
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+          const float4 e = cs[t][w][ch];
+          const float x1a = __uint_as_float(w1[w] << 16), x1b = __uint_as_float(w1[w] & 0xffff0000u);
+          const float x2a = __uint_as_float(w2[w] << 16), x2b = __uint_as_float(w2[w] & 0xffff0000u);
+          const __nv_bfloat162 o1 = __floats2bfloat162_rn(fmaf(-x2a, e.y, __fmul_rn(x1a, e.x)), fmaf(-x2b, e.w, __fmul_rn(x1b, e.z)));
+          const __nv_bfloat162 o2 = __floats2bfloat162_rn(fmaf(x1a, e.y, __fmul_rn(x2a, e.x)), fmaf(x1b, e.w, __fmul_rn(x2b, e.z)));
+          w1[w] = *reinterpret_cast<const uint32_t*>(&o1);
+          w2[w] = *reinterpret_cast<const uint32_t*>(&o2);
+        }
+        x1[t] = make_uint4(w1[0], w1[1], w1[2], w1[3]);
+        x2[t] = make_uint4(w2[0], w2[1], w2[2], w2[3]);
       }
-      x1 = make_uint4(w1[0], w1[1], w1[2], w1[3]);
-      x2 = make_uint4(w2[0], w2[1], w2[2], w2[3]);
-    }
-    unsigned short* dst;
-    if (head < a.n_heads) {
-      dst = a.q_out + (static_cast<long long>(q.t0 + tok) * a.n_heads + head) * HD + d0;
-    } else {
-      const int kvh = (head - a.n_heads) % c.n_kv;
-      const bool is_k = head < a.n_heads + c.n_kv;
-      const int slot = q.used + tok, page = kv_page(c, s, slot);
-      if (page < 0) continue;
-      const long long row = kv_row(c, 0, page, kvh) + (slot & ((1 << c.page_shift) - 1));
-      dst = (is_k ? c.k : c.v) + row * HD + d0;
-      if (is_k && d0 == 0) {
-        if (c.mass) c.mass[row] = 0.0f;
-        c.pos[row] = seen + (a.b.parent ? depth_of[t] : tok);
+      unsigned short* dst;
+      if (is_q) {
+        dst = a.q_out + (static_cast<long long>(q.t0 + first + t) * a.n_heads + head) * HD + d0;
+      } else {
+        const int slot = q.used + first + t;
+        const long long row = kv_row(c, 0, page[t], kvh) + (slot & ((1 << c.page_shift) - 1));
+        dst = (is_k ? c.k : c.v) + row * HD + d0;
+        if (is_k && ch == 0) {
+          if (c.mass) c.mass[row] = 0.0f;
+          c.pos[row] = seen + (a.b.parent ? depth_of[t] : first + t);
+        }
       }
+      *reinterpret_cast<uint4*>(dst) = x1[t];
+      *reinterpret_cast<uint4*>(dst + HALF) = x2[t];
     }
-    *reinterpret_cast<uint4*>(dst) = x1;
-    *reinterpret_cast<uint4*>(dst + HALF) = x2;
   }
 }
 
@@ -232,9 +247,9 @@ struct PlanArgs {
 };
 
 __device__ __forceinline__ uint32_t plan_key(float w) {
-  if (w != w) return 1u;
   const uint32_t u = __float_as_uint(w + 0.0f);
-  return (u & 0x80000000u) ? ~u : (u | 0x80000000u);  // -inf is 0x007fffff: above NaN
+  const uint32_t k = u ^ (static_cast<uint32_t>(static_cast<int>(u) >> 31) | 0x80000000u);  // -inf is 0x007fffff: above NaN
+  return (u & 0x7fffffffu) > 0x7f800000u ? 1u : k;
 }
 
 template <int THREADS>
@@ -269,30 +284,36 @@ __global__ void __launch_bounds__(THREADS) kv_evict_plan_kernel(const PlanArgs a
   const long long base = kv_row(c, layer, 0, head);  // pool row of slot 0 of page 0
   const float* mass = c.mass + base;
   const int* pos = c.pos + base;
-  const int page_rows = c.n_kv << c.page_shift;
-  // Keys of slots 4 i .. 4 i + 3 when protected slots stay (or, `swap`, compete while the free ones go); lo, hi: range of the
+  const uint32_t page_rows = static_cast<uint32_t>(c.n_kv) << c.page_shift;  // rows of a layer are counted in 32 bits: memory ends before
+  // pos < sink or >= recent_from, in one comparison
+  const uint32_t sink = static_cast<uint32_t>(a.sink), span_free = recent_from > a.sink ? static_cast<uint32_t>(recent_from) - sink : 0u;
+  // Keys of slots 4 i .. 4 i + 3 when protected slots stay (or, SWAP, compete while the free ones go); lo, hi: range of the
   // keys that compete; n_p: protected slots.
-  auto keys_of = [&](int i, bool swap, const float4& m, const int4& ps, uint32_t& lo, uint32_t& hi, int& n_p) {
+  auto keys_of = [&](auto swapped, int i, const float4& m, const int4& ps, uint32_t& lo, uint32_t& hi, int& n_p) {
+    constexpr bool SWAP = decltype(swapped)::value;
     const float mv[4] = {m.x, m.y, m.z, m.w};
     const int pv[4] = {ps.x, ps.y, ps.z, ps.w};
     uint32_t k[4];
+    const int have = n - 4 * i;  // slots of this quad, if it is the last
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      const bool have = 4 * i + e < n, p = pv[e] >= recent_from || pv[e] < a.sink;
-      k[e] = plan_key(mv[e]);
-      const bool in = have && p == swap;
-      lo = in ? min(lo, k[e]) : lo;
-      hi = in ? max(hi, k[e]) : hi;
-      n_p += have && p;
-      k[e] = in ? k[e] : have && p ? 0xffffffffu : 0u;
+      const uint32_t key = plan_key(mv[e]);
+      const bool p = static_cast<uint32_t>(pv[e]) - sink >= span_free;
+      k[e] = p == SWAP ? key : SWAP ? 0u : 0xffffffffu;
+      if (have < 4 && e >= have) {
+        k[e] = 0u;
+        continue;
+      }
+      lo = min(lo, SWAP && !p ? 0xffffffffu : k[e]);
+      hi = max(hi, !SWAP && p ? 0u : k[e]);
+      n_p += p;
     }
     return make_uint4(k[0], k[1], k[2], k[3]);
   };
-  auto at_quad = [&](int i, int page) { return static_cast<long long>(page) * page_rows + ((4 * i) & slot_mask); };
-  bool swap = false, bad = false;
-  int P = 0;
-  uint32_t from, to;  // the threshold key lies in from .. to, which neither 0 nor the greatest key does; `want` slots of that range stay
-  while (true) {
+  auto at_quad = [&](int i, int page) { return static_cast<uint32_t>(page) * page_rows + static_cast<uint32_t>((4 * i) & slot_mask); };
+  bool bad = false;
+  uint32_t from = 0u, to = 0u;  // the threshold key lies in from .. to, which neither 0 nor the greatest key does; `want` slots of that range stay
+  auto read = [&](auto swapped) {
     if (threadIdx.x == 0) {
       n_prot = 0;
       group_lo = 0xffffffffu;
@@ -309,14 +330,14 @@ __global__ void __launch_bounds__(THREADS) kv_evict_plan_kernel(const PlanArgs a
       for (int j = 0; j < 2; ++j) {
         const int i = i0 + j * THREADS;
         page[j] = i < quads ? pages[(4 * i) >> c.page_shift] : 0;
-        if (page[j] < 0 || page[j] >= c.n_pages) {
+        if (static_cast<uint32_t>(page[j]) >= static_cast<uint32_t>(c.n_pages)) {
           bad = true;
           page[j] = 0;
         }
       }
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
-        const long long at = at_quad(i0 + j * THREADS, page[j]);
+        const uint32_t at = at_quad(i0 + j * THREADS, page[j]);
         m[j] = *reinterpret_cast<const float4*>(mass + at);
         ps[j] = *reinterpret_cast<const int4*>(pos + at);
       }
@@ -324,7 +345,7 @@ __global__ void __launch_bounds__(THREADS) kv_evict_plan_kernel(const PlanArgs a
       for (int j = 0; j < 2; ++j) {
         const int i = i0 + j * THREADS;
         if (i >= quads) break;
-        const uint4 k = keys_of(i, swap, m[j], ps[j], lo, hi, prot);
+        const uint4 k = keys_of(swapped, i, m[j], ps[j], lo, hi, prot);
         if (cached) key_s[i] = k;
       }
     }
@@ -336,24 +357,32 @@ __global__ void __launch_bounds__(THREADS) kv_evict_plan_kernel(const PlanArgs a
       atomicMin(&group_lo, lo);
       atomicMax(&group_hi, hi);
     }
-    if (__syncthreads_or(bad)) {
-      if (threadIdx.x == 0) { report_status(BITRL_ERR_SHAPE, KV_STAGE_BAD_PAGE); a.count[list] = 0; }
-      return;
-    }
-    P = n_prot;
+    if (__syncthreads_or(bad)) return -1;
     from = group_lo;
     to = group_hi;
-    if (swap || P < B) break;
-    swap = true;
+    return n_prot;
+  };
+  using Stay = std::integral_constant<bool, false>;
+  using Compete = std::integral_constant<bool, true>;
+  int P = read(Stay{});
+  const bool swap = P >= B;
+  if (swap) {
     __syncthreads();
+    P = read(Compete{});
+  }
+  if (P < 0) {
+    if (threadIdx.x == 0) { report_status(BITRL_ERR_SHAPE, KV_STAGE_BAD_PAGE); a.count[list] = 0; }
+    return;
   }
   int want = swap ? B : B - P;
   auto keys_at = [&](int i) -> uint4 {  // i < quads
     if (cached) return key_s[i];
-    const long long at = at_quad(i, pages[(4 * i) >> c.page_shift]);
+    const uint32_t at = at_quad(i, pages[(4 * i) >> c.page_shift]);
+    const float4 m = *reinterpret_cast<const float4*>(mass + at);
+    const int4 ps = *reinterpret_cast<const int4*>(pos + at);
     uint32_t lo = 0u, hi = 0u;
     int n_p = 0;
-    return keys_of(i, swap, *reinterpret_cast<const float4*>(mass + at), *reinterpret_cast<const int4*>(pos + at), lo, hi, n_p);
+    return swap ? keys_of(Compete{}, i, m, ps, lo, hi, n_p) : keys_of(Stay{}, i, m, ps, lo, hi, n_p);
   };
   uint32_t thr = from;
   int at_thr = 0;  // slots whose key is the threshold
@@ -503,12 +532,23 @@ __global__ void __launch_bounds__(THREADS) kv_evict_plan_kernel(const PlanArgs a
   for (int b = b0; b < b1; ++b) {
     const int i = 32 * b + lane;
     const uint32_t keep = keep_bits(i, ties), low = low_bits(i);
-    uint32_t src = keep & ~low, dst = ~keep & low;
+    const uint32_t src = keep & ~low, dst = ~keep & low;
+    if (!__any_sync(0xffffffffu, (src | dst) != 0u)) continue;
     const int mine = __popc(src) | (__popc(dst) << 16);
     const int incl = inclusive(mine), before = incl - mine, all = __shfl_sync(0xffffffffu, incl, 31);
-    int js = at_src + (before & 0xffff), jd = at_dst + (before >> 16);
-    for (; src; src &= src - 1u) out[2 * js++] = 4 * i + __ffs(src) - 1;
-    for (; dst; dst &= dst - 1u) out[2 * jd++ + 1] = 4 * i + __ffs(dst) - 1;
+    int* to_src = out + 2 * (at_src + (before & 0xffff));
+    int* to_dst = out + 2 * (at_dst + (before >> 16)) + 1;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      if ((src >> e) & 1u) {
+        *to_src = 4 * i + e;
+        to_src += 2;
+      }
+      if ((dst >> e) & 1u) {
+        *to_dst = 4 * i + e;
+        to_dst += 2;
+      }
+    }
     at_src += all & 0xffff;
     at_dst += all >> 16;
   }
