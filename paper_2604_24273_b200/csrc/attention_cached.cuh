@@ -489,7 +489,7 @@ attn_few_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constan
 // Per item (sequence, kv head): joins the results of the runs that met it, in run order, and adds every slot's weights,
 // p = 2^(score - lse), to mass.  The CTAs of an item share its slots, f.join_slots each, and the results, by threads (few parts)
 // or by pieces of 8 dimensions (many parts: 4 parts side by side in a warp).  Short chains of loads bound it, so each thread
-// keeps four to eight under way.
+// keeps several under way.
 template <int HD, int SR>
 __global__ void __launch_bounds__(AJ_THREADS) attn_few_join_kernel(const __grid_constant__ AfArgs f) {
   pdl_enter();
@@ -584,16 +584,16 @@ __global__ void __launch_bounds__(AJ_THREADS) attn_few_join_kernel(const __grid_
         const int x = i / (HD / 8), dim = (i - x * (HD / 8)) * 8 + d;
         const float m = max_s[x];
         float acc = 0.0f;
-        for (int kb = k0; kb < n; kb += 32) {
-          float v[8], mk[8];
+        for (int kb = k0; kb < n; kb += 64) {
+          float v[16], mk[16];
 #pragma unroll
-          for (int j = 0; j < 8; ++j) {
+          for (int j = 0; j < 16; ++j) {
             const int k = kb + 4 * j;
             v[j] = k < n ? a.part_o[(part(k) + x) * HD + dim] : 0.0f;
             mk[j] = k < n ? a.part_ml[part(k) + x].x : -INFINITY;
           }
 #pragma unroll
-          for (int j = 0; j < 8; ++j)
+          for (int j = 0; j < 16; ++j)
             if (mk[j] != -INFINITY) acc = fmaf(v[j], ac_exp2(mk[j] - m), acc);
         }
         acc += __shfl_xor_sync(0xffffffffu, acc, 8);

@@ -1395,9 +1395,9 @@ inline AcPlan ac_plan(const KvView& c, int T, int max_new, int n_heads) {
     // (100k slots of one sequence: 66 us against 82 .. 117; 128 sequences of up to 4096: 133 against 137 .. 139)
     p.runs = sm_count() * AF_WARPS * AF_CTAS;
     // slots of a CTA of the join: long stretches, unless they would leave SMs idle (2000 slots of one sequence: 13.3 us in
-    // stretches of 2048, 6 us in stretches of 512; 128 sequences: no difference)
+    // stretches of 2048, 9 us in stretches of 512, less in shorter ones; 128 sequences: no difference)
     const long long stretches = ((c.max_pages << c.page_shift) + 2047) / 2048;
-    p.join_slots = stretches * c.n_seq * c.n_kv < 4LL * sm_count() ? 512 : 2048;
+    p.join_slots = stretches * c.n_seq * c.n_kv < 4LL * sm_count() ? (stretches * c.n_seq * c.n_kv < sm_count() / 8 ? 256 : 512) : 2048;
     p.ml_bytes = ac_up(static_cast<size_t>(2 * p.runs) * p.rows_cap * 8);
     p.o_bytes = ac_up(static_cast<size_t>(2 * p.runs) * p.rows_cap * c.hd * 4);
     p.run_bytes = 256 + ac_up(static_cast<size_t>(c.n_seq) * c.n_kv * 4);
