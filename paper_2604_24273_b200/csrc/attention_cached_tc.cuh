@@ -221,7 +221,9 @@ attn_tiles_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
   __syncthreads();
   ptx::tc_fence_after_sync();
   const uint32_t tmem = misc[0];
-  pdl_enter();
+  // The kernels that follow may start only now: the weights pass reads the cache and the queries before it waits.
+  pdl_wait_before();
+  pdl_launch_next();
   AtCut* cuts = a.cuts + 2 * blockIdx.x;
   if (threadIdx.x < 2) cuts[threadIdx.x].s = -1;
   KvSeq q;
@@ -695,6 +697,7 @@ struct AmArgs {
   int tok_tile;
   int nx;       // items of the longest sequence that the page table can hold
   float* part;  // [CTAs][2][256] sums of cut items
+  AtCut* cuts;  // [CTAs][2], not those of the forward kernel, which are still read
 };
 
 // Row tiles that see some slot of item (s, x), from `first` on.
@@ -799,8 +802,10 @@ attn_mass_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_consta
   __syncthreads();
   ptx::tc_fence_after_sync();
   const uint32_t tmem = misc[0];
-  pdl_enter();
-  AtCut* cuts = a.cuts + 2 * blockIdx.x;
+  // Of what the two kernels before it write, this one reads the rows' statistics alone (warp 2 waits for them); what comes
+  // before the forward kernel is complete, since that lets its followers start only after its own wait.
+  pdl_launch_next();
+  AtCut* cuts = t.cuts + 2 * blockIdx.x;
   if (threadIdx.x < 2) cuts[threadIdx.x].s = -1;
   KvSeq q;
   int first;
@@ -888,6 +893,7 @@ attn_mass_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_consta
     if (!ok && lane == 0) give_up(AM_WAIT_MMA);
   } else if (warp == 2) {
     // ------------------------------------------------------------------ row statistics
+    pdl_wait_before();  // in every CTA, with work or without: what follows this kernel relies on it for what came before
     uint32_t n = 0;
     while (ok && more) {
       for (int u = w.u0; u < w.u1; ++u, ++n) {
@@ -1024,7 +1030,7 @@ __global__ void __launch_bounds__(AM_KEYS) attn_mass_join_kernel(const __grid_co
   pdl_enter();
   const AcArgs& a = t.a;
   const int c0 = blockIdx.x;
-  const AtCut head = a.cuts[2 * c0 + 1];
+  const AtCut head = t.cuts[2 * c0 + 1];
   if (head.s < 0) return;
   KvSeq q;
   if (!kv_seq(a.c, a.b, head.s, q)) return;
@@ -1032,7 +1038,7 @@ __global__ void __launch_bounds__(AM_KEYS) attn_mass_join_kernel(const __grid_co
   if (slot >= q.used + q.m) return;
   float sum = t.part[(2 * static_cast<long long>(c0) + 1) * AM_KEYS + threadIdx.x];
   for (int c = c0 + 1; c < n_ctas; ++c) {
-    const AtCut cut = a.cuts[2 * c];
+    const AtCut cut = t.cuts[2 * c];
     if (cut.s < 0) continue;  // a CTA whose run is empty
     sum += t.part[2 * static_cast<long long>(c) * AM_KEYS + threadIdx.x];
     if (cut.ends) break;
@@ -1109,7 +1115,7 @@ attn_mass_near_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_c
   __syncthreads();
   ptx::tc_fence_after_sync();
   const uint32_t tmem = misc[0];
-  pdl_enter();
+  pdl_launch_next();  // as in the form above: warp 2 waits
   KvSeq q;
   auto cost = [&](int s, int) {  // units of (sequence, head)
     if (!kv_seq(a.c, a.b, s, q) || q.m == 0 || (a.tree_ok && !a.tree_ok[s])) return 0;
@@ -1206,6 +1212,7 @@ attn_mass_near_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_c
     if (!ok && lane == 0) give_up(AM_WAIT_MMA);
   } else if (warp == 2) {
     // ------------------------------------------------------------------ row statistics
+    pdl_wait_before();
     uint32_t n = 0;
     while (ok && more) {
       const int rts = row_tiles();
@@ -1409,7 +1416,7 @@ inline AcPlan ac_plan(const KvView& c, int T, int max_new, int n_heads) {
     p.ctas = sm_count();
     p.ml_bytes = ac_up(static_cast<size_t>(2 * p.ctas) * p.rows_cap * 8);
     p.o_bytes = ac_up(static_cast<size_t>(2 * p.ctas) * p.rows_cap * c.hd * 4);
-    p.cut_bytes = ac_up(static_cast<size_t>(2 * p.ctas) * sizeof(AtCut));
+    p.cut_bytes = ac_up(static_cast<size_t>(4 * p.ctas) * sizeof(AtCut));  // of the forward and of the weights kernel
     p.sum_bytes = ac_up(static_cast<size_t>(2 * p.ctas) * AM_KEYS * 4);
   }
   return p;
@@ -1473,7 +1480,7 @@ bitrl_status launch_attention_cached_hd(const AcArgs& a, const AcPlan& p, bool m
     BITRL_CUDA(launch_pdl(attn_tiles_join_kernel<HD>, dim3(p.ctas, (p.rows_cap + 31) / 32), dim3(256), 0, st, t, p.ctas));
     count_launch(2);
     if (mass) {
-      const AmArgs m{a, p.tok_tile, ((a.c.max_pages << a.c.page_shift) + AM_KEYS - 1) / AM_KEYS, sums};
+      const AmArgs m{a, p.tok_tile, ((a.c.max_pages << a.c.page_shift) + AM_KEYS - 1) / AM_KEYS, sums, a.cuts + 2 * p.ctas};
       if (p.nx == 1) {  // at most two row tiles a sequence
         static bool near_done[64] = {false};
         if ((s = ac_smem(attn_mass_near_kernel<HD>, AnSmem<HD>::LAUNCH, near_done)) != BITRL_OK) return s;

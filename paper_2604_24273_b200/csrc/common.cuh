@@ -34,6 +34,10 @@ __device__ __forceinline__ void pdl_enter() {
   asm volatile("griddepcontrol.wait;" ::: "memory");
 }
 
+// The two halves apart: the next kernel may start / everything before this kernel is complete and visible.
+__device__ __forceinline__ void pdl_launch_next() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+__device__ __forceinline__ void pdl_wait_before() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+
 __device__ __forceinline__ float bf16_bits_to_float(unsigned short h) {
   return __uint_as_float(static_cast<unsigned>(h) << 16);
 }
