@@ -44,6 +44,9 @@ __device__ __forceinline__ float ac_exp2(float x) {
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
+// The maximum that a part of a row hands on.  Maxima pass over NaN: a part with nothing but NaN would look like one that sees
+// nothing (-inf) and be left out, so a sum that is NaN takes its maximum along.
+__device__ __forceinline__ float ac_part_max(float m, float l) { return l == l ? m : l; }
 __device__ __forceinline__ void mma_bf16(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
   asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
@@ -468,7 +471,7 @@ attn_few_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constan
           for (int d = 0; d < MD; ++d)
 #pragma unroll
             for (int i = 0; i < 2; ++i) to[16 * d + 8 * i] = o[n][d][2 * i + e];
-          if (g == 0) a.part_ml[static_cast<long long>(cut) * f.rows_cap + x] = make_float2(m_run[n][e], l);
+          if (g == 0) a.part_ml[static_cast<long long>(cut) * f.rows_cap + x] = make_float2(ac_part_max(m_run[n][e], l), l);
         }
       }
     left -= u1 - u0;
@@ -617,7 +620,8 @@ __global__ void __launch_bounds__(AJ_THREADS) attn_few_join_kernel(const __grid_
       for (int x = 0; x < SR / 4; ++x) {
         const float v[4] = {sc[i][x].x, sc[i][x].y, sc[i][x].z, sc[i][x].w};
 #pragma unroll
-        for (int e = 0; e < 4; ++e) got += lse[4 * x + e] == INFINITY ? 0.0f : ac_exp2(v[e] - lse[4 * x + e]);
+        for (int e = 0; e < 4; ++e)  // -inf: not seen by the row, whatever the row's sum is (it can be NaN)
+          got += lse[4 * x + e] == INFINITY || v[e] == -INFINITY ? 0.0f : ac_exp2(v[e] - lse[4 * x + e]);
       }
       a.c.mass[row[i]] = old[i] + got;
     }

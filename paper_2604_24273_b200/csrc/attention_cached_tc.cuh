@@ -575,7 +575,7 @@ attn_tiles_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
         }
         if (exists) {
           if (whole) a.lse[row] = none ? INFINITY : m_ref + __log2f(l);
-          else a.part_ml[static_cast<long long>(cut) * t.rows_cap + cut_row] = make_float2(m_ref, l);
+          else a.part_ml[static_cast<long long>(cut) * t.rows_cap + cut_row] = make_float2(ac_part_max(m_ref, l), l);
         }
         if (!whole && threadIdx.x == 128) cuts[w.u0 == 0 ? 1 : 0] = AtCut{w.s, w.x, w.h, w.u1 == w.units};
         ptx::tc_fence_before_sync();
