@@ -361,8 +361,9 @@ BITRL_API bitrl_status bitrl_bitlinear5_forward_multi(int32_t count, const bitrl
  * the sequence's new tokens) of the token that it continues, smaller than its own, BITRL_PARENT_PAST for a token that
  * continues the cached ones, BITRL_PARENT_PAD for a place that holds no token.  A tree has at most BITRL_TREE_MAX_TOKENS.
  * anc(i) = i and the tokens above it; depth(i) = |anc(i)| - 1 (= i without a tree).
- * What is wrong on the device (offsets, a parent that is not an earlier token, a page out of range, more slots than
- * max_pages hold) makes a call skip that sequence, and the next bitrl_poll_status returns BITRL_ERR_SHAPE. */
+ * What is wrong on the device (offsets, a parent that is not an earlier token, more slots than max_pages hold) makes a call
+ * skip that sequence; a page out of range is neither read nor written, and the sequence's results mean nothing then.  The
+ * other sequences get theirs, and the next bitrl_poll_status returns BITRL_ERR_SHAPE. */
 #define BITRL_TREE_MAX_TOKENS 256
 #define BITRL_KV_MAX_SLOTS (1 << 19) /* max_pages * page_tokens at most; beyond it BITRL_ERR_LIMIT */
 #define BITRL_KV_MAX_GROUP 64 /* query heads of a kv head at most; beyond it BITRL_ERR_LIMIT */
@@ -396,7 +397,9 @@ BITRL_API bitrl_status bitrl_kv_append(const bitrl_kv_cache_t* cache, int32_t la
  * statistics, the sums over keys and mass are fp32; att is rounded once to bf16.  Weights that enter the product with the
  * values through the tensor cores are rounded to bf16 beforehand where more than 16 rows share a tile.  The same call
  * gives the same bits: every sum has a fixed order.
- * workspace: dev, >= bitrl_attention_cached_workspace_bytes(cache, T, max_new_len, n_heads). */
+ * workspace: dev, >= bitrl_attention_cached_workspace_bytes(cache, T, max_new_len, n_heads), 0 for arguments that the call
+ * refuses.  Nothing in it outlives the call; calls that can run at the same time (other streams, graphs replayed side by
+ * side) need one each.  accumulate_mass with sequences that share pages is not allowed: both would add to the same slots. */
 BITRL_API size_t bitrl_attention_cached_workspace_bytes(const bitrl_kv_cache_t* cache, int32_t T, int32_t max_new_len,
                                                         int32_t n_heads);
 BITRL_API bitrl_status bitrl_attention_cached(const bitrl_kv_cache_t* cache, int32_t layer, const void* q, int32_t T,

@@ -112,6 +112,8 @@ __device__ __forceinline__ bool ac_is_pad(const uint32_t* anc, int tok) { return
 // the 4 HD bytes of its key and value) into the weight of every slot, so that keys are read once.
 // Scores come from mma.sync (eight rows fill its N; a tcgen05 tile has 128 rows).  The weights are split into two bf16
 // halves (16 significant bits), which costs nothing where reading bounds the kernel.
+// 128 sequences of up to 4096 slots, one token each, 20 heads over 5: 115 us for 633 MB, 5.5 TB/s (the join: 14 us); one
+// sequence of 100k slots: 49 + 14 us; of 2000: 12.5 us together, a chain of two launches and their loads.
 constexpr int AF_WARPS = 4;
 constexpr int AF_CTAS = 2;  // per SM
 constexpr int AF_THREADS = 32 * AF_WARPS;

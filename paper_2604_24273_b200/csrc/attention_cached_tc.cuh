@@ -120,7 +120,10 @@ struct AcWalk {
 //               the result is rescaled rarely.  Weights are rounded to bf16 for the product (2^-9 relative each, of random
 //               sign over the keys: below the rounding of the result itself); their sum is taken before the rounding.
 // Bound: 1024 cycles of exponentials and as many of products per 128 x 128 tile for long chunks (scores take 3/4 of the rate
-// with 64 columns, as both operands come from shared memory); the reading of keys and values for few rows.  Every wait is bounded; on expiry the CTA records a status word and leaves normally.
+// with 64 columns, as both operands come from shared memory); the reading of keys and values for few rows.
+// A chunk of 4096 tokens over 4100 slots (20 heads over 5 of 128): 235 us, 1.1 PFLOP/s, tensor pipe and exponentials busy for 56 %
+// of the cycles each; 64 states of 15 .. 40 tokens over 200 .. 2000 slots: 62 us; 16 trees of 48 over 1000 .. 8000: 59 us.
+// Every wait is bounded; on expiry the CTA records a status word and leaves normally.
 constexpr int AT_THREADS = 384;
 constexpr int AT_KEYS = 128;
 constexpr int AT_RING = 5;  // odd: a place holds keys and values in turn, so its V_READY barrier turns every second round
@@ -675,6 +678,7 @@ __global__ void __launch_bounds__(256) attn_tiles_join_kernel(const __grid_const
 //   warp 0 producer (keys of an item, double-buffered; queries through a ring of two), warp 1 MMA (two accumulators per key
 //   tile), warp 2 row statistics, warps 4-11 and 12-19 the sums of key tile 0 and 1, four warps for every other unit.
 // Bound: 1024 cycles of exponentials per 128 x 128 tile (the products take 512) for long chunks; reading for short ones.
+// A chunk of 4096 tokens over 4100 slots: 203 us, the exponentials' pipe busy for 59 % of the cycles.
 constexpr int AM_THREADS = 640;
 constexpr int AM_KEYS = 256;
 enum { AM_WAIT_LOAD = 141, AM_WAIT_MMA = 142, AM_WAIT_LSE = 143, AM_WAIT_SUM = 144 };
@@ -1052,7 +1056,7 @@ __global__ void __launch_bounds__(AM_KEYS) attn_mass_join_kernel(const __grid_co
 // belongs to one CTA, so nothing is left to join.  Warps as above; with two row tiles four warps take each accumulator of a
 // unit, with one they take every other unit of their key tile.  The sums go through shared memory to warp 3, which fetched
 // the places that they are added to one unit earlier: page, weight and sum one after the other in the summing warps cost
-// them 2 us a unit.  (In the form above, whose items reload their queries, trees of 48 tokens over 8000 slots took 84 us.)
+// them 2 us a unit.  (In the form above, whose items reload their queries, trees of 48 tokens over 8000 slots took 84 us; here 48.)
 template <int HD>
 struct AnSmem {
   static constexpr uint32_t TILE = 128 * HD * 2, HALF = 128 * 128;

@@ -237,3 +237,25 @@ def test_many_sequences_of_nothing_much(B):
         att = B.attention_cached(g, 0, q.cuda(), (off.cuda(), top), 5)
         B.poll_status()
         check(att, g.mass, c, q, off, 5)
+
+
+def test_counts_that_cannot_be(B):
+    """Device-side refusals of the counters and of a list longer than a sequence has slots."""
+    c = ref.make(151, [20, 30], [1, 1], 2, 64, 16)
+    g = on_gpu(B, c)
+    room = c["page_table"].shape[1] * 16
+    moves = torch.zeros(2, room + 5, 2, dtype=torch.int32, device="cuda")
+    before = [x.clone() for x in (g.k, g.v, g.mass, g.pos)]
+    B.kv_move(g, moves, torch.tensor([room + 1, 0], dtype=torch.int32, device="cuda"))
+    with pytest.raises(B.BitrlError):
+        B.poll_status()
+    assert all(same(x, y) for x, y in zip(before, (g.k, g.v, g.mass, g.pos)))
+    for name in ("used", "seen"):
+        g = on_gpu(B, c)
+        getattr(g, name)[0] = -1
+        B.kv_advance(g, 1)
+        with pytest.raises(B.BitrlError):
+            B.poll_status()
+        assert int(getattr(g, name)[0]) == -1
+        other = "used" if name == "seen" else "seen"
+        assert int(getattr(g, other)[0]) == int(c[other][0]) and int(g.used[1]) == 31
