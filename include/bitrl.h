@@ -382,7 +382,7 @@ typedef struct bitrl_kv_cache {
 
 /* Appends the new tokens to layer `layer`: q and k of qkv (dev bf16 [T, (n_heads + 2 n_kv_heads) * head_dim] = [q|k|v]) are
  * rotated by their position seen[s] + depth(i), as for bitrl_attention (angles in fp64, rotation in fp32, one rounding to
- * bf16); q goes to q_out (dev bf16 [T, n_heads * head_dim]), k and v to their slots, mass becomes 0, pos the position.
+ * bf16); q goes to q_out (dev bf16 [T, n_heads * head_dim], not overlapping qkv: BITRL_ERR_SHAPE), k and v to their slots, mass becomes 0, pos the position.
  * Padding writes nothing. */
 BITRL_API bitrl_status bitrl_kv_append(const bitrl_kv_cache_t* cache, int32_t layer, const void* qkv, int32_t T,
                                        const int32_t* state_off, int32_t max_new_len, const int32_t* parent,
@@ -392,7 +392,8 @@ BITRL_API bitrl_status bitrl_kv_append(const bitrl_kv_cache_t* cache, int32_t la
  *   token i of s sees A(i) = {slots 0 .. used[s]-1} and {slots used[s] + j : j in anc(i)}
  *   p_r = softmax over r in A(i) of q_i . k_r / sqrt(head_dim);  att_i = sum_r p_r v_r           per query head
  *   mass[slot r] += sum over the tokens and over the query heads of the kv head of p_r           if accumulate_mass
- * Query head h reads kv head h / (n_heads / n_kv_heads).  q, att: dev bf16 [T, n_heads * head_dim].  Padding gets zeros
+ * Query head h reads kv head h / (n_heads / n_kv_heads).  q, att: dev bf16 [T, n_heads * head_dim], not
+ * overlapping (BITRL_ERR_SHAPE).  Padding gets zeros
  * and adds nothing; a slot that a token does not see has no part in its result, whatever it holds.  Scores, softmax
  * statistics, the sums over keys and mass are fp32; att is rounded once to bf16.  Weights that enter the product with the
  * values through the tensor cores are rounded to bf16 beforehand where more than 16 rows share a tile.  The same call
@@ -434,7 +435,7 @@ BITRL_API bitrl_status bitrl_kv_advance(const bitrl_kv_cache_t* cache, const int
 /* The encoder over a cache: blocks as in bitrl_encoder_forward_states, with block l's attention by bitrl_kv_append and
  * bitrl_attention_cached on layer l.  The cache has at least as many layers as the encoder and its head counts.  pooled: NULL, or dev bf16
  * [n_seq, d], the last new token of every sequence (rows of sequences without new tokens are left as they are).
- * workspace >= bitrl_encoder_cached_workspace_bytes(enc, cache, T, max_new_len).  used and seen are not advanced. */
+ * Rows of h_out behind the last sequence hold nothing of meaning.  workspace >= bitrl_encoder_cached_workspace_bytes(enc, cache, T, max_new_len).  used and seen are not advanced. */
 BITRL_API size_t bitrl_encoder_cached_workspace_bytes(const bitrl_encoder_t* enc, const bitrl_kv_cache_t* cache, int32_t T,
                                                       int32_t max_new_len);
 BITRL_API bitrl_status bitrl_encoder_forward_cached(const bitrl_encoder_t* enc, const bitrl_kv_cache_t* cache,

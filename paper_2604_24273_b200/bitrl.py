@@ -469,6 +469,7 @@ def pool_last_token(h: torch.Tensor, states) -> torch.Tensor:
 PARENT_PAST, PARENT_PAD = -1, -2
 TREE_MAX_TOKENS = 256
 KV_MAX_SLOTS = 1 << 19
+KV_MAX_GROUP = 64  # query heads of a kv head
 
 
 def _here(t: torch.Tensor, dtype, name: str, index: int) -> int:
@@ -487,7 +488,8 @@ class KVCache:
 
     ``k``, ``v``: bf16 [n_layers, n_pages, n_kv_heads, page_tokens, head_dim]; ``page_table``: int32 [n_seq, max_pages];
     ``used``, ``seen``: int32 [n_seq]; ``mass`` fp32 and ``pos`` int32 [n_layers, n_pages, n_kv_heads, page_tokens]
-    (``mass`` may be None: nothing accumulates and nothing can be evicted by weight)."""
+    (``mass`` may be None: nothing accumulates and nothing can be evicted by weight).  The library keeps their addresses: change
+    them in place."""
 
     def __init__(self, k, v, page_table, used, seen, mass=None, pos=None):
         _dev(k, torch.bfloat16, "k")

@@ -630,6 +630,11 @@ KvView kv_view(const bitrl_kv_cache_t* c, int layer) {
                 c->mass ? c->mass + rows : nullptr, c->pos + rows, c->page_table, c->used, c->seen,
                 c->n_layers, c->n_pages, c->n_kv_heads, shift, c->head_dim, c->n_seq, c->max_pages};
 }
+// Do two ranges of bf16 values share memory?
+bool kv_overlap(const void* x, long long nx, const void* y, long long ny) {
+  const uintptr_t a = reinterpret_cast<uintptr_t>(x), b = reinterpret_cast<uintptr_t>(y);
+  return a < b + 2 * static_cast<uintptr_t>(ny) && b < a + 2 * static_cast<uintptr_t>(nx);
+}
 // Lists of a call over all layers (one per layer, sequence and kv head).
 bool kv_lists_ok(const bitrl_kv_cache_t* c) {
   return static_cast<long long>(c->n_layers) * c->n_seq * c->n_kv_heads <= INT_MAX / 1024;
@@ -646,6 +651,8 @@ bitrl_status bitrl_kv_append(const bitrl_kv_cache_t* cache, int32_t layer, const
   if (T == 0 || max_new_len == 0) return BITRL_OK;
   if (!qkv || !q_out) return BITRL_ERR_NULL;
   if (!aligned16(qkv) || !aligned16(q_out)) return BITRL_ERR_ALIGN;
+  const long long q_row = static_cast<long long>(n_heads) * cache->head_dim;
+  if (kv_overlap(qkv, T * (q_row + 2LL * cache->n_kv_heads * cache->head_dim), q_out, T * q_row)) return BITRL_ERR_SHAPE;
   if ((s = check_arch()) != BITRL_OK) return s;
   return launch_kv_append(kv_view(cache, layer), KvBatch{state_off, parent, max_new_len, T}, qkv, n_heads, theta, q_out,
                           static_cast<cudaStream_t>(stream));
@@ -673,6 +680,8 @@ bitrl_status bitrl_attention_cached(const bitrl_kv_cache_t* cache, int32_t layer
   if (!p.launchable(c)) return BITRL_ERR_LIMIT;
   if (!workspace || workspace_bytes < p.bytes()) return BITRL_ERR_WORKSPACE;
   if (!aligned16(q) || !aligned16(att) || !aligned16(workspace)) return BITRL_ERR_ALIGN;
+  const long long elems = static_cast<long long>(T) * n_heads * cache->head_dim;
+  if (kv_overlap(q, elems, att, elems)) return BITRL_ERR_SHAPE;  // other CTAs still read q
   if ((s = check_arch()) != BITRL_OK) return s;
   return launch_attention_cached(c, KvBatch{state_off, parent, max_new_len, T}, q, n_heads, accumulate_mass != 0, att,
                                  workspace, static_cast<cudaStream_t>(stream));

@@ -599,6 +599,7 @@ struct MoveArgs {
   const int* moves;
   const int* count;
   int max_moves, per_head, splits;
+  int most;  // sources ascend: a list holds no more than max_moves, and no more than there are slots
 };
 
 template <int HD, int THREADS>
@@ -614,7 +615,7 @@ __global__ void __launch_bounds__(THREADS) kv_move_kernel(const MoveArgs a) {
   const int which = a.per_head ? list : s;
   const int n = a.count[which];
   const int2* mv = reinterpret_cast<const int2*>(a.moves) + static_cast<long long>(which) * a.max_moves;
-  if (n < 0 || n > a.max_moves || n > (c.max_pages << c.page_shift)) {  // sources ascend: never more than slots
+  if (n < 0 || n > a.most) {
     if (threadIdx.x == 0) report_status(BITRL_ERR_SHAPE, KV_STAGE_BAD_MOVE);
     return;
   }
@@ -707,7 +708,8 @@ bitrl_status launch_kv_move_hd(MoveArgs a, cudaStream_t st) {
 }
 
 bitrl_status launch_kv_move(const KvView& c, const int* moves, const int* count, int max_moves, int per_head, cudaStream_t st) {
-  const MoveArgs a{c, moves, count, max_moves, per_head, 1};
+  const int room = c.max_pages << c.page_shift;
+  const MoveArgs a{c, moves, count, max_moves, per_head, 1, max_moves < room ? max_moves : room};
   return c.hd == 128 ? launch_kv_move_hd<128>(a, st) : launch_kv_move_hd<64>(a, st);
 }
 

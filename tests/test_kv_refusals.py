@@ -93,6 +93,23 @@ def test_nothing_to_do_is_fine_without_a_device(L):
     assert L.bitrl_kv_move(desc(), None, None, 0, 1, None) == bitrl.OK
 
 
+def test_outputs_that_overlap_inputs(L):
+    q = 6 * 4 * 64 * 2  # bytes of the six tokens' queries
+    for at in (P, P + q - 16, P - q + 16):
+        assert append(L, q=at) == bitrl.ERR_SHAPE
+        assert attend(L, att=at) == bitrl.ERR_SHAPE
+    assert append(L, q=P + 2 * q - 16) == bitrl.ERR_SHAPE  # the values of the last token
+    if not bitrl.torch.cuda.is_available():  # beside one another: the next check is the device's
+        assert append(L, q=P + 2 * q) not in (bitrl.OK, bitrl.ERR_SHAPE)
+        assert attend(L, att=P + q) not in (bitrl.OK, bitrl.ERR_SHAPE) and attend(L, att=P - q) not in (bitrl.OK, bitrl.ERR_SHAPE)
+
+
+def test_a_group_that_is_too_large(L):
+    assert attend(L, desc(n_kv_heads=1), nh=bitrl.KV_MAX_GROUP + 1) == bitrl.ERR_LIMIT
+    assert append(L, desc(n_kv_heads=1), nh=bitrl.KV_MAX_GROUP + 1) == bitrl.ERR_LIMIT
+    assert L.bitrl_attention_cached_workspace_bytes(desc(n_kv_heads=1), 6, 4, bitrl.KV_MAX_GROUP + 1) == 0
+
+
 def test_workspace_query(L):
     assert L.bitrl_attention_cached_workspace_bytes(desc(), 6, 4, 4) > 0
     assert L.bitrl_attention_cached_workspace_bytes(desc(head_dim=80), 6, 4, 4) == 0
