@@ -397,7 +397,14 @@ __global__ void __launch_bounds__(THREADS) kv_evict_plan_kernel(const PlanArgs a
       f(k.w);
     }
   };
-  while (true) {
+  // Each round takes 11 bits off the span, so three end it.  The bounds here and in the lists below hold even if weights change
+  // meanwhile (a call on another stream, which is not allowed): then keys read twice contradict one another.
+  if (threadIdx.x == 0) {
+    chosen = 0u;
+    wanted = inside = 0;
+  }
+#pragma unroll 1
+  for (int round = 0; round < 4; ++round) {
     const uint32_t span = to - from;
     const int shift = span < PLAN_BINS ? 0 : 21 - __clz(span);  // span >> shift < PLAN_BINS
     for (int i = threadIdx.x; i < PLAN_BINS; i += THREADS) hist[i] = 0;
@@ -527,7 +534,7 @@ __global__ void __launch_bounds__(THREADS) kv_evict_plan_kernel(const PlanArgs a
   if (threadIdx.x == 0) {
     int total = 0;
     for (int w = 0; w < WARPS; ++w) total += part[w];
-    a.count[list] = total;
+    a.count[list] = min(total, a.max_moves);
   }
   int* out = a.moves + static_cast<long long>(list) * a.max_moves * 2;
   ties = ties0;
@@ -540,6 +547,9 @@ __global__ void __launch_bounds__(THREADS) kv_evict_plan_kernel(const PlanArgs a
     const int incl = inclusive(mine), before = incl - mine, all = __shfl_sync(0xffffffffu, incl, 31);
     int* to_src = out + 2 * (at_src + (before & 0xffff));
     int* to_dst = out + 2 * (at_dst + (before >> 16)) + 1;
+    at_src += all & 0xffff;
+    at_dst += all >> 16;
+    if (max(at_src, at_dst) > a.max_moves) break;
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       if ((src >> e) & 1u) {
@@ -551,8 +561,6 @@ __global__ void __launch_bounds__(THREADS) kv_evict_plan_kernel(const PlanArgs a
         to_dst += 2;
       }
     }
-    at_src += all & 0xffff;
-    at_dst += all >> 16;
   }
 }
 
