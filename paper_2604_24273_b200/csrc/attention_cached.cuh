@@ -63,6 +63,19 @@ __device__ __forceinline__ uint32_t pack_bf16x2(float x0, float x1) {
   const __nv_bfloat162 p = __floats2bfloat162_rn(x0, x1);
   return *reinterpret_cast<const uint32_t*>(&p);
 }
+// Weights p0, p1 >= 0 as two bf16 halves each, p = hi + lo (p0 in the low half of a word): 16 significant bits, where one bf16 would
+// move a result of few keys by up to 2^-8 of their magnitudes, as much as its own rounding.  hi is cut, not rounded, and 2^-20 of p
+// keeps lo above zero wherever p is (down to 2^-113): hi and lo then have one sign, and the two products with a value that is infinite
+// are the same infinity.
+__device__ __forceinline__ void ac_split(float p0, float p1, uint32_t& hi, uint32_t& lo) {
+  const uint32_t b0 = __float_as_uint(p0), b1 = __float_as_uint(p1);
+  hi = __byte_perm(b0, b1, 0x7632);
+  constexpr float up = 1.0f + 0x1p-20f;
+  float l0, l1;
+  ptx::unpack_f32x2(ptx::fma_f32x2(ptx::pack_f32x2(b0, b1), ptx::pack_f32x2(__float_as_uint(up), __float_as_uint(up)),
+                                   ptx::pack_f32x2((b0 & 0xffff0000u) | 0x80000000u, (b1 & 0xffff0000u) | 0x80000000u)), l0, l1);
+  lo = pack_bf16x2(l0, l1);
+}
 // Ancestors of every new token as bits, anc[row][AC_TREE_WORDS]: bit j is set when token j of the sequence is the token
 // itself or above it; padding has no bits.  desc is the transpose.  ok[s]: the sequence's tree is one.  One CTA per sequence.
 __global__ void __launch_bounds__(BITRL_TREE_MAX_TOKENS)

@@ -109,7 +109,7 @@ struct AcWalk {
 // An item is 256 rows (two tiles of 128, whole tokens each) of one kv head; a unit is 128 slots of its keys.  One CTA per SM:
 //   warp 0      producer: queries of an item (3-D TMA: dims x heads of the group x tokens), then per unit the keys and the
 //               values, page by page, 128-byte swizzled, through a ring of five tiles
-//   warps 1, 2  MMA: S_a = Q_a K^T and O_a += P_a V for row tile a, 64 slots at a time (one issuer for both was what the
+//   warps 1, 2  MMA: S_a = Q_a K^T and O_a += (P_a hi + P_a lo) V for row tile a, 64 slots at a time (one issuer for both was what the
 //               kernel waited for: 2400 cycles a step, of which 1360 issuing and 1000 in waits); each row tile has two score
 //               buffers, so the scores of the next 64 slots are there when the softmax of the last 64 ends.  P replaces S in
 //               tensor memory (A operand); V is the MN-major B operand.  512 columns: 2 x (2 x 64 of S, 128 of O).
@@ -117,8 +117,9 @@ struct AcWalk {
 //               become zero, and so do values that are not finite (rows that do see them get them back at the end)
 //   warps 4-7, 8-11   softmax of row tile 0 / 1, one row per thread: no exchange between threads.  The running maximum is
 //               followed only when it has grown by more than 2^8 (weights stay below 2^8, statistics and sums are fp32), so
-//               the result is rescaled rarely.  Weights are rounded to bf16 for the product (2^-9 relative each, of random
-//               sign over the keys: below the rounding of the result itself); their sum is taken before the rounding.
+//               the result is rescaled rarely.  Weights enter the product as two bf16 halves (ac_split), side by side in
+//               the 64 columns that their scores leave; their sum is taken before.  (One bf16 each, half the value products,
+//               added as much error as the rounding of the result: a chunk took 489 us with its weights pass in place of 564.)
 // Bound: 1024 cycles of exponentials and as many of products per 128 x 128 tile for long chunks (scores take 3/4 of the rate
 // with 64 columns, as both operands come from shared memory); the reading of keys and values for few rows.
 // A chunk of 4096 tokens over 4100 slots (20 heads over 5 of 128): 235 us, 1.1 PFLOP/s, tensor pipe and exponentials busy for 56 %
@@ -347,8 +348,8 @@ attn_tiles_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
         if (ptx::elect_one()) {
           const uint64_t vd = ptx::smem_desc_mn_sw128(base + M::RING + (ve % AT_RING) * M::TILE + b * 8192, M::HALF);
 #pragma unroll
-          for (int k = 0; k < 4; ++k)
-            ptx::mma_bf16_ts(tmem + 256 + 128 * x, tmem + 128 * x + 64 * b + 8 * k, vd + k * (2048 >> 4), id_o, i != 0 || k != 0);
+          for (int k = 0; k < 8; ++k)  // the upper halves of the weights, then the lower ones
+            ptx::mma_bf16_ts(tmem + 256 + 128 * x, tmem + 128 * x + 64 * b + 8 * k, vd + (k & 3) * (2048 >> 4), id_o, i != 0 || k != 0);
           ptx::mma_commit(base + M::O_DONE + 8 * (2 * x + b));
         }
         __syncwarp();
@@ -501,7 +502,7 @@ attn_tiles_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
           const float sub = m_ref == -INFINITY ? 0.0f : -m_ref;
           const uint64_t sub_x2 = ptx::pack_f32x2(__float_as_uint(sub), __float_as_uint(sub));
           uint64_t sum[2] = {0ull, 0ull};
-          uint32_t p[32];
+          uint32_t p[2][32];  // upper and lower halves of the weights
 #pragma unroll
           for (int j = 0; j < 32; ++j) {
             const int c = j >> 4, k = 2 * (j & 15);
@@ -510,9 +511,10 @@ attn_tiles_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
             p0 = ac_exp2(p0);
             p1 = ac_exp2(p1);
             sum[j & 1] = ptx::add_f32x2(sum[j & 1], ptx::pack_f32x2(__float_as_uint(p0), __float_as_uint(p1)));
-            p[j] = pack_bf16x2(p0, p1);
+            ac_split(p0, p1, p[0][j], p[1][j]);
           }
-          ptx::tmem_st_32x32b_x32(s_addr + 64 * b, p);
+          ptx::tmem_st_32x32b_x32(s_addr + 64 * b, p[0]);
+          ptx::tmem_st_32x32b_x32(s_addr + 64 * b + 32, p[1]);
           float l0, l1;
           ptx::unpack_f32x2(ptx::add_f32x2(sum[0], sum[1]), l0, l1);
           l += l0 + l1;
