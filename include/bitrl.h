@@ -396,7 +396,8 @@ BITRL_API bitrl_status bitrl_kv_append(const bitrl_kv_cache_t* cache, int32_t la
  * overlapping (BITRL_ERR_SHAPE).  Padding gets zeros
  * and adds nothing; a slot that a token does not see has no part in its result, whatever it holds.  Scores, softmax
  * statistics, the sums over keys and mass are fp32; att is rounded once to bf16.  Weights meet the values on the tensor cores
- * as two bf16 halves (16 significant bits).  The same call gives the same bits: every sum has a fixed order.
+ * as two bf16 halves (16 significant bits); a value that is not finite reaches every row that sees its slot, as in fp32 products
+ * and sums (an infinity of one sign stays one).  The same call gives the same bits: every sum has a fixed order.
  * workspace: dev, >= bitrl_attention_cached_workspace_bytes(cache, T, max_new_len, n_heads), 0 for arguments that the call
  * refuses.  Nothing in it outlives the call; calls that can run at the same time (other streams, graphs replayed side by
  * side) need one each.  accumulate_mass with sequences that share pages is not allowed: both would add to the same slots. */

@@ -411,10 +411,10 @@ attn_few_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constan
         for (int n = 0; n < NG; ++n)
 #pragma unroll
           for (int i = 0; i < 2; ++i) {
-            const float p0 = c[n][2 * i], p1 = c[n][2 * i + 1];
-            const uint32_t hi = pack_bf16x2(p0, p1);
+            uint32_t hi, lo;
+            ac_split(c[n][2 * i], c[n][2 * i + 1], hi, lo);
             ph[n][i] = movmatrix_trans(hi);
-            pl[n][i] = movmatrix_trans(pack_bf16x2(p0 - __uint_as_float(hi << 16), p1 - __uint_as_float(hi & 0xffff0000u)));
+            pl[n][i] = movmatrix_trans(lo);
           }
 #pragma unroll
         for (int d = 0; d < MD; ++d) {

@@ -67,3 +67,45 @@ def test_weights_meet_the_values_with_sixteen_bits(B, nh, nkv, hd, page, used, n
     want, tol = exact(c, q, off, nh, par)
     err = (att.cpu().double().reshape(want.shape) - want).abs() - tol
     assert not att.isnan().any() and err.max() <= 0, f"{float(err.max()):.3g} beyond, {int((err > 0).sum())} of {err.numel()}"
+
+
+@pytest.mark.parametrize("nh,nkv,hd,page,used,news,is_tree", FORMS + [(8, 1, 128, 64, [5000, 130], [1, 1], False)])
+def test_infinite_values_reach_those_who_see_them(B, nh, nkv, hd, page, used, news, is_tree):
+    """An infinite value in a slot that a row sees makes that dimension of the row's result the same infinity (both signs: NaN),
+    whatever the weight's bits are; every other result, and the weights, stay what they were."""
+    c = ref.make(221, used, news, nkv, hd, page, scale=0.25)
+    par = torch.tensor([p for s, m in enumerate(news) for p in ref.tree(230 + s, m)], dtype=torch.int32) if is_tree else None
+    q = fill_new(c, 222, news, par, nh, scale=0.25)
+    off = ref.offsets(news)
+    states = (off.cuda(), max(news))
+    gp = None if par is None else par.cuda()
+    plain = on_gpu(B, c)
+    B.attention_cached(plain, 0, q.cuda(), states, nh, parent=gp)
+    g = ref.gen(223)
+    up, down = (torch.zeros(q.shape[0], nh, hd, dtype=torch.bool) for _ in range(2))
+    for s, (u, m) in enumerate(zip(used, news)):
+        t0, rep = int(off[s]), nh // nkv
+        tree = [i - 1 for i in range(m)] if par is None else par[t0 : t0 + m].tolist()
+        slots = sorted({0, u // 3, u // 2, max(u - 1, 0), u + m // 2, u + m - 1})
+        for h in range(nkv):
+            for slot in slots:
+                dims = torch.randperm(hd, generator=g)[: hd // 6]
+                sign = torch.where(torch.rand(len(dims), generator=g) < 0.5, 1.0, -1.0)
+                pg, at = ref.at(c, s, [slot])
+                c["v"][0, pg[0], h, at[0], dims] = (sign * math.inf).to(torch.bfloat16)
+                for i in range(m):
+                    if slot < u or slot - u in ref.above(tree, i):
+                        for j in range(h * rep, (h + 1) * rep):
+                            up[t0 + i, j, dims] |= sign > 0
+                            down[t0 + i, j, dims] |= sign < 0
+    # what the finite values of a dimension give; the infinite ones count as zero in `want`
+    zeroed = {**c, "v": torch.where(c["v"].isinf(), 0.0, c["v"])}
+    want, tol = exact(zeroed, q, off, nh, par)
+    got = on_gpu(B, c)
+    att = B.attention_cached(got, 0, q.cuda(), states, nh, parent=gp).cpu().double().reshape(want.shape)
+    B.poll_status()
+    assert (up & ~down).any() and (down & ~up).any() and not (up | down).all()
+    assert (att[up & ~down] == math.inf).all() and (att[down & ~up] == -math.inf).all() and att[up & down].isnan().all()
+    rest = ~(up | down)
+    assert ((att - want).abs()[rest] <= tol[rest]).all()
+    assert torch.equal(got.mass, plain.mass)
