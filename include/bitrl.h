@@ -398,7 +398,7 @@ BITRL_API bitrl_status bitrl_kv_append(const bitrl_kv_cache_t* cache, int32_t la
  * statistics, the sums over keys and mass are fp32; att is rounded once to bf16.  Weights meet the values on the tensor cores
  * as two bf16 halves (16 significant bits); a value that is not finite reaches every row that sees its slot, as in fp32 products
  * and sums (an infinity of one sign stays one).  The same call gives the same bits: every sum has a fixed order.
- * workspace: dev, >= bitrl_attention_cached_workspace_bytes(cache, T, max_new_len, n_heads), 0 for arguments that the call
+ * workspace: dev, >= bitrl_attention_cached_workspace_bytes(cache, T, max_new_len, n_heads), 0 for a cache and sizes that the call
  * refuses.  Nothing in it outlives the call; calls that can run at the same time (other streams, graphs replayed side by
  * side) need one each.  accumulate_mass with sequences that share pages is not allowed: both would add to the same slots. */
 BITRL_API size_t bitrl_attention_cached_workspace_bytes(const bitrl_kv_cache_t* cache, int32_t T, int32_t max_new_len,
@@ -435,7 +435,8 @@ BITRL_API bitrl_status bitrl_kv_advance(const bitrl_kv_cache_t* cache, const int
 /* The encoder over a cache: blocks as in bitrl_encoder_forward_states, with block l's attention by bitrl_kv_append and
  * bitrl_attention_cached on layer l.  The cache has at least as many layers as the encoder and its head counts.  pooled: NULL, or dev bf16
  * [n_seq, d], the last new token of every sequence (rows of sequences without new tokens are left as they are).
- * Rows of h_out behind the last sequence hold nothing of meaning.  workspace >= bitrl_encoder_cached_workspace_bytes(enc, cache, T, max_new_len).  used and seen are not advanced. */
+ * Rows of h_out behind the last sequence hold nothing of meaning.  workspace >= bitrl_encoder_cached_workspace_bytes(enc, cache, T,
+ * max_new_len), 0 for a cache and sizes that the call refuses.  used and seen are not advanced. */
 BITRL_API size_t bitrl_encoder_cached_workspace_bytes(const bitrl_encoder_t* enc, const bitrl_kv_cache_t* cache, int32_t T,
                                                       int32_t max_new_len);
 BITRL_API bitrl_status bitrl_encoder_forward_cached(const bitrl_encoder_t* enc, const bitrl_kv_cache_t* cache,

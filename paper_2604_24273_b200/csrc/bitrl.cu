@@ -630,6 +630,13 @@ KvView kv_view(const bitrl_kv_cache_t* c, int layer) {
                 c->mass ? c->mass + rows : nullptr, c->pos + rows, c->page_table, c->used, c->seen,
                 c->n_layers, c->n_pages, c->n_kv_heads, shift, c->head_dim, c->n_seq, c->max_pages};
 }
+// For the size queries: does an attention call of these sizes get past its checks?  (Offsets and a tree, which are not known here,
+// can still have it refused.)  ac_plan relies on them: a group of more than 128 heads would leave no token in a tile.
+bool kv_sizes_ok(const bitrl_kv_cache_t* c, int32_t T, int32_t max_new, int32_t n_heads) {
+  return kv_check(c) == BITRL_OK && T >= 1 && max_new >= 1 &&
+         kv_check_batch(c, 0, T, c->page_table /* not null: sequences of any lengths */, max_new, nullptr, n_heads) == BITRL_OK &&
+         ac_plan(kv_view(c, 0), T, max_new, n_heads).launchable(kv_view(c, 0));
+}
 // Do two ranges of bf16 values share memory?
 bool kv_overlap(const void* x, long long nx, const void* y, long long ny) {
   const uintptr_t a = reinterpret_cast<uintptr_t>(x), b = reinterpret_cast<uintptr_t>(y);
@@ -659,10 +666,7 @@ bitrl_status bitrl_kv_append(const bitrl_kv_cache_t* cache, int32_t layer, const
 }
 
 size_t bitrl_attention_cached_workspace_bytes(const bitrl_kv_cache_t* cache, int32_t T, int32_t max_new_len, int32_t n_heads) {
-  if (kv_check(cache) != BITRL_OK || T < 1 || max_new_len < 1 || n_heads < 1 || n_heads % cache->n_kv_heads != 0 ||
-      n_heads / cache->n_kv_heads > BITRL_KV_MAX_GROUP)
-    return 0;
-  return ac_plan(kv_view(cache, 0), T, max_new_len, n_heads).bytes();
+  return kv_sizes_ok(cache, T, max_new_len, n_heads) ? ac_plan(kv_view(cache, 0), T, max_new_len, n_heads).bytes() : 0;
 }
 
 bitrl_status bitrl_attention_cached(const bitrl_kv_cache_t* cache, int32_t layer, const void* q, int32_t T,
@@ -755,7 +759,7 @@ bool enc_cache_match(const bitrl_encoder_t* enc, const bitrl_kv_cache_t* cache) 
 
 size_t bitrl_encoder_cached_workspace_bytes(const bitrl_encoder_t* enc, const bitrl_kv_cache_t* cache, int32_t T,
                                             int32_t max_new_len) {
-  if (!enc || kv_check(cache) != BITRL_OK || !enc_cache_match(enc, cache) || T < 1 || max_new_len < 1) return 0;
+  if (!enc || kv_check(cache) != BITRL_OK || !enc_cache_match(enc, cache) || !kv_sizes_ok(cache, T, max_new_len, enc->n_heads)) return 0;
   return carve_enc_cached(nullptr, enc, cache, T, max_new_len).bytes;
 }
 
