@@ -434,8 +434,9 @@ BITRL_API bitrl_status bitrl_kv_advance(const bitrl_kv_cache_t* cache, const int
 
 /* The encoder over a cache: blocks as in bitrl_encoder_forward_states, with block l's attention by bitrl_kv_append and
  * bitrl_attention_cached on layer l.  The cache has at least as many layers as the encoder and its head counts.  pooled: NULL, or dev bf16
- * [n_seq, d], the last new token of every sequence (rows of sequences without new tokens are left as they are).
- * Rows of h_out behind the last sequence hold nothing of meaning.  workspace >= bitrl_encoder_cached_workspace_bytes(enc, cache, T,
+ * [n_seq, d], the last new token of every sequence that is not padding (rows of sequences without one, and of those that are
+ * skipped because their offsets or their tree are wrong, are left as they are).  Rows of h_out behind the last sequence and those
+ * of a skipped one hold nothing of meaning.  workspace >= bitrl_encoder_cached_workspace_bytes(enc, cache, T,
  * max_new_len), 0 for a cache and sizes that the call refuses.  used and seen are not advanced. */
 BITRL_API size_t bitrl_encoder_cached_workspace_bytes(const bitrl_encoder_t* enc, const bitrl_kv_cache_t* cache, int32_t T,
                                                       int32_t max_new_len);

@@ -721,12 +721,25 @@ bitrl_status launch_kv_move(const KvView& c, const int* moves, const int* count,
   return c.hd == 128 ? launch_kv_move_hd<128>(a, st) : launch_kv_move_hd<64>(a, st);
 }
 
-// out[s, :] = row of the last new token of sequence s; sequences without new tokens keep theirs.
+// out[s, :] = row of the last new token of sequence s that is one (a tree may end in padding); sequences without such a token, and
+// those whose tree is none, keep theirs.
 __global__ void kv_pool_last_kernel(const KvView c, const KvBatch b, const uint4* h, int d8, uint4* out) {
+  __shared__ int par[BITRL_TREE_MAX_TOKENS];
+  __shared__ int last_s;
   pdl_enter();
   KvSeq q;
-  if (!kv_seq(c, b, blockIdx.x, q) || q.m == 0) return;
-  const uint4* src = h + static_cast<long long>(q.t0 + q.m - 1) * d8;
+  if (!kv_seq(c, b, blockIdx.x, q)) return;
+  int last = q.m - 1;
+  if (b.parent) {
+    if (threadIdx.x == 0) last_s = -1;
+    if (!kv_load_tree(b, q, par, blockDim.x)) return;
+    for (int i = threadIdx.x; i < q.m; i += blockDim.x)
+      if (par[i] != BITRL_PARENT_PAD) atomicMax(&last_s, i);
+    __syncthreads();
+    last = last_s;
+  }
+  if (last < 0) return;
+  const uint4* src = h + static_cast<long long>(q.t0 + last) * d8;
   uint4* dst = out + static_cast<long long>(blockIdx.x) * d8;
   for (int i = threadIdx.x; i < d8; i += blockDim.x) dst[i] = src[i];
 }
