@@ -137,7 +137,7 @@ struct AtSmem {
   static constexpr uint32_t Q = 0, RING = 2 * TILE, BAR = RING + AT_RING * TILE;
   static constexpr uint32_t KV_FULL = BAR, KV_EMPTY = KV_FULL + 8 * AT_RING, Q_FULL = KV_EMPTY + 8 * AT_RING, Q_EMPTY = Q_FULL + 8,
                             S_FULL = Q_EMPTY + 8, P_FULL = S_FULL + 32, O_DONE = P_FULL + 32, V_READY = O_DONE + 32, DRAIN = V_READY + 8 * AT_RING;
-  static constexpr uint32_t MISC = DRAIN + 8;  // tensor-memory base, failed, odd[4]
+  static constexpr uint32_t MISC = DRAIN + 8;  // tensor-memory base, failed, odd
   static constexpr uint32_t RUN = MISC + 32, PART = RUN + 32;
   static constexpr uint32_t BYTES = PART + 8 * (AT_THREADS / 32 + 1) + 1024;  // + slack to align the base
   static_assert(AT_RING % 2 == 1 && BYTES <= 232448, "ring");
@@ -186,7 +186,7 @@ attn_tiles_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
   unsigned char* sm = at_smem_raw + (base - raw);
   volatile uint32_t* misc = reinterpret_cast<volatile uint32_t*>(sm + M::MISC);
   volatile uint32_t* failed = misc + 1;
-  volatile uint32_t* odd = misc + 4;
+  volatile uint32_t* odd = misc + 4;  // a value was made harmless
   const uint32_t failed_addr = base + M::MISC + 4;
   const AcArgs& a = t.a;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -198,7 +198,7 @@ attn_tiles_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
 
   if (threadIdx.x == 0) {
     *failed = 0u;
-    for (int i = 0; i < 4; ++i) odd[i] = 0u;
+    *odd = 0u;
     for (int i = 0; i < AT_RING; ++i) {
       ptx::mbar_init(base + M::KV_FULL + 8 * i, 1);
       ptx::mbar_init(base + M::KV_EMPTY + 8 * i, 2);
@@ -368,7 +368,7 @@ attn_tiles_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
     if (!ok && lane == 0) give_up(AT_WAIT_MMA);
   } else {
     // ------------------------------------------------------------------ values of masked units
-    uint32_t e = 1, item = 0;
+    uint32_t e = 1;
     bool ok = true;
     while (ok && more) {
       const int end = q.used + q.m;
@@ -427,13 +427,12 @@ attn_tiles_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
                 if (touch) ptx::sts128(addr, make_uint4(x[0], x[1], x[2], x[3]));
                 found |= touch;
               }
-          if (__any_sync(0xffffffffu, found) && lane == 0) odd[item & 3] = item + 1;
+          if (__any_sync(0xffffffffu, found) && lane == 0) *odd = 1u;  // for good: this warp runs ahead of the softmax by as many items as the ring allows
           ptx::fence_proxy_async_smem();
         }
         __syncwarp();
         if (lane == 0) ptx::mbar_arrive(base + M::V_READY + 8 * slot);
       }
-      ++item;
       if (ok) more = w.next(cost);
       __syncwarp();
     }
@@ -446,7 +445,7 @@ attn_tiles_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
     const int r = (warp & 3) * 32 + lane, r_tok = r / a.rep, r_head = r - r_tok * a.rep;
     const uint32_t s_addr = tmem + 128 * x + lane_base, o_addr = tmem + 256 + 128 * x + lane_base;
     const bool wide = (reinterpret_cast<uintptr_t>(a.att) & 31u) == 0;  // att is 16-byte aligned at least
-    uint32_t s_par = 0, o_par = 0, item = 0;  // phases, as bits: of either score buffer, of the products from either buffer
+    uint32_t s_par = 0, o_par = 0;  // phases, as bits: of either score buffer, of the products from either buffer
     const uint64_t scale_x2 = ptx::pack_f32x2(__float_as_uint(a.scale2), __float_as_uint(a.scale2));
     bool ok = true;
     while (ok && more) {
@@ -529,7 +528,7 @@ attn_tiles_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
         if (!__any_sync(0xffffffffu, wait(M::O_DONE + 8 * (2 * x + lb), ((o_par >> lb) & 1) ^ 1))) { ok = false; break; }
         ptx::tc_fence_after_sync();
         const bool whole = w.u0 == 0 && w.u1 == w.units;
-        const bool fix = odd[item & 3] == item + 1;
+        const bool fix = *odd != 0u;  // perhaps of another item: then there is nothing to give back below
         const bool pad = a.b.parent && exists && a.b.parent[q.t0 + tok] == BITRL_PARENT_PAD;
         const bool none = l == 0.0f || pad;
         const float inv = !whole ? 1.0f : none ? 0.0f : __fdiv_rn(1.0f, l);
@@ -585,7 +584,6 @@ attn_tiles_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
         if (!whole && threadIdx.x == 128) cuts[w.u0 == 0 ? 1 : 0] = AtCut{w.s, w.x, w.h, w.u1 == w.units};
         ptx::tc_fence_before_sync();
       }
-      ++item;
       more = w.next(cost);
       __syncwarp();
     }

@@ -109,3 +109,33 @@ def test_infinite_values_reach_those_who_see_them(B, nh, nkv, hd, page, used, ne
     rest = ~(up | down)
     assert ((att - want).abs()[rest] <= tol[rest]).all()
     assert torch.equal(got.mass, plain.mass)
+
+
+@pytest.mark.parametrize("hd,page", [(64, 16), (128, 64)])
+def test_infinities_among_many_short_items(B, hd, page):
+    """Sequences of one and of two row tiles in turn, a few with values that some of their drafted tokens must not see."""
+    nh, nkv, n_seq = 8, 2, 320
+    news = [[40, 9, 12, 7, 20][s % 5] for s in range(n_seq)]
+    used = [(37 * s) % 150 for s in range(n_seq)]
+    c = ref.make(241, used, news, nkv, hd, page, scale=0.25)
+    trees = [[ref.PAST, ref.PAST] + [0] * (m - 2) for m in news]  # token 1 is seen by itself alone
+    par = torch.tensor([p for t in trees for p in t], dtype=torch.int32)
+    q = fill_new(c, 242, news, par, nh, scale=0.25)
+    off = ref.offsets(news)
+    want, tol = exact(c, q, off, nh, par)
+    odd = [s for s in range(n_seq) if s % 7 in (0, 3)]
+    for s in odd:
+        pg, at = ref.at(c, s, [used[s] + 1])
+        c["v"][0, pg, :, at] = math.inf
+        pg, at = ref.at(c, s, [used[s]])  # token 0 is seen by all but token 1
+        c["v"][0, pg, 0, at, 5] = -math.inf
+    att = B.attention_cached(on_gpu(B, c), 0, q.cuda(), (off.cuda(), max(news)), nh, parent=par.cuda()).cpu().double().reshape(want.shape)
+    B.poll_status()
+    for s in odd:
+        t0, m, rep = int(off[s]), news[s], nh // nkv
+        want[t0 + 1] = math.inf
+        rows = [t0] + list(range(t0 + 2, t0 + m))
+        want[rows, :rep, 5] = -math.inf
+    bad = want.isinf()
+    assert torch.equal(att[bad], want[bad])
+    assert ((att - want).abs()[~bad] <= tol[~bad]).all()
