@@ -695,7 +695,7 @@ bitrl_status bitrl_kv_evict_plan(const bitrl_kv_cache_t* cache, int32_t budget, 
                                  int32_t max_moves, int32_t* moves, int32_t* count, void* stream) {
   bitrl_status s = kv_check(cache);
   if (s != BITRL_OK) return s;
-  if (!cache->mass || !moves || !count) return BITRL_ERR_NULL;
+  if (!cache->mass || (!moves && max_moves > 0) || !count) return BITRL_ERR_NULL;  // a budget of all slots needs no list
   if (budget < 1 || recent < 0 || sink < 0 || max_moves < 0) return BITRL_ERR_SHAPE;
   const int room = cache->max_pages * cache->page_tokens;
   if (budget < room && max_moves < (budget < room - budget ? budget : room - budget)) return BITRL_ERR_SHAPE;

@@ -49,3 +49,26 @@ def test_an_encoder_whose_group_is_too_large(group):
     assert e.value.status == bitrl.ERR_LIMIT
     assert ctypes.c_size_t(enc.workspace_bytes(2)).value > 0
     bitrl.poll_status()
+
+
+def test_a_budget_of_all_slots_needs_no_list(L):  # noqa: F811
+    """max_moves >= min(budget, slots - budget) is 0 or less then, and an empty tensor has no address."""
+    P = 1 << 20
+    if not torch.cuda.is_available():  # past the arguments' checks, the next one is the device's
+        for budget in (64, 1000):
+            assert L.bitrl_kv_evict_plan(desc(), budget, 4, 0, 0, None, P, None) not in (bitrl.OK, bitrl.ERR_NULL, bitrl.ERR_SHAPE)
+    assert L.bitrl_kv_evict_plan(desc(), 63, 4, 0, 0, None, P, None) == bitrl.ERR_SHAPE
+    assert L.bitrl_kv_evict_plan(desc(), 63, 4, 0, 1, None, P, None) == bitrl.ERR_NULL
+    assert L.bitrl_kv_evict_plan(desc(), 64, 4, 0, 0, None, None, None) == bitrl.ERR_NULL
+
+
+@pytest.mark.gpu
+def test_a_plan_without_moves():
+    cache = bitrl.KVCache.empty(2, 3, 64, 2, 64, page_tokens=16)
+    cache.used.copy_(torch.tensor([64, 0, 10], dtype=torch.int32))
+    moves = torch.empty(2, 3, 2, 0, 2, dtype=torch.int32, device="cuda")
+    count = torch.full((2, 3, 2), 7, dtype=torch.int32, device="cuda")
+    bitrl.kv_evict_plan(cache, 64, 4, moves=moves, count=count)
+    bitrl.kv_move(cache, moves, count)
+    bitrl.poll_status()
+    assert not count.any()
