@@ -201,7 +201,7 @@ attn_tiles_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
     *odd = 0u;
     for (int i = 0; i < AT_RING; ++i) {
       ptx::mbar_init(base + M::KV_FULL + 8 * i, 1);
-      ptx::mbar_init(base + M::KV_EMPTY + 8 * i, 2);
+      ptx::mbar_init(base + M::KV_EMPTY + 8 * i, 3);  // either issuer, and the warp that looks the values over
       ptx::mbar_init(base + M::V_READY + 8 * i, 1);
     }
     ptx::mbar_init(base + M::Q_FULL, 1);
@@ -374,12 +374,12 @@ attn_tiles_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
       const int end = q.used + q.m;
       for (int u = w.u0; u < w.u1; ++u, e += 2) {
         const uint32_t slot = e % AT_RING;
-        // the keys' tile too: a place's barrier must be followed through every round, or a later one looks like this one
-        if (!__any_sync(0xffffffffu, wait(M::KV_FULL + 8 * ((e - 1) % AT_RING), ((e - 1) / AT_RING) & 1)) ||
-            !__any_sync(0xffffffffu, wait(M::KV_FULL + 8 * slot, (e / AT_RING) & 1))) {
-          ok = false;
-          break;
-        }
+        // The keys' tile too: a place's barrier must be followed through every round, or a later one looks like this one.  And
+        // the place goes on to the next round with this warp's leave alone: without it, this warp could come too late for a
+        // round (one launch in 700 did), wait for the one after it, and nobody would say that its values are ready.
+        if (!(ok = __any_sync(0xffffffffu, wait(M::KV_FULL + 8 * ((e - 1) % AT_RING), ((e - 1) / AT_RING) & 1)))) break;
+        if (lane == 0) ptx::mbar_arrive(base + M::KV_EMPTY + 8 * ((e - 1) % AT_RING));
+        if (!(ok = __any_sync(0xffffffffu, wait(M::KV_FULL + 8 * slot, (e / AT_RING) & 1)))) break;
         if (masked(u)) {
           // from the first slot that some row does not see; a lane takes 16 bytes of a row, four rows side by side (the swizzle
           // moves pieces inside a row, which does not matter here)
@@ -431,7 +431,10 @@ attn_tiles_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
           ptx::fence_proxy_async_smem();
         }
         __syncwarp();
-        if (lane == 0) ptx::mbar_arrive(base + M::V_READY + 8 * slot);
+        if (lane == 0) {
+          ptx::mbar_arrive(base + M::V_READY + 8 * slot);
+          ptx::mbar_arrive(base + M::KV_EMPTY + 8 * slot);
+        }
       }
       if (ok) more = w.next(cost);
       __syncwarp();
