@@ -481,15 +481,17 @@ attn_tiles_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
             for (int j = 0; j < 32; j += 2)
               mx[(j >> 1) & 3] = fmaxf(mx[(j >> 1) & 3], fmaxf(__uint_as_float(s[c][j]), __uint_as_float(s[c][j + 1])));
           const float m2 = __fmul_rn(fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])), a.scale2);
+          // every row goes by its own scores: which steps the warp walks through here does not change the others' bits (a tile
+          // may hold rows of nobody, whatever shared memory held)
+          const bool grown = m2 > m_ref + AT_GROWTH;
           if (i == 0) {
             m_ref = m2;
-          } else if (__any_sync(0xffffffffu, m2 > m_ref + AT_GROWTH)) {
+          } else if (__any_sync(0xffffffffu, grown && exists)) {
             // the product of the step before (the one before that is done: this step's scores came after it)
             if (!__any_sync(0xffffffffu, wait(M::O_DONE + 8 * (2 * x + (b ^ 1)), ((o_par >> (b ^ 1)) & 1) ^ 1))) { ok = false; break; }
             ptx::tc_fence_after_sync();
-            const float m_new = fmaxf(m_ref, m2);
-            const float f = m_new == m_ref ? 1.0f : ac_exp2(m_ref - m_new);
-            m_ref = m_new;
+            const float f = grown ? ac_exp2(m_ref - m2) : 1.0f;
+            if (grown) m_ref = m2;
             l = __fmul_rn(l, f);
 #pragma unroll 1
             for (int c = 0; c < HD / 32; ++c) {
