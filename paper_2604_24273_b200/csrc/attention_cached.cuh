@@ -392,61 +392,69 @@ attn_few_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constan
 #pragma unroll
             for (int e = 0; e < 4; ++e) o[n][d][e] = __fmul_rn(o[n][d][e], alpha[n][e & 1]);
       }
-      // A value that is not finite in a slot that some row does not see (or behind the last slot) must not reach that row
-      // as 0 * inf: such a unit goes through scalar sums over the seen slots.
+      // A value that is not finite in a slot that some row does not see (or behind the last slot) must not reach that row as
+      // 0 * inf: from the first new token's slot on such values become zero, and the rows that see them get them back below.
       bool odd = false;
       if (masked) {
 #pragma unroll
         for (int i = 0; i < static_cast<int>(TILE / 512); ++i) {
-          const uint4 x = ptx::lds128(vs_addr + (lane + 32 * i) * 16);
-          const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+          const uint32_t at = vs_addr + (lane + 32 * i) * 16;
+          const uint4 x = ptx::lds128(at);
+          uint32_t w[4] = {x.x, x.y, x.z, x.w};
+          bool hit = false;
 #pragma unroll
-          for (int j = 0; j < 4; ++j) odd |= (w[j] & 0x7f80u) == 0x7f80u || (w[j] & 0x7f800000u) == 0x7f800000u;
+          for (int j = 0; j < 4; ++j) {
+            const bool lo = (w[j] & 0x7f80u) == 0x7f80u, hi = (w[j] & 0x7f800000u) == 0x7f800000u;
+            hit |= lo || hi;
+            w[j] &= (lo ? 0xffff0000u : 0xffffffffu) & (hi ? 0x0000ffffu : 0xffffffffu);
+          }
+          if (hit && slot0 + (((lane + 32 * i) & 127) >> 3) >= q.used) {
+            ptx::sts128(at, make_uint4(w[0], w[1], w[2], w[3]));
+            odd = true;
+          }
         }
         odd = __any_sync(0xffffffffu, odd);
+        if (odd) ptx::fence_proxy_async_smem();  // the next copy into this place comes after these writes
+        __syncwarp();
       }
-      if (!odd) {
-        uint32_t ph[NG][2], pl[NG][2];  // B operand: row g, slots 2 t and the next (and + 8): blocks of 8 x 8 transposed
+      uint32_t ph[NG][2], pl[NG][2];  // B operand: row g, slots 2 t and the next (and + 8): blocks of 8 x 8 transposed
 #pragma unroll
-        for (int n = 0; n < NG; ++n)
+      for (int n = 0; n < NG; ++n)
 #pragma unroll
-          for (int i = 0; i < 2; ++i) {
-            uint32_t hi, lo;
-            ac_split(c[n][2 * i], c[n][2 * i + 1], hi, lo);
-            ph[n][i] = movmatrix_trans(hi);
-            pl[n][i] = movmatrix_trans(lo);
-          }
-#pragma unroll
-        for (int d = 0; d < MD; ++d) {
-          const int key = 8 * (lm >> 1) + lr, ch = 2 * d + (lm & 1);
-          uint32_t va[4];
-          ldmatrix_x4_trans(vs_addr + (ch >> 3) * HALF + key * 128 + (((ch ^ key) & 7) << 4), va);
-#pragma unroll
-          for (int n = 0; n < NG; ++n) mma_bf16(o[n][d], va, ph[n][0], ph[n][1]);
-#pragma unroll
-          for (int n = 0; n < NG; ++n) mma_bf16(o[n][d], va, pl[n][0], pl[n][1]);
+        for (int i = 0; i < 2; ++i) {
+          uint32_t hi, lo;
+          ac_split(c[n][2 * i], c[n][2 * i + 1], hi, lo);
+          ph[n][i] = movmatrix_trans(hi);
+          pl[n][i] = movmatrix_trans(lo);
         }
-      } else {
-        for (int key = 0; key < AF_SLOTS; ++key) {
-          const int from = 4 * (key & 7) + t, slot = slot0 + key;  // the lane that holds this slot's weights of the lane's rows
+#pragma unroll
+      for (int d = 0; d < MD; ++d) {
+        const int key = 8 * (lm >> 1) + lr, ch = 2 * d + (lm & 1);
+        uint32_t va[4];
+        ldmatrix_x4_trans(vs_addr + (ch >> 3) * HALF + key * 128 + (((ch ^ key) & 7) << 4), va);
+#pragma unroll
+        for (int n = 0; n < NG; ++n) mma_bf16(o[n][d], va, ph[n][0], ph[n][1]);
+#pragma unroll
+        for (int n = 0; n < NG; ++n) mma_bf16(o[n][d], va, pl[n][0], pl[n][1]);
+      }
+      const int pool_row = odd ? static_cast<int>(ptx::lds32(rows_at + 4 * stage)) : none_row;
+      if (pool_row < none_row) {  // rare
+        const unsigned short* v = a.c.v + static_cast<long long>(pool_row) * HD;
+#pragma unroll 1
+        for (int key = max(q.used - slot0, 0); key < min(end - slot0, AF_SLOTS); ++key)
 #pragma unroll
           for (int n = 0; n < NG; ++n)
 #pragma unroll
-            for (int e = 0; e < 2; ++e) {
-              const float lo = __shfl_sync(0xffffffffu, c[n][e], from), hi = __shfl_sync(0xffffffffu, c[n][2 + e], from);
-              const float p = key < 8 ? lo : hi;
-              const bool see = slot < end && (slot < q.used || ac_sees_new(anc, tok[n][e], slot - q.used));
+            for (int e = 0; e < 2; ++e)
+              if (ac_sees_new(anc, tok[n][e], slot0 + key - q.used)) {
 #pragma unroll
-              for (int d = 0; d < MD; ++d)
+                for (int d = 0; d < MD; ++d)
 #pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                  const int dim = 16 * d + 8 * i + g;
-                  unsigned short v;
-                  asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(vs_addr + (dim >> 6) * HALF + key * 128 + ((((dim >> 3) ^ key) & 7) << 4) + 2 * (dim & 7)));
-                  if (see) o[n][d][2 * i + e] = fmaf(p, bf16_bits_to_float(v), o[n][d][2 * i + e]);
-                }
-            }
-        }
+                  for (int i = 0; i < 2; ++i) {
+                    const unsigned short b = v[key * HD + 16 * d + 8 * i + g];
+                    if ((b & 0x7f80u) == 0x7f80u) o[n][d][2 * i + e] += bf16_bits_to_float(b);
+                  }
+              }
       }
       __syncwarp();
       load(stage);  // the unit AF_STAGES ahead takes this one's place
