@@ -399,8 +399,13 @@ BITRL_API bitrl_status bitrl_kv_append(const bitrl_kv_cache_t* cache, int32_t la
  * as two bf16 halves (16 significant bits); a value that is not finite reaches every row that sees its slot, as in fp32 products
  * and sums (an infinity of one sign stays one).  The same call gives the same bits: every sum has a fixed order.
  * workspace: dev, >= bitrl_attention_cached_workspace_bytes(cache, T, max_new_len, n_heads), 0 for a cache and sizes that the call
- * refuses.  Nothing in it outlives the call; calls that can run at the same time (other streams, graphs replayed side by
- * side) need one each.  accumulate_mass with sequences that share pages is not allowed: both would add to the same slots. */
+ * refuses.  With at most 16 rows (max_new_len * n_heads / n_kv_heads) and a cache with mass it holds the scores too, 16 to 64 bytes for
+ * every row of a layer's pool (n_pages * n_kv_heads * page_tokens).  Nothing in it outlives the call; calls that can run at the same
+ * time (other streams, graphs replayed side by side) need one each.
+ * accumulate_mass with sequences that share pages is not allowed: both would add to the same slots.  A tree's tokens all add their
+ * weights, also those that are rejected afterwards, and nothing takes them back: a caller whose evictions should go by the tokens that
+ * were kept passes accumulate_mass 0 for the draft, and attends the accepted tokens again, with weights, between bitrl_kv_move and
+ * bitrl_kv_advance. */
 BITRL_API size_t bitrl_attention_cached_workspace_bytes(const bitrl_kv_cache_t* cache, int32_t T, int32_t max_new_len,
                                                         int32_t n_heads);
 BITRL_API bitrl_status bitrl_attention_cached(const bitrl_kv_cache_t* cache, int32_t layer, const void* q, int32_t T,
@@ -428,7 +433,8 @@ BITRL_API bitrl_status bitrl_kv_move(const bitrl_kv_cache_t* cache, const int32_
 
 /* After all layers of a step: n = new tokens of s (state_off, max_new_len as above), or n_keep[s] of them where n_keep
  * (dev int32 [n_seq]) is given; used[s] = min(used[s] + n, budget) (budget 0: no limit), seen[s] += n.  With state_off NULL and
- * max_new_len 0 it applies the budget alone, as after bitrl_kv_evict_plan and bitrl_kv_move. */
+ * max_new_len 0 it applies the budget alone, as after bitrl_kv_evict_plan and bitrl_kv_move.  After a tree n_keep leaves out the
+ * places that bitrl_kv_move did not bring to the front: the rejected tokens, and padding, whose slots nothing was written to. */
 BITRL_API bitrl_status bitrl_kv_advance(const bitrl_kv_cache_t* cache, const int32_t* state_off, int32_t max_new_len,
                                         const int32_t* n_keep, int32_t budget, void* stream);
 

@@ -121,12 +121,12 @@ __device__ __forceinline__ bool ac_is_pad(const uint32_t* anc, int tok) { return
 // warp of the grid takes an equal run of it, whatever the lengths are.  A warp needs nothing from the others: it brings its
 // units in by TMA through a ring of its own, keeps a running maximum, sum and 16 x HD result, and leaves one result per
 // (sequence, head) that it met.  Results of items that lie within one run are final; the others are joined by
-// attn_few_join_kernel, which also turns the scores that this kernel leaves behind (fp32, 4 to 64 bytes per slot beside
+// attn_few_join_kernel, which also turns the scores that this kernel leaves behind (fp32, 16 to 64 bytes per slot beside
 // the 4 HD bytes of its key and value) into the weight of every slot, so that keys are read once.
 // Scores come from mma.sync (eight rows fill its N; a tcgen05 tile has 128 rows).  The weights are split into two bf16
 // halves (16 significant bits), which costs nothing where reading bounds the kernel.
 // 128 sequences of up to 4096 slots, one token each, 20 heads over 5: 115 us for 633 MB, 5.5 TB/s (the join: 14 us); one
-// sequence of 100k slots: 49 + 14 us; of 2000: 12.5 us together, a chain of two launches and their loads.
+// sequence of 100k slots: 49 + 14 us; of 2000: 12.6 us together, a chain of two launches and their loads.
 constexpr int AF_WARPS = 4;
 constexpr int AF_CTAS = 2;  // per SM
 constexpr int AF_THREADS = 32 * AF_WARPS;

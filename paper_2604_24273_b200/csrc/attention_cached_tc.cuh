@@ -119,11 +119,11 @@ struct AcWalk {
 //               followed only when it has grown by more than 2^8 (weights stay below 2^8, statistics and sums are fp32), so
 //               the result is rescaled rarely.  Weights enter the product as two bf16 halves (ac_split), side by side in
 //               the 64 columns that their scores leave; their sum is taken before.  (One bf16 each, half the value products,
-//               added as much error as the rounding of the result: a chunk took 489 us with its weights pass in place of 564.)
-// Bound: 1024 cycles of exponentials and as many of products per 128 x 128 tile for long chunks (scores take 3/4 of the rate
+//               added as much error as the rounding of the result: a chunk took 489 us with its weights pass in place of 561.)
+// Bound: 1536 cycles of products and 1024 of exponentials per 128 x 128 tile for long chunks (scores take 3/4 of the rate
 // with 64 columns, as both operands come from shared memory); the reading of keys and values for few rows.
-// A chunk of 4096 tokens over 4100 slots (20 heads over 5 of 128): 235 us, 1.1 PFLOP/s, tensor pipe and exponentials busy for 56 %
-// of the cycles each; 64 states of 15 .. 40 tokens over 200 .. 2000 slots: 62 us; 16 trees of 48 over 1000 .. 8000: 59 us.
+// A chunk of 4096 tokens over 4100 slots (20 heads over 5 of 128): 298 us with the join behind it, tensor pipe busy for 69 % of the
+// cycles, exponentials for 46 %; 64 states of 15 .. 40 tokens over 200 .. 2000 slots: 74 us; 16 trees of 48 over 1000 .. 8000: 77 us.
 // Every wait is bounded; on expiry the CTA records a status word and leaves normally.
 constexpr int AT_THREADS = 384;
 constexpr int AT_KEYS = 128;
@@ -1408,7 +1408,7 @@ inline AcPlan ac_plan(const KvView& c, int T, int max_new, int n_heads) {
     p.rows_cap = static_cast<int>(rows);
     p.score_rows = rows <= 4 ? 4 : rows <= 8 ? 8 : 16;
     // one run per resident warp: with two to four times as many, parts and their joining cost more than the evener end gives
-    // (100k slots of one sequence: 66 us against 82 .. 117; 128 sequences of up to 4096: 133 against 137 .. 139)
+    // (when tried, 100k slots of one sequence: 66 us against 82 .. 117; 128 sequences of up to 4096: 133 against 137 .. 139)
     p.runs = sm_count() * AF_WARPS * AF_CTAS;
     // slots of a CTA of the join: long stretches, unless they would leave SMs idle (2000 slots of one sequence: 13.3 us in
     // stretches of 2048, 9 us in stretches of 512, less in shorter ones; 128 sequences: no difference)
