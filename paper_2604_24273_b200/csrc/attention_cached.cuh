@@ -65,8 +65,8 @@ __device__ __forceinline__ uint32_t pack_bf16x2(float x0, float x1) {
 }
 // Weights p0, p1 >= 0 as two bf16 halves each, p = hi + lo (p0 in the low half of a word): 16 significant bits, where one bf16 would
 // move a result of few keys by up to 2^-8 of their magnitudes, as much as its own rounding.  hi is cut, not rounded, and 2^-20 of p
-// keeps lo above zero wherever p is (down to 2^-113): hi and lo then have one sign, and the two products with a value that is infinite
-// are the same infinity.
+// keeps lo above zero wherever p is (down to 2^-100 and less): hi and lo then have one sign, and the two products with a value that is
+// infinite are the same infinity.
 __device__ __forceinline__ void ac_split(float p0, float p1, uint32_t& hi, uint32_t& lo) {
   const uint32_t b0 = __float_as_uint(p0), b1 = __float_as_uint(p1);
   hi = __byte_perm(b0, b1, 0x7632);

@@ -70,3 +70,31 @@ def test_the_same_number_of_tokens_everywhere(B, nh, nkv, hd, page, m, is_tree):
     B.poll_status()
     for x, y in zip(*outs):
         assert same(x, y)
+
+
+@pytest.mark.parametrize("nh,nkv,hd,page,news", [(4, 2, 64, 16, [2, 1, 0]), (8, 2, 128, 64, [30, 3, 41]), (8, 1, 128, 128, [150, 40, 300])])
+def test_a_page_table_with_room_for_half_a_million_slots(B, nh, nkv, hd, page, news):
+    """As many entries as a page table may have, of which few name a page: the others are never read as pages."""
+    used = [70, 5, 400]
+    c = ref.make(521, used, news, nkv, hd, page)
+    wide = torch.full((3, B.KV_MAX_SLOTS // page), -1, dtype=torch.int32)
+    wide[:, : c["page_table"].shape[1]] = c["page_table"]
+    for s in range(3):
+        wide[s, -(-(used[s] + news[s]) // page) :] = -1
+    c["page_table"] = wide
+    q = fill_new(c, 522, news, None, nh)
+    check_attend(B, c, q, news, nh, None)
+    g = on_gpu(B, c)
+    off = ref.offsets(news)
+    B.kv_append(g, 0, torch.randn(int(off[-1]), (nh + 2 * nkv) * hd, generator=ref.gen(523)).to(torch.bfloat16).cuda(), (off.cuda(), max(news)), nh)
+    B.kv_advance(g, (off.cuda(), max(news)))
+    now = {n: getattr(g, n).cpu() for n in ("k", "v", "mass", "pos", "page_table", "used", "seen")}
+    moves, count = B.kv_evict_plan(g, 64, 20, sink=2)
+    B.kv_move(g, moves, count)
+    B.poll_status()
+    want = ref.plan(now, 64, 20, 2)
+    new = ref.move(now, want)
+    for (layer, s, h), lst in want.items():
+        assert int(count[layer, s, h]) == len(lst)
+    for name in ("k", "v", "mass", "pos"):
+        assert same(getattr(g, name).cpu(), new[name]), name
