@@ -277,11 +277,17 @@ template <class E>
 __device__ __forceinline__ float tl_x(const TlRows<E>& a, float v, float ref) {
   return tl_fused(a, ref) ? __fmaf_rn(v, a.c, -__fmul_rn(ref, a.c)) : __fmul_rn(v - ref, a.c);
 }
-// From sums relative to `ref` to sums relative to `to` >= ref.
+// R - c ref, exactly: what sums relative to R lack of being relative to c ref.  0 where they subtract first.
+template <class E>
+__device__ __forceinline__ float tl_rounding(const TlRows<E>& a, float ref) {
+  return tl_fused(a, ref) ? __fmaf_rn(-ref, a.c, __fmul_rn(ref, a.c)) : 0.0f;
+}
+// From sums relative to `ref` to sums relative to `to` >= ref.  R's rounding (up to a half at |R| = 2^24) is part of the step, as another
+// reference has another, or none.
 template <bool ENT, class E>
 __device__ __forceinline__ void tl_rebase(const TlRows<E>& a, TlAcc& s, float to) {
   if (s.ref == to) return;
-  const float sh = fmaxf(tl_fused(a, s.ref) && tl_fused(a, to) ? __fmul_rn(s.ref, a.c) - __fmul_rn(to, a.c) : (s.ref - to) * a.c, TL_FAR);
+  const float sh = fmaxf(__fmaf_rn(s.ref - to, a.c, tl_rounding(a, s.ref) - tl_rounding(a, to)), TL_FAR);
   const float f = tl_exp2(sh);
   s.W = f * (ENT ? __fmaf_rn(s.S, sh, s.W) : s.W);
   s.S *= f;
