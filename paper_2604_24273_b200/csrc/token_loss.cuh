@@ -33,7 +33,7 @@ constexpr int TL_MAX_CLUSTER = 16;
 constexpr int TL_MAX_SMEM = 220 * 1024;
 constexpr int TL_CANDIDATES = 2560;   // of a share for the top alternatives: all elements of a row that has a vector for fewer than 128 threads, and some
 constexpr int TL_SEGMENTS = 1024;     // of which single elements are looked at
-constexpr float TL_FAR = -1e30f;      // an exponent that leaves nothing, but is finite
+constexpr float TL_FAR = -1024.0f;    // an exponent that leaves nothing, and whose product with a gradient's factor stays finite
 constexpr float TL_REST_ROUNDING = 0x1p-20f;  // what rounding its log probabilities may leave of a teacher's mass outside its tokens
 constexpr double TL_LOG2E = 1.4426950408889634074, TL_LN2 = 0.69314718055994530942;
 
@@ -125,15 +125,15 @@ __device__ __forceinline__ float2 tl_pair(const uint32_t* w, int i, const __nv_b
 __device__ __forceinline__ float2 tl_pair(const uint32_t* w, int i, const __half*) {
   return __half22float2(*reinterpret_cast<const __half2*>(w + i));
 }
-// The same with -inf raised to a number (NaN stays), where 0 * x must not be 0 * -inf.  Beside any maximum between ref_lo and ref_hi the
-// exponential of that number is 0, and no product with its x overflows.
+// The same with -inf raised to a number (NaN stays), where 0 * x must not be 0 * -inf.  Beside any maximum between ref_lo and ref_hi (at most
+// 2^24 2^20 ln 2 from 0) the exponential of that number is 0; it is no further away than that needs, so that products of a gradient's factor with its x stay finite.
 __device__ __forceinline__ float2 tl_pair_raised(const uint32_t* w, int i, const float* e) {
   const float2 f = tl_pair(w, i, e);
-  return make_float2(tl_max_nan(f.x, -0x1p60f), tl_max_nan(f.y, -0x1p60f));
+  return make_float2(tl_max_nan(f.x, -0x1p46f), tl_max_nan(f.y, -0x1p46f));
 }
 __device__ __forceinline__ float2 tl_pair_raised(const uint32_t* w, int i, const __nv_bfloat16* e) {
   uint32_t r;
-  asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(w[i]), "r"(0xdd80dd80u));  // -2^60
+  asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(w[i]), "r"(0xd680d680u));  // -2^46
   return tl_pair(&r, 0, e);
 }
 __device__ __forceinline__ float2 tl_pair_raised(const uint32_t* w, int i, const __half* e) {
@@ -1420,7 +1420,7 @@ bitrl_status tl_dispatch(int32_t dtype, F&& f) {
 }
 
 // The rows of a call.  Maxima may use x = z c - R as long as R is off by no more than 1 (|R| <= 2^24), so that the largest x is near 0.  That is
-// also far above -2^60 (fp16: -65504, for maxima from -16384 on at temperatures up to 256), which a -inf counts as where a number is needed.
+// also far above -2^46 (fp16: -65504, for maxima from -16384 on at temperatures up to 256), which a -inf counts as where a number is needed.
 template <class E>
 TlRows<E> tl_rows(const void* z, int T, int V, long long ld, double temperature) {
   TlRows<E> a;

@@ -77,3 +77,23 @@ def test_half_precision_rows_across_their_lower_limit(B, V, tau):
     for tail in (False, True):
         ids, values = teacher(torch.zeros(6, V), 6, tail, 1.0, 4, few=False)
         check_distill(B, z, ids, values, tail, tau)
+
+
+@pytest.mark.parametrize("top,dent", [(20.0, 1e5), (5.0, 1e11)])
+@pytest.mark.parametrize("V", [60, 9000])
+def test_large_entropy_terms_leave_masked_tokens_without_gradient(B, V, top, dent):
+    """At the lowest temperature, with maxima beyond the limit (11.1) and below it: the gradient of a token that is left out is 0, however large the
+    entropy's part."""
+    tau = 2.0 ** -20
+    z = top + tc.logits(4, V, F32, V)[0] * 1e-6
+    z[:, 1::3] = -INF
+    z[3, 4:] = -INF
+    G, E = np.array([1.0, 0.0, -1.0, 1.0]), dent * np.array([1.0, -1.0, 0.5, 1.0])
+    got, _ = check_policy(B, z, np.array([0, 2, 3, 0]), tau, G, E)
+    assert not got[:, 1::3].any()
+    r = tc.Rows(tc.f64(z), tau)
+    tokens = np.array([0, 2, 3, 0], np.int32)
+    old, one = torch.tensor(r.lp[np.arange(4), tokens], dtype=F32).cuda(), torch.ones(4, device="cuda")
+    ppo = B.ppo_token_loss(z.cuda(), torch.from_numpy(tokens).cuda(), old, one, beta=dent, temperature=tau)["dlogits"]
+    B.poll_status()
+    assert torch.isfinite(ppo).all() and not ppo[:, 1::3].any()
