@@ -307,8 +307,9 @@ BITRL_API bitrl_status bitrl_ppo_token_loss(const void* logits, int32_t dtype, i
  *           tokens, p_r the student's:  loss as above + q_r (log q_r - log p_r)
  * An entry of value -inf has q = 0; terms with q = 0 are 0.  Rows without an entry (with tail 0: without one above -inf) are
  * padded: loss 0, gradient zeros.  An id >= V is left out, and the next bitrl_poll_status returns BITRL_ERR_SHAPE.  A row that
- * leaves out what the teacher names has a loss of +inf; where it leaves out all other tokens (p_r = 0), a q_r of at most 2^-20 counts as 0,
- * as the rounding of the values may leave it.
+ * leaves out what the teacher names has a loss of +inf.  Where p_r is below what 64 bits hold (2^-1074, 745 nats), a q_r of at most 2^-20 counts as
+ * 0, as the rounding of the values may leave it; with a greater one log p_r is still a number, unless the row leaves out all other tokens or has them at
+ * the lowest value of its type (a mask): then the loss is +inf, and the other tokens' gradient 0.
  * loss: dev fp32 [T] (required).  dlogits: NULL, or the gradient of sum_t weight_t loss_t,
  *   dz_j = weight ((sum q + q_r) p_j - sum_{id_k = j} q_k - [j not among the ids] q_r p_j / p_r) / temperature
  * weight: dev fp32 [T] or NULL (ones); the gradient of a row of weight 0 is zeros. */

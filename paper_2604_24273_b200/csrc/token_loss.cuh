@@ -20,6 +20,8 @@
 
 #include <cuda_fp16.h>
 
+#include <cfloat>
+
 #include "common.cuh"
 #include "ptx.cuh"
 
@@ -62,7 +64,7 @@ __device__ __forceinline__ void tl_set(float* p, float v) { *p = v; }
 __device__ __forceinline__ void tl_set(__nv_bfloat16* p, float v) { *p = __float2bfloat16_rn(v); }
 __device__ __forceinline__ void tl_set(__half* p, float v) { *p = __float2half_rn(v); }
 
-// What differs by type: elements in a 32-bit word, -inf in all of them, conversions.
+// What differs by type: elements in a 32-bit word, -inf in all of them, the lowest number, conversions.
 template <class E>
 struct TlType;
 template <>
@@ -70,18 +72,21 @@ struct TlType<float> {
   static constexpr int LOW_BITS = 0;  // of fp32 that the type does not have
   static constexpr int PER_WORD = 1;
   static constexpr uint32_t NEG_INF = 0xff800000u;
+  static constexpr float LOWEST = -FLT_MAX;
 };
 template <>
 struct TlType<__nv_bfloat16> {
   static constexpr int LOW_BITS = 16;
   static constexpr int PER_WORD = 2;
   static constexpr uint32_t NEG_INF = 0xff80ff80u;
+  static constexpr float LOWEST = -0x1.fep127f;
 };
 template <>
 struct TlType<__half> {
   static constexpr int LOW_BITS = 13;
   static constexpr int PER_WORD = 2;
   static constexpr uint32_t NEG_INF = 0xfc00fc00u;
+  static constexpr float LOWEST = -65504.0f;
 };
 
 __device__ __forceinline__ float tl_max_nan(float a, float b) {  // NaN if either is
@@ -1184,8 +1189,10 @@ __device__ __forceinline__ TlMark tl_conclude(const TlRows<E>& a, const TlTeache
   const double far = (static_cast<double>(ref) - r.m) * a.it + tl_shift(a, ref), part = sum == 0.0f ? 0.0 : static_cast<double>(sum) * exp(far);
   const double gap = __shfl_sync(0xffffffffu, far, 0), so = __shfl_sync(0xffffffffu, part, 0), sn = __shfl_sync(0xffffffffu, part, 1);
   double q_rest = o.tail && l.mass < 1.0 ? 1.0 - l.mass : 0.0;
-  const bool nothing = so == 0.0;  // outside: no logit, or p_r below what 64 bits hold (a mask of the type's lowest value)
-  if (o.tail && nothing && q_rest <= TL_REST_ROUNDING) q_rest = 0.0;
+  const bool below = so == 0.0;  // p_r, below what 64 bits hold; its logarithm need not be
+  // Outside: no logit, none within fp32's reach, or a mask of the type's lowest value.
+  const bool nothing = acc.S == 0.0f || (below && (acc.ref - r.m == -INFINITY || acc.ref == TlType<E>::LOWEST));
+  if (o.tail && below && q_rest <= TL_REST_ROUNDING) q_rest = 0.0;
   const double lg = log(lane == 0 ? so + sn : lane == 1 ? static_cast<double>(acc.S) : lane == 2 ? q_rest : l.mass);  // all that are needed, at once
   r.log_s = __shfl_sync(0xffffffffu, lg, 0);
   const double log_out = nothing ? -INFINITY : gap + __shfl_sync(0xffffffffu, lg, 1);

@@ -1,5 +1,5 @@
-"""Rows of logits on both sides of the limit up to which a kernel may use x = z c - R (|R| = 2^24), against the statement in 64 bits
-(tests/token_cases.py, which derives the bounds)."""
+"""Rows of logits where a number leaves its type: on both sides of the limit up to which a kernel may use x = z c - R (|R| = 2^24), factors of masked
+tokens' exponents, masses below what 64 bits hold; against the statement in 64 bits (tests/token_cases.py, which derives the bounds)."""
 import math
 
 import numpy as np
@@ -97,3 +97,76 @@ def test_large_entropy_terms_leave_masked_tokens_without_gradient(B, V, top, den
     ppo = B.ppo_token_loss(z.cuda(), torch.from_numpy(tokens).cuda(), old, one, beta=dent, temperature=tau)["dlogits"]
     B.poll_status()
     assert torch.isfinite(ppo).all() and not ppo[:, 1::3].any()
+
+
+def distill_with_tail(z, ids, values, tau, w, lowest):
+    """(loss, its error, dz, its error) of distill_topk with tail, p_r by its logarithm, so that it may lie below what 64 bits hold.  Bounds as those of
+    tc.Rows: S outside the names has its terms' errors, 6 |d| + 8 each, and its additions'; log p_r is a difference of 64-bit numbers beside those.
+    There, logits of the type's lowest value are a mask."""
+    T, V = z.shape
+    r = tc.Rows(z, tau)
+    loss, err_loss, dz, err_dz = np.zeros(T), np.zeros(T), np.zeros((T, V)), np.zeros((T, V))
+    with np.errstate(all="ignore"):
+        for t in range(T):
+            j, q = ids[t], np.exp(values[t].astype(np.float64))
+            outside = np.ones(V, bool)
+            outside[j] = False
+            rows = tc.Rows(np.where(outside, z[t], -INF)[None], tau)
+            gap = (rows.m[0] - r.m[t]) / tau
+            log_rest = gap + rows.log_s[0] - r.log_s[t]
+            q_rest = max(0.0, 1.0 - q.sum())
+            if log_rest < -745 and q_rest <= 2.0 ** -20:
+                q_rest = 0.0
+            masked = log_rest < -745 and rows.m[0] <= lowest
+            if masked:
+                log_rest = -INF
+            named = q * (values[t] - r.lp[t, j])
+            term = q_rest * (np.log(q_rest) - log_rest) if q_rest > 0 else 0.0
+            loss[t] = named.sum() + term
+            err_rest = rows.err_s[0] + r.err_log_s[t]
+            err_loss[t] = (q * r.err_lp[t, j]).sum() + 16 * tc.U * np.abs(named).sum() + q_rest * err_rest + (0.0 if masked else 2.0 ** -50 * abs(log_rest))
+            ratio = np.where(outside, 0.0 if masked else rows.p[0], 0.0)  # p_j / p_r
+            total = q.sum() + q_rest
+            g = total * r.p[t] - q_rest * ratio
+            np.subtract.at(g, j, q)
+            dz[t] = w[t] * g / tau
+            rel = np.where(rows.p[0] > 0, tc.U * (8 * np.abs(np.where(np.isfinite(rows.d[0]), rows.d[0], 0)) + 20) + rows.err_s[0], 0.0)
+            size = np.where(outside, total * r.p[t], 1.0)
+            err_dz[t] = w[t] / tau * (q_rest * ratio * (rel + 8 * tc.U) + size * (r.rel_p()[t] + 16 * tc.U) + 4 * tc.EXP_MIN)
+    return loss, err_loss, dz, err_dz
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16, F32])
+@pytest.mark.parametrize("T,V", [(8, 40), (8, 9000), (4, 128000), (1200, 300)])
+@pytest.mark.parametrize("tau,gap", [(1.0, 1e4), (0.05, 50.0), (2.0 ** -20, 3.0), (1.0, 700.0), (4.0, 1e4), (1.0, INF), (200.0, INF)])
+def test_distill_of_a_mass_outside_the_names_below_64_bits(B, T, V, dtype, tau, gap):
+    """Named tokens that lie far above all others (an additive mask of -10000, a low temperature): log p_r is a number as long as a logit is there that is no
+    mask, and the gradient outside the names follows it.  With the type's lowest value it is -inf."""
+    K = 5
+    g = torch.Generator().manual_seed(V)
+    z = torch.randn(T, V, generator=g) * tau
+    ids = torch.rand(T, V, generator=g).topk(K, 1).indices
+    named = z.gather(1, ids)
+    z = torch.full_like(z, torch.finfo(dtype).min) if gap == INF else z - gap
+    z = z.scatter(1, ids, named).to(dtype)
+    z[1::4, 7:] = torch.where(torch.rand(z[1::4, 7:].shape, generator=g) < 0.5, z[1::4, 7:], torch.tensor(-INF, dtype=dtype))  # some left out altogether
+    z = z.scatter(1, ids, named.to(dtype))
+    q = torch.softmax(torch.randn(T, K, generator=g).double(), 1) * torch.tensor([0.9, 0.3, 0.999, 1.0]).double().repeat(T // 4)[:, None]
+    ids, values, w = ids.numpy().astype(np.int32), q.log().float().numpy(), (np.linspace(0.5, 2.0, T) * min(1.0, tau)).astype(np.float32).astype(np.float64)
+    out = B.distill_topk(z.cuda(), torch.from_numpy(ids).cuda(), torch.from_numpy(values).cuda(), torch.tensor(w, dtype=F32).cuda(), tail=True, temperature=tau)
+    B.poll_status()
+    loss, el, dz, ed = distill_with_tail(tc.f64(z), ids, values, tau, w, torch.finfo(dtype).min)
+    tc.close(out["loss"], loss, el, what="loss")
+    tc.close(out["dlogits"], dz, ed, dtype, "gradient")
+
+
+def test_distill_of_a_student_that_leaves_out_all_but_the_names(B):
+    """-inf outside the names, and logits further below than fp32 reaches: p_r = 0, the loss +inf unless what the teacher has outside is rounding."""
+    z = torch.full((4, 300), -INF)
+    z[2:] = -3.4e38
+    z[:, :3] = torch.tensor([3e38, 2.9e38, 3e38])
+    values = torch.tensor([[0.3, 0.0, 0.3], [0.5, 0.0, 0.5], [0.3, 0.0, 0.3], [0.5, 0.0, 0.5]]).log()
+    out = B.distill_topk(z.cuda(), torch.tensor([[0, 1, 2]] * 4, dtype=torch.int32).cuda(), values.cuda(), tail=True)
+    B.poll_status()
+    assert torch.isposinf(out["loss"][[0, 2]]).all() and (out["loss"][[1, 3]].abs() < 8 * tc.U).all()
+    assert not out["dlogits"][:, 3:].any() and torch.isfinite(out["dlogits"]).all()
