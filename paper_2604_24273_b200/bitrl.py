@@ -850,14 +850,15 @@ def _per_row(t, dtype, name: str, index: int, shape):
 
 
 def _gradient_rows(dlogits, logits: torch.Tensor):
-    """(tensor, address, distance of its rows) of the gradient of ``logits``; where None is given it is allocated, as far as that is
-    not far apart with rows like those of the logits."""
+    """(tensor, address, distance of its rows) of the gradient of ``logits``; where None is given it is allocated, every row at the place
+    of its logits within 32 bytes (the kernels then write whole vectors), and rows as far apart unless the logits' are much further than V."""
     if dlogits is None:
         T, V = logits.shape
-        ld = logits.stride(0)
+        ld, size = logits.stride(0), logits.element_size()
         if T < 2 or ld - V >= 128:  # a block of a much wider matrix
-            ld = (V + 7) // 8 * 8
-        dlogits = torch.empty((T, ld), dtype=logits.dtype, device=logits.device)[:, :V]
+            ld = V + (ld - V) % (32 // size)
+        start = logits.data_ptr() % 32 // size
+        dlogits = torch.empty(start + T * ld, dtype=logits.dtype, device=logits.device).as_strided((T, V), (ld, 1), start)
     elif dlogits is not logits and (dlogits.dtype != logits.dtype or dlogits.shape != logits.shape):
         raise ValueError("dlogits must have the logits' shape and dtype")
     dst, _, _, _, ld, _ = _logit_rows(dlogits, "dlogits")
