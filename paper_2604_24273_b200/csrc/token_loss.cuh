@@ -11,7 +11,7 @@
 // What bounds it: memory where a row is read once (4096 x 128000 bf16: 161..171 us, 5.5..5.9 TB/s; its gradient from statistics: 98 % of the rate of a
 // copy).  An exponential and five to six other instructions fall on every element of a pass; at the rate of memory the special function unit has
 // 11 of its 16 exponentials a cycle to do, and under the power limit (1.5 GHz) 14, so that the second pass of the objectives makes arithmetic and
-// memory equals (PPO 4096 x 128000: 398..416 us, floor 309; distillation with 64 tokens and the tail 465..474).
+// memory equals (PPO 4096 x 128000: 398..416 us, floor 309; distillation with 64 tokens and the tail 465..481).
 //
 // Exponents are base 2: x_j = z_j c - R with c = log2(e) / temperature and R = c m rounded, one fused multiply-add per element.  That R
 // is rounded does not matter, as every x of a row has the same one; the results' scalars are made in 64 bits and add back the
@@ -1483,8 +1483,9 @@ bitrl_status tl_launch(int threads, long long ctas, int C, size_t smem, cudaStre
 //     others' reading (distillation's loss, 1000 x 50021: 32, by 256 threads 35, by 512 44).
 //   * Rows above 128 KB with a gradient: 512 threads.  They are read again behind their statistics, and the fewer rows are under way the more of
 //     that comes out of L2 (PPO 4096 x 128000: 402 by 512, 423 by 256, 452 by 128).
-//   * Few rows are cut into shares until three CTAs an SM have some, none below 256 vectors (PPO 20 x 128000: 33 whole, 8 in 8 shares; 100 x 32000:
-//     8.4 and 7.5 in 4).  Alternatives cost every share a selection: as many shares as SMs, none below 512 (16 x 32000: 8.8 whole, 14 in 16).
+//   * Few rows are cut into shares until three CTAs an SM have some, none below 256 vectors (PPO 20 x 128000: 22 whole, 8.0 in 8 shares, 7.9 in
+//     16; 1 x 128000: 22, 6.2 and 5.6; 100 x 32000: 8.4 and 7.5 in 4).  Alternatives cost every share a selection: as many shares as SMs, none below
+//     512 (16 x 32000: 8.8 whole, 14 in 16).
 enum TlKind { TL_TOP, TL_SUMS, TL_GRADIENT };
 struct TlPlan {
   int NT, C;
